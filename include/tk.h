@@ -295,6 +295,195 @@ tk_status tk_attn_decode_append(const tk_cache_desc* desc, const void* q, void* 
                                 int32_t max_seq_len, void* out, int32_t out_dtype, float scale,
                                 void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Between a projection and the attention (not part of the paper's method,
+ * whose q', k' and v arrive after any positional transform): per-head RMS norm
+ * and rotation of queries and keys, forward, backward and straight into the
+ * cache, and the page tables and slot maps of a paged cache.
+ * ------------------------------------------------------------------------ */
+
+#define TK_ROPE_MAX_PAIRS 64
+#define TK_ROPE_MAX_AXES 4
+/* Positions lie in [-2^24, 2^24]; others are clamped and recorded (code 1). */
+#define TK_ROPE_MAX_POSITION 16777216
+
+typedef enum tk_rope_layout {
+  TK_ROPE_HALF = 0, /* pair j = elements (j, j + rot_dim / 2)   */
+  TK_ROPE_PAIR = 1  /* pair j = elements (2j, 2j + 1)           */
+} tk_rope_layout;
+
+/* What a model fixes about its queries and keys.
+ *   r        : head width, in {16, 32, 64, 128}
+ *   rot_dim  : leading elements that are rotated, 0 .. r, a multiple of 8; the
+ *              others pass through
+ *   layout   : tk_rope_layout
+ *   n_axes   : position axes, 1 .. TK_ROPE_MAX_AXES (1 for text; e.g. row and
+ *              column for images; frame, row and column for video)
+ *   norm     : nonzero = RMS norm of each head's row before the rotation
+ *   eps      : added to the mean square (finite, > 0; unused without norm)
+ *   w_offset : added to the norm weights (1 for weights stored as w - 1)
+ *   inv_freq : angle of pair j = position[pair_axis[j]] * inv_freq[j];
+ *              finite, magnitude at most 4; the first rot_dim / 2 are used
+ *   pair_axis: axis of each pair, < n_axes: any split of the pairs over the
+ *              axes, in runs or interleaved                               */
+typedef struct tk_rope_desc {
+  int32_t r;
+  int32_t rot_dim;
+  int32_t layout;
+  int32_t n_axes;
+  int32_t norm;
+  float eps;
+  float w_offset;
+  float inv_freq[TK_ROPE_MAX_PAIRS];
+  uint8_t pair_axis[TK_ROPE_MAX_PAIRS];
+} tk_rope_desc;
+
+/* One tensor of heads: element (b, token, head, i) is data[b * batch_stride +
+ * token * token_stride + head * head_stride + i] of type dtype (TK_BF16 or
+ * TK_F32).  data is 16-byte aligned; the stride of every dimension longer than
+ * 1 is a multiple of 16 bytes and not negative, and, for a tensor that a call
+ * writes, keeps its rows apart.  A slice of a packed projection is such a
+ * tensor, and so are [batch][head][token][i] and [batch][token][head][i].   */
+typedef struct tk_heads {
+  void* data;
+  int32_t n_heads;
+  int32_t dtype;
+  int64_t batch_stride;
+  int64_t token_stride;
+  int64_t head_stride;
+} tk_heads;
+
+/* Norm and rotation of every head of q and k, in one launch with the layout
+ * change (and conversion) of v:
+ *   y = x (mean(x^2) + eps)^(-1/2) (w + w_offset)   (norm; w = 1 - w_offset if
+ *                                                    the weight is NULL)
+ *   (a, b) of pair j -> (a cos t - b sin t, a sin t + b cos t),
+ *   t = position[pair_axis[j]] * inv_freq[j]
+ * with the arithmetic in fp32 and one rounding, at the output.  The angle is
+ * reduced without rounding the product first, so it is as exact at position
+ * 10^6 as at 10 (absolute error of cos and sin below 2^-19).
+ *   q, k, v      : inputs of one dtype, d_v wide for v (d_v in {64, 128}); NULL
+ *                  (with its output) leaves that one out
+ *   q_weight, k_weight: device [r] of w_dtype, 16-byte aligned, or NULL
+ *   positions    : device int32, element (axis, b, token) at axis *
+ *                  pos_axis_stride + b * pos_batch_stride + token (a stride
+ *                  of 0 shares them); NULL only if rot_dim == 0
+ *   q_out, k_out, v_out: outputs of one dtype.  An output may be its own input
+ *                  (same address, dtype and strides); any other overlap is an
+ *                  error that is not detected.
+ * A row's result depends on that row, its token's positions and the weights
+ * alone: infinities and NaNs stay in their row, and a row of zeros gives
+ * zeros.  batch == 0 or seq == 0 is a no-op; batch * seq < 2^31.  Launched with
+ * programmatic dependent launch (see tk_attn_decode).                       */
+tk_status tk_qk_norm_rope(const tk_rope_desc* desc, int32_t batch, int32_t seq, int32_t d_v,
+                          const tk_heads* q, const tk_heads* k, const tk_heads* v,
+                          const void* q_weight, const void* k_weight, int32_t w_dtype,
+                          const int32_t* positions, int64_t pos_axis_stride,
+                          int64_t pos_batch_stride, const tk_heads* q_out, const tk_heads* k_out,
+                          const tk_heads* v_out, void* stream);
+
+/* tk_qk_norm_rope with k and v written to their cache slots instead:
+ * token (b, t)'s key and value of kv head g go to
+ *   paged      : page slots / page_size, row slots % page_size
+ *   contiguous : sequence slots / capacity, row slots % capacity
+ * with slots = slots[b * seq + t].  A negative slot caches nothing (its query
+ * is still written); a slot beyond the cache is not written and sets the
+ * device error word.  Two tokens must not share a slot.  (batch, seq) only
+ * arrange the step's tokens and need not match the cache's batch: packed
+ * requests of any lengths are batch 1.
+ *   cache   : h_q, h_kv, r and d_v agree with q, k, v and desc; no page table
+ *             is read
+ *   q, q_out: as above, q_out TK_BF16 (what decode and prefill read); both
+ *             NULL to cache keys and values alone.  k and v are required.
+ * bf16 keys and values are what tk_qk_norm_rope followed by tk_kv_append would
+ * store, bit for bit.  int8 / int4 keys use tk_kv_append's scheme on the fp32
+ * result of the rotation, without rounding it to bf16 first.               */
+tk_status tk_qk_norm_rope_append(const tk_cache_desc* cache, const tk_rope_desc* desc,
+                                 int32_t batch, int32_t seq, const tk_heads* q, const tk_heads* k,
+                                 const tk_heads* v, const void* q_weight, const void* k_weight,
+                                 int32_t w_dtype, const int32_t* positions,
+                                 int64_t pos_axis_stride, int64_t pos_batch_stride,
+                                 const int32_t* slots, const tk_heads* q_out, void* k_cache,
+                                 void* v_cache, float* k_scale, void* stream);
+
+/* Bytes of workspace tk_qk_norm_rope_backward needs for weight gradients on the
+ * current device; 0 for an invalid descriptor.  Zero-filled once before its
+ * first use; it holds an arrival counter, which every call leaves at zero,
+ * and partial sums, so it can be reused in stream order (never by two calls
+ * that may run concurrently).                                             */
+size_t tk_qk_norm_rope_workspace_size(const tk_rope_desc* desc);
+
+/* Gradients of tk_qk_norm_rope.  With g = the incoming gradient turned back by
+ * the token's angles, rho = (mean(x^2) + eps)^(-1/2), u = w + w_offset:
+ *   dw = sum over tokens and heads of g x rho,
+ *   dx = rho (g u - x rho^2 mean(g u x))       (without norm: dx = g)
+ *   q, k         : the forward's inputs (unused, may be NULL, without norm)
+ *   dq_out, dk_out, dv_out: gradients of its outputs, one dtype (TK_F32 as
+ *                  tk_attn_backward writes them, or TK_BF16); NULL (with its
+ *                  dq, dk, dv) leaves that one out
+ *   dq, dk, dv   : gradients of its inputs, of the inputs' dtype (written)
+ *   dq_weight, dk_weight: device fp32 [r] (overwritten), or NULL; norm only
+ *   workspace    : needed for a weight gradient
+ * Sums over rows are fp32 in an order fixed by the device's SM count: results
+ * repeat bit for bit.  One launch.  An empty call writes zero weight
+ * gradients.  Other arguments and errors as tk_qk_norm_rope.               */
+tk_status tk_qk_norm_rope_backward(const tk_rope_desc* desc, int32_t batch, int32_t seq,
+                                   int32_t d_v, const tk_heads* q, const tk_heads* k,
+                                   const void* q_weight, const void* k_weight, int32_t w_dtype,
+                                   const int32_t* positions, int64_t pos_axis_stride,
+                                   int64_t pos_batch_stride, const tk_heads* dq_out,
+                                   const tk_heads* dk_out, const tk_heads* dv_out,
+                                   const tk_heads* dq, const tk_heads* dk, const tk_heads* dv,
+                                   float* dq_weight, float* dk_weight, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* Pages, slots and positions of a step's new tokens in a paged cache, from
+ * request lengths, on the device and in one launch.
+ *   seq_lens  : device int32 [batch], tokens cached per sequence; its pages are
+ *               the first ceil(seq_lens / page_size) of its page_table row
+ *   new_lens  : device int32 [batch], tokens to add: 0 = idle, -1 = the
+ *               request is finished and gives its pages back
+ *   page_table: device int32 [batch][max_pages_per_seq], entries of pages
+ *               taken by this call are written, no others
+ *   free_pages: device int32 [num_pages], a stack of page ids, its bottom
+ *               free_count entries in use
+ *   free_count: device int32 [1]
+ *   tokens_per_seq: rows of each sequence in the slot map, or 0 for packed
+ *   rows      : rows of the slot map: batch * tokens_per_seq, or (packed) a
+ *               bound of the step's tokens
+ *   slots, positions: device int32 [rows], 16-byte aligned: token t of sequence
+ *               b, at row b * tokens_per_seq + t or token_offsets[b] + t, has
+ *               position seq_lens[b] + t and slot page * page_size + position
+ *               % page_size; rows without a token have slot -1, position 0
+ *   token_offsets: device int32 [batch + 1] or NULL: first row of each
+ *               sequence when packed, and the number of granted tokens
+ *   seq_lens_out: device int32 [batch]: lengths after the step (0 for finished
+ *               requests); may be seq_lens
+ *   free_count_out: device int32 [1]; may be free_count
+ *   refused   : device int32 [1] or NULL: requests that were refused
+ *   workspace : 4 bytes of device memory, zero before the first call, left
+ *               at zero (never shared by calls that may run concurrently)
+ * First the finished requests' pages are pushed on the stack, in order of
+ * sequence and page.  Then requests are served in order, each wholly or not at
+ * all: page i of the step's is popped from the top.  A request is refused if
+ * it exceeds the page table's row or the slot map (its tokens_per_seq, or,
+ * packed, the requested tokens up to and with it exceed rows), or if it
+ * needs pages and the needs of the accepted requests up to and with it exceed
+ * the free pages; a refused request keeps its pages and length and gets no
+ * slots.  Lengths below 0 or beyond the row, counts below -1, a free count
+ * or a page id out of range set the device error word (the request is
+ * refused; tokens on a bad page get slot -1).
+ * page_size as in tk_cache_desc; batch <= 4096; num_pages * page_size,
+ * max_pages_per_seq * page_size and batch * max_pages_per_seq at most 2^30.
+ * Launched with programmatic dependent launch.                             */
+tk_status tk_block_tables(int32_t batch, int32_t page_size, int32_t num_pages,
+                          int32_t max_pages_per_seq, const int32_t* seq_lens,
+                          const int32_t* new_lens, int32_t* page_table, int32_t* free_pages,
+                          const int32_t* free_count, int32_t tokens_per_seq, int32_t rows,
+                          int32_t* slots, int32_t* positions, int32_t* token_offsets,
+                          int32_t* seq_lens_out, int32_t* free_count_out, int32_t* refused,
+                          void* workspace, void* stream);
+
 /* Stream-ordered copy of `bytes` bytes between any two of device memory and
  * page-locked host memory (cudaMemcpyAsync with the direction taken from the
  * pointers), for serving loops that bring a step's inputs from the host:

@@ -18,6 +18,8 @@ import torch
 
 TK_OK, TK_ERR_INVALID_ARG, TK_ERR_UNSUPPORTED, TK_ERR_WORKSPACE, TK_ERR_CUDA, TK_ERR_DEVICE = range(6)
 TK_BF16, TK_F32, TK_I8, TK_I4 = 0, 1, 2, 3
+TK_ROPE_HALF, TK_ROPE_PAIR = 0, 1
+TK_ROPE_MAX_PAIRS, TK_ROPE_MAX_AXES = 64, 4
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtk.so")
 
@@ -25,6 +27,8 @@ EXPORTED = ("tk_kv_append", "tk_attn_prefill", "tk_decode_workspace_size", "tk_a
             "tk_attn_decode_append", "tk_attn_decode_noalloc", "tk_attn_prefill_cached",
             "tk_prefill_cached_workspace_size",
             "tk_attn_forward", "tk_backward_workspace_size", "tk_attn_backward", "tk_copy_async",
+            "tk_qk_norm_rope", "tk_qk_norm_rope_append", "tk_qk_norm_rope_backward",
+            "tk_qk_norm_rope_workspace_size", "tk_block_tables",
             "tk_check_wait_timeout", "tk_get_device_error", "tk_status_string", "tk_last_error",
             "tk_abi_version", "tk_graph_begin", "tk_graph_end", "tk_graph_launch",
             "tk_graph_destroy")
@@ -42,6 +46,19 @@ class tk_cache_desc(ctypes.Structure):
         "max_pages_per_seq", "k_dtype")]
 
 
+class tk_rope_desc(ctypes.Structure):
+    """What a model fixes about its queries and keys (include/tk.h); see rope_plan."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("r", "rot_dim", "layout", "n_axes", "norm")]
+                + [("eps", ctypes.c_float), ("w_offset", ctypes.c_float),
+                   ("inv_freq", ctypes.c_float * TK_ROPE_MAX_PAIRS),
+                   ("pair_axis", ctypes.c_uint8 * TK_ROPE_MAX_PAIRS)])
+
+
+class tk_heads(ctypes.Structure):
+    _fields_ = ([("data", ctypes.c_void_p), ("n_heads", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+                + [(n, ctypes.c_int64) for n in ("batch_stride", "token_stride", "head_stride")])
+
+
 _lib = None
 
 
@@ -55,7 +72,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                            "(or __graft_entry__.build()) first")
     L = ctypes.CDLL(path)
     vp, i32, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
-    dp = ctypes.POINTER(tk_cache_desc)
+    i64 = ctypes.c_int64
+    dp, rp, hp = (ctypes.POINTER(t) for t in (tk_cache_desc, tk_rope_desc, tk_heads))
     sig = {
         "tk_kv_append": (i32, [dp, vp, vp, vp, vp, vp, vp, vp, i32, vp]),
         "tk_attn_prefill": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, f32, i32, vp]),
@@ -72,6 +90,15 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "tk_attn_decode_append": (i32, [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, f32, vp,
                                         sz, vp]),
         "tk_attn_decode_noalloc": (i32, [dp, vp, vp, vp, vp, vp, vp, i32, vp, i32, f32, vp]),
+        "tk_qk_norm_rope": (i32, [rp, i32, i32, i32, hp, hp, hp, vp, vp, i32, vp, i64, i64, hp, hp,
+                                  hp, vp]),
+        "tk_qk_norm_rope_append": (i32, [dp, rp, i32, i32, hp, hp, hp, vp, vp, i32, vp, i64, i64,
+                                         vp, hp, vp, vp, vp, vp]),
+        "tk_qk_norm_rope_workspace_size": (sz, [rp]),
+        "tk_qk_norm_rope_backward": (i32, [rp, i32, i32, i32, hp, hp, vp, vp, i32, vp, i64, i64,
+                                           hp, hp, hp, hp, hp, hp, vp, vp, vp, sz, vp]),
+        "tk_block_tables": (i32, [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp,
+                                  vp, vp, vp, vp]),
         "tk_get_device_error": (i32, [ctypes.POINTER(i32), vp]),
         "tk_check_wait_timeout": (i32, [i32, vp]),
         "tk_copy_async": (i32, [vp, vp, sz, vp]),
@@ -470,6 +497,280 @@ def prepare_decode_append(cache: ThinKeyCache, q, k_new, v_new, seq_lens, max_se
     return PreparedCall("tk_attn_decode_append", args,
                         (cache, q, k_new, v_new, seq_lens, out, workspace) + keep_in, before,
                         graph=graph, stream=stream)
+
+
+# ------------------------------------------------- between a projection and the attention
+
+def rope_plan(r: int, rot_dim: int | None = None, layout: str = "half", base: float = 10000.0,
+              axes=None, inv_freq=None, pair_axis=None, norm: bool = True, eps: float = 1e-6,
+              w_offset: float = 0.0) -> tk_rope_desc:
+    """The rotation and norm of a model's queries and keys, built once.
+
+    rot_dim leading elements of a head are rotated (default all r), as pairs (j, j + rot_dim/2)
+    (layout "half") or (2j, 2j+1) ("pair").  Frequencies: one position axis and
+    base^(-j/pairs) by default; axes=(n0, n1, ...) gives each position axis a run of so many
+    pairs with frequencies base^(-i/n) of its own; inv_freq and pair_axis set both freely
+    (one entry per pair), e.g. scaled frequencies or axes interleaved over the pairs."""
+    rot = r if rot_dim is None else int(rot_dim)
+    pairs = rot // 2
+    if layout not in ("half", "pair"):
+        raise ValueError(f"layout must be 'half' or 'pair', got {layout!r}")
+    if axes is not None and inv_freq is not None:
+        raise ValueError("axes and inv_freq are exclusive")
+    if inv_freq is None:
+        runs = tuple(axes) if axes is not None else (pairs,)
+        if any(n < 0 for n in runs) or sum(runs) != pairs:
+            raise ValueError(f"axes {runs} do not add up to {pairs} pairs")
+        inv_freq = [base ** (-i / n) for n in runs for i in range(n)]
+        if pair_axis is None:
+            pair_axis = [a for a, n in enumerate(runs) for _ in range(n)]
+    inv_freq = [float(f) for f in inv_freq]
+    pair_axis = [0] * pairs if pair_axis is None else [int(a) for a in pair_axis]
+    if len(inv_freq) != pairs or len(pair_axis) != pairs or pairs > TK_ROPE_MAX_PAIRS:
+        raise ValueError(f"{len(inv_freq)} frequencies and {len(pair_axis)} axes for {pairs} pairs "
+                         f"(at most {TK_ROPE_MAX_PAIRS})")
+    if any(not 0 <= a < TK_ROPE_MAX_AXES for a in pair_axis):
+        raise ValueError(f"pair_axis entries must be in 0 .. {TK_ROPE_MAX_AXES - 1}")
+    d = tk_rope_desc(r, rot, TK_ROPE_HALF if layout == "half" else TK_ROPE_PAIR,
+                     max(pair_axis, default=0) + 1, 1 if norm else 0, eps, w_offset)
+    d.inv_freq[:pairs] = inv_freq
+    d.pair_axis[:pairs] = pair_axis
+    return d
+
+
+def _heads(t, name, shape, device):
+    """A tensor of logical shape [B, H, S, width], any strides with the width contiguous."""
+    if t is None:
+        return None
+    if t.dtype is torch.bfloat16:
+        dt = TK_BF16
+    elif t.dtype is torch.float32:
+        dt = TK_F32
+    else:
+        raise TypeError(f"{name} must be float32 or bfloat16")
+    if t.device != device or not t.is_cuda:
+        raise ValueError(f"{name} is on {t.device}, expected {device} (CUDA)")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} is {tuple(t.shape)}, expected {shape}")
+    sb, sh, st, sw = t.stride()
+    if sw != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    return tk_heads(t.data_ptr(), shape[1], dt, sb, st, sh)
+
+
+def _weights(plan, q_weight, k_weight, device):
+    dts = {t.dtype for t in (q_weight, k_weight) if t is not None}
+    if len(dts) > 1 or not dts <= {torch.float32, torch.bfloat16}:
+        raise TypeError("norm weights must be float32 or bfloat16, both alike")
+    for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if t is not None:
+            _need(t, t.dtype, n, device)
+            if t.numel() != plan.r:
+                raise ValueError(f"{n} has {t.numel()} elements, expected {plan.r}")
+    return TK_BF16 if torch.bfloat16 in dts else TK_F32
+
+
+def _positions(plan, positions, B, S, device):
+    """(pointer, axis stride, batch stride) of positions [B, S] or [n_axes, B, S] int32."""
+    if positions is None:
+        return None, 0, 0
+    if positions.dtype is not torch.int32 or positions.device != device:
+        raise TypeError(f"positions must be int32 on {device}")
+    if positions.dim() == 2:
+        positions = positions.unsqueeze(0).expand(plan.n_axes, *positions.shape)
+    if tuple(positions.shape) != (plan.n_axes, B, S):
+        raise ValueError(f"positions are {tuple(positions.shape)}, expected {(plan.n_axes, B, S)} or {(B, S)}")
+    sa, sb, st = positions.stride()
+    if st != 1 and S > 1:
+        raise ValueError("positions must be contiguous along the tokens")
+    return ctypes.c_void_p(positions.data_ptr()), sa, sb
+
+
+def _ref(h):
+    return None if h is None else ctypes.byref(h)
+
+
+def _dims(*tensors):
+    for t in tensors:
+        if t is not None:
+            if t.dim() != 4:
+                raise ValueError(f"expected [B, H, S, width] tensors, got {tuple(t.shape)}")
+            return t.shape[0], t.shape[2], t.device
+    raise ValueError("q, k and v are all None")
+
+
+def _shape(t, B, S, width):
+    return None if t is None else (B, t.shape[1], S, width)
+
+
+def tk_qk_norm_rope(plan: tk_rope_desc, q, k, v, positions, q_out, k_out, v_out, q_weight=None,
+                    k_weight=None, stream=None):
+    """Per-head RMS norm and rotation of q [B, H_q, S, r] and k [B, H_kv, S, r], and the layout
+    change of v [B, H_kv, S, d_v], in one launch.  Tensors are [B, H, S, width] with any strides
+    (a transposed slice of a packed projection, say); bf16 or fp32 in and out.  positions int32
+    [B, S] or [n_axes, B, S].  Any of the three may be None together with its output."""
+    B, S, dev = _dims(q, k, v)
+    dv = 0 if v is None else v.shape[3]
+    sq, sk, sv = _shape(q, B, S, plan.r), _shape(k, B, S, plan.r), _shape(v, B, S, dv)
+    hs = [_heads(t, n, s, dev) for t, n, s in (
+        (q, "q", sq), (k, "k", sk), (v, "v", sv), (q_out, "q_out", sq), (k_out, "k_out", sk),
+        (v_out, "v_out", sv))]
+    wd = _weights(plan, q_weight, k_weight, dev)
+    pos = _positions(plan, positions, B, S, dev)
+    _check(load_library().tk_qk_norm_rope(
+        ctypes.byref(plan), B, S, dv, _ref(hs[0]), _ref(hs[1]), _ref(hs[2]), _ptr(q_weight),
+        _ptr(k_weight), wd, *pos, _ref(hs[3]), _ref(hs[4]), _ref(hs[5]), _stream(stream)),
+        "tk_qk_norm_rope")
+    return q_out, k_out, v_out
+
+
+def _append_args(cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight, stream):
+    """Checked and marshalled arguments of tk_qk_norm_rope_append, and what they point into."""
+    d = cache.desc
+    B, S, dev = _dims(k)
+    if v is None or v.dim() != 4:
+        raise ValueError("k and v are required")
+    sq, sk = (B, d.h_q, S, plan.r), (B, d.h_kv, S, plan.r)
+    hq, ho = _heads(q, "q", sq, dev), _heads(q_out, "q_out", sq, dev)
+    hk, hv = _heads(k, "k", sk, dev), _heads(v, "v", (B, d.h_kv, S, d.d_v), dev)
+    _need(slots, torch.int32, "slots", dev)
+    if slots.numel() != B * S:
+        raise ValueError(f"slots has {slots.numel()} entries for {B * S} tokens")
+    for t, n in ((cache.k, "cache.k"), (cache.v, "cache.v"), (cache.k_scale, "cache.k_scale")):
+        if t is not None and t.device != dev:
+            raise ValueError(f"{n} is on {t.device}, expected {dev}")
+    wd = _weights(plan, q_weight, k_weight, dev)
+    pos = _positions(plan, positions, B, S, dev)
+    args = (ctypes.byref(d), ctypes.byref(plan), B, S, _ref(hq), _ref(hk), _ref(hv), _ptr(q_weight),
+            _ptr(k_weight), wd, *pos, _ptr(slots), _ref(ho), _ptr(cache.k), _ptr(cache.v),
+            _ptr(cache.k_scale), _stream(stream))
+    return args, (cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight, hq, hk, hv, ho)
+
+
+def tk_qk_norm_rope_append(cache: ThinKeyCache, plan: tk_rope_desc, q, k, v, positions, slots, q_out,
+                           q_weight=None, k_weight=None, stream=None):
+    """tk_qk_norm_rope with k and v written to the cache at slots [B, S] int32 (tk_block_tables
+    makes them; negative = not cached) and q to q_out [B, H_q, S, r] bf16.  q and q_out may be None."""
+    args, _keep = _append_args(cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight, stream)
+    _check(load_library().tk_qk_norm_rope_append(*args), "tk_qk_norm_rope_append")
+    return q_out
+
+
+def prepare_qk_norm_rope_append(cache: ThinKeyCache, plan: tk_rope_desc, q, k, v, positions, slots, q_out,
+                                q_weight=None, k_weight=None, stream=None,
+                                graph: bool = False) -> PreparedCall:
+    """tk_qk_norm_rope_append on fixed buffers, checked and marshalled once (see PreparedCall)."""
+    args, keep = _append_args(cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight, stream)
+    return PreparedCall("tk_qk_norm_rope_append", args, keep, graph=graph, stream=stream)
+
+
+def qk_norm_rope_workspace(plan: tk_rope_desc, device="cuda") -> torch.Tensor:
+    """A zero-filled workspace of the size tk_qk_norm_rope_backward needs for weight gradients."""
+    n = int(load_library().tk_qk_norm_rope_workspace_size(ctypes.byref(plan)))
+    if n == 0:
+        raise TkError(TK_ERR_INVALID_ARG, "tk_qk_norm_rope_workspace_size", tk_last_error())
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def tk_qk_norm_rope_backward(plan: tk_rope_desc, q, k, positions, dq_out, dk_out, dv_out, dq, dk, dv,
+                             q_weight=None, k_weight=None, dq_weight=None, dk_weight=None,
+                             workspace=None, stream=None):
+    """Gradients of tk_qk_norm_rope: from dq_out, dk_out, dv_out (gradients of its outputs, fp32 as
+    tk_attn_backward writes them, or bf16) to dq, dk, dv (the inputs' dtype, any strides: slices of
+    a packed gradient, say) and the weights' dq_weight, dk_weight [r] fp32.  q and k (the
+    forward's inputs) may be None for a plan without norm.  Weight gradients need a workspace
+    (qk_norm_rope_workspace; allocated here if None)."""
+    B, S, dev = _dims(dq_out, dk_out, dv_out)
+    width = 0 if dv_out is None else dv_out.shape[3]
+    sq, sk, sv = _shape(dq_out, B, S, plan.r), _shape(dk_out, B, S, plan.r), _shape(dv_out, B, S, width)
+    if not plan.norm:
+        q = k = None
+    hs = [_heads(t, n, s, dev) for t, n, s in (
+        (q, "q", sq), (k, "k", sk), (dq_out, "dq_out", sq), (dk_out, "dk_out", sk), (dv_out, "dv_out", sv),
+        (dq, "dq", sq), (dk, "dk", sk), (dv, "dv", sv))]
+    wd = _weights(plan, q_weight, k_weight, dev)
+    for t, n in ((dq_weight, "dq_weight"), (dk_weight, "dk_weight")):
+        _need(t, torch.float32, n, dev)
+        if t is not None and t.numel() != plan.r:
+            raise ValueError(f"{n} has {t.numel()} elements, expected {plan.r}")
+    if workspace is None and (dq_weight is not None or dk_weight is not None):
+        workspace = qk_norm_rope_workspace(plan, dev)
+    _need(workspace, torch.uint8, "workspace", dev)
+    pos = _positions(plan, positions, B, S, dev)
+    _check(load_library().tk_qk_norm_rope_backward(
+        ctypes.byref(plan), B, S, width, _ref(hs[0]), _ref(hs[1]), _ptr(q_weight), _ptr(k_weight), wd, *pos,
+        *(_ref(h) for h in hs[2:]), _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream(stream)), "tk_qk_norm_rope_backward")
+    return dq, dk, dv
+
+
+@dataclass
+class PagePool:
+    """The page tables of a batch and the free pages of a paged cache (all int32, on one device).
+
+    page_table [B, max_pages], free_pages [num_pages] with its first free_count[0] entries in
+    use, free_count [1], seq_lens [B] tokens cached per sequence, workspace [1] (zero)."""
+    page_size: int
+    page_table: torch.Tensor
+    free_pages: torch.Tensor
+    free_count: torch.Tensor
+    seq_lens: torch.Tensor
+    workspace: torch.Tensor
+
+    @staticmethod
+    def allocate(batch, max_pages, page_size, num_pages, device="cuda"):
+        """An empty pool: every page free, every sequence empty."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return PagePool(page_size, torch.full((batch, max_pages), -1, **i32),
+                        torch.arange(num_pages - 1, -1, -1, **i32), torch.full((1,), num_pages, **i32),
+                        torch.zeros(batch, **i32), torch.zeros(1, **i32))
+
+
+def _table_args(pool, new_lens, slots, positions, tokens_per_seq, offsets, seq_lens_out, free_count_out,
+                refused, stream):
+    dev = pool.page_table.device
+    if pool.page_table.dim() != 2:
+        raise ValueError("page_table must be [B, max_pages]")
+    B, max_pages = pool.page_table.shape
+    seq_lens_out = pool.seq_lens if seq_lens_out is None else seq_lens_out
+    free_count_out = pool.free_count if free_count_out is None else free_count_out
+    num_pages, rows = pool.free_pages.numel(), slots.numel()
+    for t, n, size in ((pool.page_table, "page_table", B * max_pages), (pool.free_pages, "free_pages", num_pages),
+                       (pool.free_count, "free_count", 1), (pool.seq_lens, "seq_lens", B),
+                       (pool.workspace, "workspace", 1), (new_lens, "new_lens", B), (slots, "slots", rows),
+                       (positions, "positions", rows), (offsets, "offsets", B + 1),
+                       (seq_lens_out, "seq_lens_out", B), (free_count_out, "free_count_out", 1),
+                       (refused, "refused", 1)):
+        _need(t, torch.int32, n, dev)
+        if t is not None and t.numel() != size:
+            raise ValueError(f"{n} has {t.numel()} elements, expected {size}")
+    args = (B, pool.page_size, num_pages, max_pages, _ptr(pool.seq_lens), _ptr(new_lens), _ptr(pool.page_table),
+            _ptr(pool.free_pages), _ptr(pool.free_count), int(tokens_per_seq), rows, _ptr(slots),
+            _ptr(positions), _ptr(offsets), _ptr(seq_lens_out), _ptr(free_count_out), _ptr(refused),
+            _ptr(pool.workspace), _stream(stream))
+    return args, (pool, new_lens, slots, positions, offsets, seq_lens_out, free_count_out, refused)
+
+
+def tk_block_tables(pool: PagePool, new_lens, slots, positions, tokens_per_seq: int = 0, offsets=None,
+                    seq_lens_out=None, free_count_out=None, refused=None, stream=None):
+    """Pages, slots and positions of a step's new tokens: new_lens [B] int32 per sequence (0 idle,
+    -1 finished: its pages are freed) -> the pool's page table and free stack updated, slots
+    and positions [rows] filled (padded [B, tokens_per_seq], or packed by offsets [B + 1] when
+    tokens_per_seq is 0).  seq_lens and free_count are updated in place unless outputs are given;
+    refused [1] counts requests that did not fit (their length stays).  See include/tk.h."""
+    args, _keep = _table_args(pool, new_lens, slots, positions, tokens_per_seq, offsets, seq_lens_out,
+                              free_count_out, refused, stream)
+    _check(load_library().tk_block_tables(*args), "tk_block_tables")
+    return slots, positions
+
+
+def prepare_block_tables(pool: PagePool, new_lens, slots, positions, tokens_per_seq: int = 0, offsets=None,
+                         seq_lens_out=None, free_count_out=None, refused=None, stream=None,
+                         graph: bool = False) -> PreparedCall:
+    """tk_block_tables on fixed buffers, checked and marshalled once (see PreparedCall)."""
+    args, keep = _table_args(pool, new_lens, slots, positions, tokens_per_seq, offsets, seq_lens_out,
+                             free_count_out, refused, stream)
+    return PreparedCall("tk_block_tables", args, keep, graph=graph, stream=stream)
 
 
 def tk_attn_prefill(q, k, v, out, scale: float | None = None, causal: bool = True, stream=None):

@@ -1,0 +1,272 @@
+// Per-head RMS norm and rotation of queries and keys in one pass, from the
+// projection's token-major rows to the layout the attention reads, or (k and
+// v) straight into the cache.
+//
+//   y = x (mean(x^2) + eps)^(-1/2) (w + w_offset),
+//   (a, b) of pair j -> (a cos t - b sin t, a sin t + b cos t),
+//   t = position[axis j] * inv_freq[j]
+//
+// Nothing is computed twice and every element is read and written once, so
+// the bound is HBM for long prompts and the launch for single tokens.
+//
+// A warp takes the 256 / r tokens that fit its lanes (qk_row.cuh) and a run
+// of up to 8 heads: the run's rows are all loaded before the first is used
+// (8 x 512 bytes in flight per warp, which is what covers HBM's latency), and
+// the token's angles are computed once for the run.  Lanes of one store
+// instruction then hold neighbouring tokens of one head, which is the
+// contiguous direction of the head-major output.  Values are copied by
+// further runs of the same launch.
+#include <type_traits>
+
+#include "kernels.h"
+#include "qk_row.cuh"
+
+namespace tk {
+namespace {
+
+constexpr int kWarps = 4;
+
+// The cache row of kv head g for a slot: block = page or sequence.
+struct SlotRow {
+  int64_t block_row;   // block * h_kv * rows + offset
+  bool ok;
+};
+__device__ __forceinline__ SlotRow slot_row(const QkParams& p, uint32_t token, bool token_ok) {
+  SlotRow r{0, false};
+  if (!token_ok) return r;
+  const int slot = p.slots[token];
+  if (slot < 0) return r;              // no slot: the token is not cached
+  if (slot >= p.slot_limit) {
+    record_error(p.err, TK_DEVERR_INDEX);
+    return r;
+  }
+  uint32_t off;
+  const uint32_t block = p.div_rows.divmod(static_cast<uint32_t>(slot), &off);
+  r.block_row = static_cast<int64_t>(block) * p.k.n * p.slot_rows + off;
+  r.ok = true;
+  return r;
+}
+
+// A lane's eight key elements as codes: symmetric absmax per (token, kv head),
+// scale = amax / Q, code = clamp(rint(y / scale), -Q, Q), both divisions in
+// IEEE binary32, amax 0 storing scale 0 and zero codes.  y is the fp32 result
+// of the rotation, not rounded to bf16 first: one rounding less than an
+// append of bf16 keys makes.
+template <int R, int KF>
+__device__ __forceinline__ void store_codes(const QkParams& p, int64_t row, bool ok, int sub, int oa,
+                                            int ob, const float* y) {
+  float amax = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[e]));
+  amax = row_max<R / 8>(amax);
+  if (!ok) return;
+  constexpr float Q = KF == 1 ? 127.0f : 7.0f;
+  const float scale = amax / Q;
+  int code[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float cf = 0.f;
+    if (scale != 0.f) cf = fminf(fmaxf(rintf(y[e] / scale), -Q), Q);
+    code[e] = static_cast<int>(cf);
+  }
+  unsigned char* k = static_cast<unsigned char*>(p.k_cache);
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int* c = code + 4 * half;
+    const int o = half ? ob : oa;      // a multiple of 4
+    if constexpr (KF == 1) {
+      *reinterpret_cast<uint32_t*>(k + row * R + o) =
+          (c[0] & 0xFF) | (c[1] & 0xFF) << 8 | (c[2] & 0xFF) << 16 | static_cast<uint32_t>(c[3] & 0xFF) << 24;
+    } else {
+      *reinterpret_cast<uint16_t*>(k + row * (R / 2) + o / 2) = static_cast<uint16_t>(
+          (c[0] & 0xF) | (c[1] & 0xF) << 4 | (c[2] & 0xF) << 8 | (c[3] & 0xF) << 12);
+    }
+  }
+  if (sub == 0) p.k_scale[row] = scale;
+}
+
+// Eight neighbouring elements, converted from X to O; equal types are copied bit for bit.
+template <typename X, typename O>
+struct Piece {
+  Raw<X> r;
+  __device__ __forceinline__ void load(const X* s) {
+    if constexpr (sizeof(X) == 2) {
+      const uint4 w = *reinterpret_cast<const uint4*>(s);
+      r.a = make_uint2(w.x, w.y);
+      r.b = make_uint2(w.z, w.w);
+    } else {
+      r.load(s, 0, 4);
+    }
+  }
+  __device__ __forceinline__ void store(O* d) const {
+    if constexpr (std::is_same<X, O>::value && sizeof(X) == 2) {
+      *reinterpret_cast<uint4*>(d) = make_uint4(r.a.x, r.a.y, r.b.x, r.b.y);
+    } else {
+      float y[8];
+      r.get(y);
+      if constexpr (sizeof(O) == 2)
+        *reinterpret_cast<uint4*>(d) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]),
+                                                  pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+      else
+        store_quads(d, 0, 4, y);
+    }
+  }
+};
+
+// KF: -1 = k and v go to strided tensors of type O, else to the cache with key
+// format KF (0 bf16, 1 int8, 2 int4).
+template <int R, typename X, typename O, int KF>
+__global__ void __launch_bounds__(kWarps * 32) norm_rope_kernel(const __grid_constant__ QkParams p) {
+  constexpr int G = R / 8, T = 32 / G;
+  constexpr int H = sizeof(X) == 2 ? 8 : 4;      // rows a lane holds at a time
+  const int lane = threadIdx.x & 31;
+  const uint32_t unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  if (unit >= p.units) return;
+  uint32_t run;
+  const uint32_t group = p.div_runs.divmod(unit, &run);
+  pdl_wait();
+  pdl_trigger();
+
+  if (run < static_cast<uint32_t>(p.nq + p.nk)) {
+    const int sub = lane % G;
+    const uint32_t token = group * T + lane / G;
+    const bool ok = token < p.n_tokens;
+    uint32_t s;
+    const uint32_t b = p.div_s.divmod(ok ? token : 0u, &s);
+    const bool is_q = run < static_cast<uint32_t>(p.nq);
+    const HeadsView in = is_q ? p.q : p.k;
+    const int per = is_q ? p.hq_run : p.hk_run;
+    const int h0 = static_cast<int>(is_q ? run : run - p.nq) * per;
+    const int nh = min(per, in.n - h0);
+    int oa, ob;
+    quad_offsets(sub, p.rot, p.pair_layout, &oa, &ob);
+    const X* src = static_cast<const X*>(in.p) + b * in.sb + s * in.st + h0 * in.sh;
+    Raw<X> raw[H];
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+      raw[i].zero();
+      if (ok && i < nh) raw[i].load(src + i * in.sh, oa, ob);
+    }
+    SlotRow slot{0, false};
+    if (KF >= 0 && !is_q) slot = slot_row(p, token, ok);
+    float w[8];
+    if (p.norm) load_weights(is_q ? p.wq : p.wk, p.w_f32, p.w_offset, oa, ob, w);
+    const Turns t = load_turns(p, sub, b, s, ok);
+    const HeadsView out = is_q ? p.qo : p.ko;
+    O* dst = static_cast<O*>(out.p) + b * out.sb + s * out.st + h0 * out.sh;
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+      if (i >= nh) break;
+      float y[8];
+      raw[i].get(y);
+      if (p.norm) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = __fmaf_rn(y[e], y[e], ss);
+        const float rho = rsqrtf(__fmaf_rn(row_sum<G>(ss), 1.0f / R, p.eps));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __fmul_rn(__fmul_rn(y[e], rho), w[e]);
+      }
+      rotate8(y, t, p.pair_layout, false);
+      if (KF < 0 || is_q) {
+        if (ok) store_quads(dst + i * out.sh, oa, ob, y);
+      } else {
+        const int64_t row = slot.block_row + static_cast<int64_t>(h0 + i) * p.slot_rows;
+        if constexpr (KF <= 0) {
+          if (slot.ok) store_quads(static_cast<__nv_bfloat16*>(p.k_cache) + row * R, oa, ob, y);
+        } else {
+          store_codes<R, KF>(p, row, slot.ok, sub, oa, ob, y);
+        }
+      }
+    }
+    return;
+  }
+
+  // values: the group's tokens x a run of heads, as 8-element pieces
+  constexpr int log_t = T == 16 ? 4 : T == 8 ? 3 : T == 4 ? 2 : 1;
+  const int log_c = p.DV == 128 ? 4 : 3;
+  const int h0 = static_cast<int>(run - p.nq - p.nk) * p.hv_run;
+  const int nh = min(p.hv_run, p.v.n - h0);
+  const int pieces = nh << (log_t + log_c);
+  for (int c0 = lane; c0 < pieces; c0 += 32 * H) {
+    Piece<X, O> piece[H];
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+      const int c = c0 + 32 * i;
+      const uint32_t token = group * T + ((c >> log_c) & (T - 1));
+      if (c < pieces && token < p.n_tokens) {
+        uint32_t s;
+        const uint32_t b = p.div_s.divmod(token, &s);
+        piece[i].load(static_cast<const X*>(p.v.p) + b * p.v.sb + s * p.v.st +
+                      (h0 + (c >> (log_c + log_t))) * p.v.sh + 8 * (c & ((1 << log_c) - 1)));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+      const int c = c0 + 32 * i;
+      const uint32_t token = group * T + ((c >> log_c) & (T - 1));
+      const bool ok = c < pieces && token < p.n_tokens;
+      const int h = h0 + (c >> (log_c + log_t));
+      const int col = 8 * (c & ((1 << log_c) - 1));
+      if constexpr (KF < 0) {
+        if (ok) {
+          uint32_t s;
+          const uint32_t b = p.div_s.divmod(token, &s);
+          piece[i].store(static_cast<O*>(p.vo.p) + b * p.vo.sb + s * p.vo.st + h * p.vo.sh + col);
+        }
+      } else {
+        const SlotRow slot = slot_row(p, token, ok);
+        if (slot.ok)
+          piece[i].store(static_cast<O*>(p.v_cache) +
+                         (slot.block_row + static_cast<int64_t>(h) * p.slot_rows) * p.DV + col);
+      }
+    }
+  }
+}
+
+template <int R, typename X, typename O, int KF>
+cudaError_t launch_t(QkParams& p, int num_sms, cudaStream_t s) {
+  if (!plan_runs(p, sizeof(X) == 2 ? 8 : 4, num_sms, 8)) return cudaErrorInvalidConfiguration;
+  return launch_pdl(norm_rope_kernel<R, X, O, KF>, dim3((p.units + kWarps - 1) / kWarps),
+                    dim3(kWarps * 32), 0, s, p);
+}
+
+template <typename X, typename O, int KF>
+cudaError_t by_r(QkParams& p, int num_sms, cudaStream_t s) {
+  switch (p.R) {
+    case 16:
+      if constexpr (KF != 2) return launch_t<16, X, O, KF>(p, num_sms, s);
+      break;  // int4 keys need r >= 32
+    case 32: return launch_t<32, X, O, KF>(p, num_sms, s);
+    case 64: return launch_t<64, X, O, KF>(p, num_sms, s);
+    case 128: return launch_t<128, X, O, KF>(p, num_sms, s);
+  }
+  return cudaErrorInvalidValue;
+}
+
+template <typename X>
+cudaError_t by_format(QkParams& p, int num_sms, cudaStream_t s) {
+  switch (p.k_fmt) {
+    case 0: return by_r<X, __nv_bfloat16, 0>(p, num_sms, s);
+    case 1: return by_r<X, __nv_bfloat16, 1>(p, num_sms, s);
+    case 2: return by_r<X, __nv_bfloat16, 2>(p, num_sms, s);
+  }
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace
+
+cudaError_t launch_qk_norm_rope(const QkParams& params, int num_sms, cudaStream_t s) {
+  QkParams p = params;
+  if (p.x_f32)
+    return p.o_f32 ? by_r<float, float, -1>(p, num_sms, s) : by_r<float, __nv_bfloat16, -1>(p, num_sms, s);
+  return p.o_f32 ? by_r<__nv_bfloat16, float, -1>(p, num_sms, s)
+                 : by_r<__nv_bfloat16, __nv_bfloat16, -1>(p, num_sms, s);
+}
+
+cudaError_t launch_qk_norm_rope_append(const QkParams& params, int num_sms, cudaStream_t s) {
+  QkParams p = params;
+  return p.x_f32 ? by_format<float>(p, num_sms, s) : by_format<__nv_bfloat16>(p, num_sms, s);
+}
+
+}  // namespace tk

@@ -9,10 +9,9 @@
 #include <cstdio>
 #include <cstring>
 #include <mutex>
-#include <string>
 
+#include "api.h"
 #include "kernels.h"
-#include "tk.h"
 
 namespace {
 
@@ -21,23 +20,21 @@ __device__ int g_tk_device_error;
 
 constexpr int kMaxDevices = 64;
 
-struct DeviceInfo {
-  int num_sms = 0;
-  int* err = nullptr;  // device address of g_tk_device_error
-};
 int g_num_sms[kMaxDevices];  // 0 until read
 std::mutex g_dev_mu;
 
-thread_local std::string t_last_error;
+thread_local char t_last_error[512];
 
-tk_status fail(tk_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+}  // namespace
+
+namespace tk {
+namespace api {
+
 tk_status fail(tk_status s, const char* fmt, ...) {
-  char buf[512];
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
+  vsnprintf(t_last_error, sizeof(t_last_error), fmt, ap);
   va_end(ap);
-  t_last_error = buf;
   return s;
 }
 
@@ -45,8 +42,7 @@ tk_status cuda_fail(cudaError_t e, const char* what) {
   return fail(TK_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
-// Per-call device facts for the current device: its SM count (read once per
-// device and kept) and the device address of the error word.  The address is
+// The SM count is read once per device and kept.  The error word's address is
 // looked up on every call (cudaGetSymbolAddress allocates nothing): after a
 // cudaDeviceReset the library's device code is loaded again, possibly at
 // another address, and a cached pointer would be stale.
@@ -110,7 +106,6 @@ tk_status check_desc(const tk_cache_desc* d) {
   return TK_OK;
 }
 
-// Key format index used by the kernels: 0 bf16, 1 int8, 2 int4.
 int key_format(int32_t k_dtype) { return k_dtype == TK_I8 ? 1 : (k_dtype == TK_I4 ? 2 : 0); }
 
 tk_status check_cache_ptrs(const tk_cache_desc* d, const void* k, const void* v, const void* ks,
@@ -124,7 +119,10 @@ tk_status check_cache_ptrs(const tk_cache_desc* d, const void* k, const void* v,
   return TK_OK;
 }
 
-}  // namespace
+}  // namespace api
+}  // namespace tk
+
+using namespace tk::api;
 
 extern "C" {
 
@@ -563,7 +561,7 @@ const char* tk_status_string(tk_status status) {
   return "TK_ERR_UNKNOWN";
 }
 
-const char* tk_last_error(void) { return t_last_error.c_str(); }
+const char* tk_last_error(void) { return t_last_error; }
 
 int32_t tk_abi_version(void) { return TK_ABI_VERSION; }
 

@@ -10,8 +10,10 @@ kernels; there is no CPU or PyTorch fallback, and a missing library raises.
 from __future__ import annotations
 
 import ctypes
+import itertools
 import math
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -73,7 +75,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     L = ctypes.CDLL(path)
     vp, i32, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
     i64 = ctypes.c_int64
-    dp, rp, hp = (ctypes.POINTER(t) for t in (tk_cache_desc, tk_rope_desc, tk_heads))
+    dp = ctypes.POINTER(tk_cache_desc)
+    rp = hp = vp     # addresses or byref(): checking a pointer's type costs more than passing it
     sig = {
         "tk_kv_append": (i32, [dp, vp, vp, vp, vp, vp, vp, vp, i32, vp]),
         "tk_attn_prefill": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, f32, i32, vp]),
@@ -92,7 +95,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "tk_attn_decode_noalloc": (i32, [dp, vp, vp, vp, vp, vp, vp, i32, vp, i32, f32, vp]),
         "tk_qk_norm_rope": (i32, [rp, i32, i32, i32, hp, hp, hp, vp, vp, i32, vp, i64, i64, hp, hp,
                                   hp, vp]),
-        "tk_qk_norm_rope_append": (i32, [dp, rp, i32, i32, hp, hp, hp, vp, vp, i32, vp, i64, i64,
+        "tk_qk_norm_rope_append": (i32, [vp, rp, i32, i32, hp, hp, hp, vp, vp, i32, vp, i64, i64,
                                          vp, hp, vp, vp, vp, vp]),
         "tk_qk_norm_rope_workspace_size": (sz, [rp]),
         "tk_qk_norm_rope_backward": (i32, [rp, i32, i32, i32, hp, hp, vp, vp, i32, vp, i64, i64,
@@ -132,9 +135,14 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _raw_stream(stream):
+    # the current stream's handle without building a torch.cuda.Stream (60 ns against 2.9 us)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None \
+        else stream.cuda_stream
+
+
 def _stream(stream):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    return ctypes.c_void_p(_raw_stream(stream))
 
 
 def _need_out(t, name, device):
@@ -388,6 +396,15 @@ def tk_attn_prefill_cached(cache: ThinKeyCache, q, k_new, v_new, seq_lens, max_s
     return out
 
 
+def _marshalled(lib, name, args):
+    """A handle of the entry point without argument types, and the arguments as C values: a call
+    then converts nothing (1.0 us against 2.4 us for 17 arguments)."""
+    typed = getattr(lib, name)
+    fn = lib[name]
+    fn.restype = typed.restype
+    return fn, tuple(t(a) if isinstance(a, (int, float)) else a for t, a in zip(typed.argtypes, args, strict=True))
+
+
 class PreparedCall:
     """Entry-point calls with their arguments checked and marshalled once.
 
@@ -401,7 +418,7 @@ class PreparedCall:
     def __init__(self, name: str, args: tuple, keep: tuple, before: tuple = (), graph: bool = False,
                  stream=None):
         L = load_library()
-        self._calls = tuple((getattr(L, n), n, a) for n, a in (*before, (name, args)))
+        self._calls = tuple((*_marshalled(L, n, a), n) for n, a in (*before, (name, args)))
         self._keep = keep  # the tensors whose pointers are in args stay alive
         self._graph = None
         if graph:
@@ -421,7 +438,7 @@ class PreparedCall:
             self._destroy = L.tk_graph_destroy
 
     def _run_calls(self):
-        for fn, name, args in self._calls:
+        for fn, args, name in self._calls:
             st = fn(*args)
             if st != TK_OK:
                 _check(st, name)
@@ -538,56 +555,66 @@ def rope_plan(r: int, rot_dim: int | None = None, layout: str = "half", base: fl
     return d
 
 
+_HEADS_DTYPE = {torch.bfloat16: TK_BF16, torch.float32: TK_F32}
+_HEADS_SIZE = ctypes.sizeof(tk_heads)
+_HEADS_PACK = {n: struct.Struct("Piiqqq" * n) for n in (4, 6, 8)}
+
+
 def _heads(t, name, shape, device):
-    """A tensor of logical shape [B, H, S, width], any strides with the width contiguous."""
+    """The fields of tk_heads for a tensor of logical shape [B, H, S, width], any strides with the
+    width contiguous; zeros for None."""
     if t is None:
-        return None
-    if t.dtype is torch.bfloat16:
-        dt = TK_BF16
-    elif t.dtype is torch.float32:
-        dt = TK_F32
-    else:
+        return 0, 0, 0, 0, 0, 0
+    dt = _HEADS_DTYPE.get(t.dtype)
+    if dt is None:
         raise TypeError(f"{name} must be float32 or bfloat16")
-    if t.device != device or not t.is_cuda:
+    if not t.is_cuda or t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device} (CUDA)")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} is {tuple(t.shape)}, expected {shape}")
     sb, sh, st, sw = t.stride()
     if sw != 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
-    return tk_heads(t.data_ptr(), shape[1], dt, sb, st, sh)
+    return t.data_ptr(), shape[1], dt, sb, st, sh
+
+
+def _pack_heads(*fields):
+    """A buffer of tk_heads (keep it alive during the call) and the address of each, None if absent."""
+    n = len(fields)
+    buf = (tk_heads * n)()
+    _HEADS_PACK[n].pack_into(buf, 0, *itertools.chain.from_iterable(fields))
+    at = ctypes.addressof(buf)
+    return buf, [at + i * _HEADS_SIZE if f[1] else None for i, f in enumerate(fields)]
 
 
 def _weights(plan, q_weight, k_weight, device):
-    dts = {t.dtype for t in (q_weight, k_weight) if t is not None}
-    if len(dts) > 1 or not dts <= {torch.float32, torch.bfloat16}:
+    """The weights' type, checked, and their addresses."""
+    given = [(t, n) for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")) if t is not None]
+    kinds = {_HEADS_DTYPE.get(t.dtype) for t, _ in given}
+    if None in kinds or len(kinds) > 1:
         raise TypeError("norm weights must be float32 or bfloat16, both alike")
-    for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if t is not None:
-            _need(t, t.dtype, n, device)
-            if t.numel() != plan.r:
-                raise ValueError(f"{n} has {t.numel()} elements, expected {plan.r}")
-    return TK_BF16 if torch.bfloat16 in dts else TK_F32
+    for t, n in given:
+        _need(t, t.dtype, n, device)
+        if t.numel() != plan.r:
+            raise ValueError(f"{n} has {t.numel()} elements, expected {plan.r}")
+    return (None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+            kinds.pop() if kinds else TK_F32)
 
 
 def _positions(plan, positions, B, S, device):
-    """(pointer, axis stride, batch stride) of positions [B, S] or [n_axes, B, S] int32."""
+    """(address, axis stride, batch stride) of positions [B, S] or [n_axes, B, S] int32."""
     if positions is None:
         return None, 0, 0
     if positions.dtype is not torch.int32 or positions.device != device:
         raise TypeError(f"positions must be int32 on {device}")
-    if positions.dim() == 2:
-        positions = positions.unsqueeze(0).expand(plan.n_axes, *positions.shape)
-    if tuple(positions.shape) != (plan.n_axes, B, S):
+    shape, stride = positions.shape, positions.stride()
+    if len(shape) == 2:                       # shared by every axis
+        shape, stride = (plan.n_axes, *shape), (0, *stride)
+    if shape != (plan.n_axes, B, S):
         raise ValueError(f"positions are {tuple(positions.shape)}, expected {(plan.n_axes, B, S)} or {(B, S)}")
-    sa, sb, st = positions.stride()
-    if st != 1 and S > 1:
+    if stride[2] != 1 and S > 1:
         raise ValueError("positions must be contiguous along the tokens")
-    return ctypes.c_void_p(positions.data_ptr()), sa, sb
-
-
-def _ref(h):
-    return None if h is None else ctypes.byref(h)
+    return positions.data_ptr(), stride[0], stride[1]
 
 
 def _dims(*tensors):
@@ -612,15 +639,14 @@ def tk_qk_norm_rope(plan: tk_rope_desc, q, k, v, positions, q_out, k_out, v_out,
     B, S, dev = _dims(q, k, v)
     dv = 0 if v is None else v.shape[3]
     sq, sk, sv = _shape(q, B, S, plan.r), _shape(k, B, S, plan.r), _shape(v, B, S, dv)
-    hs = [_heads(t, n, s, dev) for t, n, s in (
-        (q, "q", sq), (k, "k", sk), (v, "v", sv), (q_out, "q_out", sq), (k_out, "k_out", sk),
-        (v_out, "v_out", sv))]
-    wd = _weights(plan, q_weight, k_weight, dev)
-    pos = _positions(plan, positions, B, S, dev)
-    _check(load_library().tk_qk_norm_rope(
-        ctypes.byref(plan), B, S, dv, _ref(hs[0]), _ref(hs[1]), _ref(hs[2]), _ptr(q_weight),
-        _ptr(k_weight), wd, *pos, _ref(hs[3]), _ref(hs[4]), _ref(hs[5]), _stream(stream)),
-        "tk_qk_norm_rope")
+    _buf, h = _pack_heads(
+        _heads(q, "q", sq, dev), _heads(k, "k", sk, dev), _heads(v, "v", sv, dev),
+        _heads(q_out, "q_out", sq, dev), _heads(k_out, "k_out", sk, dev), _heads(v_out, "v_out", sv, dev))
+    st = load_library().tk_qk_norm_rope(
+        ctypes.byref(plan), B, S, dv, h[0], h[1], h[2], *_weights(plan, q_weight, k_weight, dev),
+        *_positions(plan, positions, B, S, dev), h[3], h[4], h[5], _raw_stream(stream))
+    if st != TK_OK:
+        _check(st, "tk_qk_norm_rope")
     return q_out, k_out, v_out
 
 
@@ -631,20 +657,18 @@ def _append_args(cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weig
     if v is None or v.dim() != 4:
         raise ValueError("k and v are required")
     sq, sk = (B, d.h_q, S, plan.r), (B, d.h_kv, S, plan.r)
-    hq, ho = _heads(q, "q", sq, dev), _heads(q_out, "q_out", sq, dev)
-    hk, hv = _heads(k, "k", sk, dev), _heads(v, "v", (B, d.h_kv, S, d.d_v), dev)
+    buf, h = _pack_heads(_heads(q, "q", sq, dev), _heads(k, "k", sk, dev),
+                         _heads(v, "v", (B, d.h_kv, S, d.d_v), dev), _heads(q_out, "q_out", sq, dev))
     _need(slots, torch.int32, "slots", dev)
     if slots.numel() != B * S:
         raise ValueError(f"slots has {slots.numel()} entries for {B * S} tokens")
     for t, n in ((cache.k, "cache.k"), (cache.v, "cache.v"), (cache.k_scale, "cache.k_scale")):
         if t is not None and t.device != dev:
             raise ValueError(f"{n} is on {t.device}, expected {dev}")
-    wd = _weights(plan, q_weight, k_weight, dev)
-    pos = _positions(plan, positions, B, S, dev)
-    args = (ctypes.byref(d), ctypes.byref(plan), B, S, _ref(hq), _ref(hk), _ref(hv), _ptr(q_weight),
-            _ptr(k_weight), wd, *pos, _ptr(slots), _ref(ho), _ptr(cache.k), _ptr(cache.v),
-            _ptr(cache.k_scale), _stream(stream))
-    return args, (cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight, hq, hk, hv, ho)
+    args = (ctypes.byref(d), ctypes.byref(plan), B, S, h[0], h[1], h[2],
+            *_weights(plan, q_weight, k_weight, dev), *_positions(plan, positions, B, S, dev), _ptr(slots),
+            h[3], _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_scale), _stream(stream))
+    return args, (cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight, buf)
 
 
 def tk_qk_norm_rope_append(cache: ThinKeyCache, plan: tk_rope_desc, q, k, v, positions, slots, q_out,
@@ -685,10 +709,10 @@ def tk_qk_norm_rope_backward(plan: tk_rope_desc, q, k, positions, dq_out, dk_out
     sq, sk, sv = _shape(dq_out, B, S, plan.r), _shape(dk_out, B, S, plan.r), _shape(dv_out, B, S, width)
     if not plan.norm:
         q = k = None
-    hs = [_heads(t, n, s, dev) for t, n, s in (
-        (q, "q", sq), (k, "k", sk), (dq_out, "dq_out", sq), (dk_out, "dk_out", sk), (dv_out, "dv_out", sv),
-        (dq, "dq", sq), (dk, "dk", sk), (dv, "dv", sv))]
-    wd = _weights(plan, q_weight, k_weight, dev)
+    _buf, h = _pack_heads(
+        _heads(q, "q", sq, dev), _heads(k, "k", sk, dev), _heads(dq_out, "dq_out", sq, dev),
+        _heads(dk_out, "dk_out", sk, dev), _heads(dv_out, "dv_out", sv, dev), _heads(dq, "dq", sq, dev),
+        _heads(dk, "dk", sk, dev), _heads(dv, "dv", sv, dev))
     for t, n in ((dq_weight, "dq_weight"), (dk_weight, "dk_weight")):
         _need(t, torch.float32, n, dev)
         if t is not None and t.numel() != plan.r:
@@ -696,11 +720,14 @@ def tk_qk_norm_rope_backward(plan: tk_rope_desc, q, k, positions, dq_out, dk_out
     if workspace is None and (dq_weight is not None or dk_weight is not None):
         workspace = qk_norm_rope_workspace(plan, dev)
     _need(workspace, torch.uint8, "workspace", dev)
-    pos = _positions(plan, positions, B, S, dev)
-    _check(load_library().tk_qk_norm_rope_backward(
-        ctypes.byref(plan), B, S, width, _ref(hs[0]), _ref(hs[1]), _ptr(q_weight), _ptr(k_weight), wd, *pos,
-        *(_ref(h) for h in hs[2:]), _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace),
-        0 if workspace is None else workspace.numel(), _stream(stream)), "tk_qk_norm_rope_backward")
+    st = load_library().tk_qk_norm_rope_backward(
+        ctypes.byref(plan), B, S, width, h[0], h[1], *_weights(plan, q_weight, k_weight, dev),
+        *_positions(plan, positions, B, S, dev), *h[2:], None if dq_weight is None else dq_weight.data_ptr(),
+        None if dk_weight is None else dk_weight.data_ptr(),
+        None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel(), _raw_stream(stream))
+    if st != TK_OK:
+        _check(st, "tk_qk_norm_rope_backward")
     return dq, dk, dv
 
 

@@ -26,7 +26,6 @@ namespace tk {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kPer = 4;    // rows of the slot map a thread fills at a time
 
 // Exclusive prefix sums over the block of one value a thread each, two at a
 // time; *ta and *tb: their totals.
@@ -63,8 +62,9 @@ struct Shared {
   int last;
 };
 
-// K: sequences of one thread.
-template <int K>
+// K: sequences of one thread; kPer: rows of the slot map that it fills at a
+// time.
+template <int K, int kPer>
 __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_constant__ BlockTableParams p) {
   extern __shared__ int dyn[];
   __shared__ Shared sh;
@@ -236,9 +236,9 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
       }
       if (page >= 0) slot[i] = (page << p.page_shift) + (pos[i] & (ps - 1));
     }
-    if (row0 + kPer <= p.rows) {
-      *reinterpret_cast<int4*>(p.slots + row0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
-      *reinterpret_cast<int4*>(p.positions + row0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+    if (kPer == 4 && row0 + kPer <= p.rows) {
+      *reinterpret_cast<int4*>(p.slots + row0) = make_int4(slot[0], slot[1 % kPer], slot[2 % kPer], slot[3 % kPer]);
+      *reinterpret_cast<int4*>(p.positions + row0) = make_int4(pos[0], pos[1 % kPer], pos[2 % kPer], pos[3 % kPer]);
     } else {
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
@@ -264,18 +264,27 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
   }
 }
 
-template <int K>
-cudaError_t launch_k(const BlockTableParams& p, int num_sms, cudaStream_t s) {
+template <int K, int kPer>
+cudaError_t launch_t(const BlockTableParams& p, int num_sms, cudaStream_t s) {
   const size_t smem = (4 * static_cast<size_t>(p.B) + 2) * sizeof(int);
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(block_tables_kernel<K>,
+    const cudaError_t e = cudaFuncSetAttribute(block_tables_kernel<K, kPer>,
                                                cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                static_cast<int>(smem));
     if (e != cudaSuccess) return e;
   }
   const int64_t want = (static_cast<int64_t>(p.rows) + kThreads * kPer - 1) / (kThreads * kPer);
   const unsigned grid = static_cast<unsigned>(want < 1 ? 1 : want > num_sms ? num_sms : want);
-  return launch_pdl(block_tables_kernel<K>, dim3(grid), dim3(kThreads), smem, s, p);
+  return launch_pdl(block_tables_kernel<K, kPer>, dim3(grid), dim3(kThreads), smem, s, p);
+}
+
+// Four rows a thread share a search and a page and store 16 bytes, but their
+// page loads follow one another; one row a thread does while that fills no
+// more than one block per SM.
+template <int K>
+cudaError_t launch_k(const BlockTableParams& p, int num_sms, cudaStream_t s) {
+  if (p.rows <= num_sms * kThreads) return launch_t<K, 1>(p, num_sms, s);
+  return launch_t<K, 4>(p, num_sms, s);
 }
 
 }  // namespace

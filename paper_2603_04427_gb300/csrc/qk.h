@@ -53,11 +53,11 @@ struct QkParams {
   int x_f32, o_f32;         // type of q, k, v; type of qo, ko, vo
   uint32_t n_tokens;        // B * S
   FastDiv div_s;
-  // set by the launchers: heads a warp takes at a time, and how many such
-  // runs of q, k and v heads there are
+  // set by the launchers (plan_runs): heads a warp takes, how many such runs
+  // q, k and v have, groups of tokens, and units = groups x runs
   int hq_run, hk_run, hv_run, nq, nk, nv;
-  FastDiv div_runs;
-  uint32_t units;
+  uint32_t groups, groups_v, units_qk, units;
+  FastDiv div_qk, div_nq, div_nk, div_nv;   // by nq + nk, nq, nk, nv
   // append: k and v go to the cache at slots[token]
   const int32_t* slots;
   void* k_cache;

@@ -10,14 +10,11 @@
 // the bound is HBM for long prompts and the launch for single tokens.
 //
 // A warp takes the 256 / r tokens that fit its lanes (qk_row.cuh) and a run
-// of up to 8 heads: the run's rows are all loaded before the first is used
-// (8 x 512 bytes in flight per warp, which is what covers HBM's latency), and
-// the token's angles are computed once for the run.  Lanes of one store
-// instruction then hold neighbouring tokens of one head, which is the
-// contiguous direction of the head-major output.  Values are copied by
-// further runs of the same launch.
-#include <type_traits>
-
+// of up to 8 heads, whose angles it computes once: four rows (two of fp32) are
+// loaded before the first is used, 64 bytes a lane, which with 32 warps an SM
+// covers HBM's latency.  Lanes of one store instruction hold neighbouring
+// tokens of one head, the contiguous direction of the head-major output.
+// Values are copied by further units of the same launch.
 #include "kernels.h"
 #include "qk_row.cuh"
 
@@ -48,10 +45,16 @@ __device__ __forceinline__ SlotRow slot_row(const QkParams& p, uint32_t token, b
 }
 
 // A lane's eight key elements as codes: symmetric absmax per (token, kv head),
-// scale = amax / Q, code = clamp(rint(y / scale), -Q, Q), both divisions in
-// IEEE binary32, amax 0 storing scale 0 and zero codes.  y is the fp32 result
-// of the rotation, not rounded to bf16 first: one rounding less than an
-// append of bf16 keys makes.
+// scale = amax / Q, code = clamp(rint(y / scale), -Q, Q), both quotients as
+// binary32 division rounds them, amax 0 storing scale 0 and zero codes.  y is
+// the fp32 result of the rotation, not rounded to bf16 first: one rounding
+// less than an append of bf16 keys makes.
+// y / scale takes the row's one reciprocal and two corrections by the FMA
+// remainder; after the first the quotient is off by less than a unit, and the
+// second then rounds as division does (Markstein, 1990).  Both operands are
+// scaled by a power of two where the remainder could underflow.  Eight
+// divisions a lane instead made the unrolled kernel miss the instruction
+// cache (5.6 of 12 stall cycles an instruction).
 template <int R, int KF>
 __device__ __forceinline__ void store_codes(const QkParams& p, int64_t row, bool ok, int sub, int oa,
                                             int ob, const float* y) {
@@ -62,12 +65,18 @@ __device__ __forceinline__ void store_codes(const QkParams& p, int64_t row, bool
   if (!ok) return;
   constexpr float Q = KF == 1 ? 127.0f : 7.0f;
   const float scale = amax / Q;
+  const float up = scale < 1e-25f ? 0x1p100f : scale > 1e25f ? 0x1p-60f : 1.0f;
+  const bool plain = scale > 0.f && scale < INFINITY;
+  const float s = plain ? scale * up : 0.f;
+  const float inv = plain ? 1.0f / s : 0.f;
   int code[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    float cf = 0.f;
-    if (scale != 0.f) cf = fminf(fmaxf(rintf(y[e] / scale), -Q), Q);
-    code[e] = static_cast<int>(cf);
+    const float a = y[e] * up;
+    float x = __fmul_rn(a, inv);
+    x = __fmaf_rn(__fmaf_rn(-x, s, a), inv, x);
+    x = __fmaf_rn(__fmaf_rn(-x, s, a), inv, x);
+    code[e] = static_cast<int>(fminf(fmaxf(rintf(x), -Q), Q));
   }
   unsigned char* k = static_cast<unsigned char*>(p.k_cache);
 #pragma unroll
@@ -85,150 +94,106 @@ __device__ __forceinline__ void store_codes(const QkParams& p, int64_t row, bool
   if (sub == 0) p.k_scale[row] = scale;
 }
 
-// Eight neighbouring elements, converted from X to O; equal types are copied bit for bit.
-template <typename X, typename O>
-struct Piece {
-  Raw<X> r;
-  __device__ __forceinline__ void load(const X* s) {
-    if constexpr (sizeof(X) == 2) {
-      const uint4 w = *reinterpret_cast<const uint4*>(s);
-      r.a = make_uint2(w.x, w.y);
-      r.b = make_uint2(w.z, w.w);
-    } else {
-      r.load(s, 0, 4);
-    }
-  }
-  __device__ __forceinline__ void store(O* d) const {
-    if constexpr (std::is_same<X, O>::value && sizeof(X) == 2) {
-      *reinterpret_cast<uint4*>(d) = make_uint4(r.a.x, r.a.y, r.b.x, r.b.y);
-    } else {
-      float y[8];
-      r.get(y);
-      if constexpr (sizeof(O) == 2)
-        *reinterpret_cast<uint4*>(d) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]),
-                                                  pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-      else
-        store_quads(d, 0, 4, y);
-    }
-  }
-};
-
 // KF: -1 = k and v go to strided tensors of type O, else to the cache with key
 // format KF (0 bf16, 1 int8, 2 int4).
-template <int R, typename X, typename O, int KF>
-__global__ void __launch_bounds__(kWarps * 32) norm_rope_kernel(const __grid_constant__ QkParams p) {
+template <int R, bool PAIR, typename X, typename O, int KF>
+__global__ void __launch_bounds__(kWarps * 32, 7) norm_rope_kernel(const __grid_constant__ QkParams p) {
   constexpr int G = R / 8, T = 32 / G;
-  constexpr int H = sizeof(X) == 2 ? 8 : 4;      // rows a lane holds at a time
+  constexpr int H = sizeof(X) == 2 ? 4 : 2;      // rows a lane holds at a time
   const int lane = threadIdx.x & 31;
   const uint32_t unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (unit >= p.units) return;
-  uint32_t run;
-  const uint32_t group = p.div_runs.divmod(unit, &run);
   pdl_wait();
   pdl_trigger();
 
-  if (run < static_cast<uint32_t>(p.nq + p.nk)) {
-    const int sub = lane % G;
-    const uint32_t token = group * T + lane / G;
-    const bool ok = token < p.n_tokens;
-    uint32_t s;
-    const uint32_t b = p.div_s.divmod(ok ? token : 0u, &s);
-    const bool is_q = run < static_cast<uint32_t>(p.nq);
-    const HeadsView in = is_q ? p.q : p.k;
-    const int per = is_q ? p.hq_run : p.hk_run;
-    const int h0 = static_cast<int>(is_q ? run : run - p.nq) * per;
-    const int nh = min(per, in.n - h0);
-    int oa, ob;
-    quad_offsets(sub, p.rot, p.pair_layout, &oa, &ob);
-    const X* src = static_cast<const X*>(in.p) + b * in.sb + s * in.st + h0 * in.sh;
-    Raw<X> raw[H];
+  if (unit >= p.units_qk) {
+    auto src = [&](uint32_t b, uint32_t s) {
+      return static_cast<const X*>(p.v.p) + b * p.v.sb + s * p.v.st;
+    };
+    if constexpr (KF < 0) {
+      copy_values<2 * H, X, O>(p, unit - p.units_qk, p.v.n, p.v.sh, p.vo.sh, lane, src,
+                               [&](uint32_t b, uint32_t s, uint32_t) {
+                                 return static_cast<O*>(p.vo.p) + b * p.vo.sb + s * p.vo.st;
+                               });
+    } else {
+      copy_values<2 * H, X, O>(p, unit - p.units_qk, p.v.n, p.v.sh,
+                               static_cast<int64_t>(p.slot_rows) * p.DV, lane, src,
+                               [&](uint32_t, uint32_t, uint32_t token) -> O* {
+                                 const SlotRow slot = slot_row(p, token, true);
+                                 return slot.ok ? static_cast<O*>(p.v_cache) + slot.block_row * p.DV : nullptr;
+                               });
+    }
+    return;
+  }
+
+  uint32_t run, s;
+  const uint32_t group = p.div_qk.divmod(unit, &run);
+  const int sub = lane % G;
+  const uint32_t token = group * T + lane / G;
+  const bool ok = token < p.n_tokens;
+  const uint32_t b = p.div_s.divmod(ok ? token : 0u, &s);
+  const bool is_q = run < static_cast<uint32_t>(p.nq);
+  const HeadsView in = is_q ? p.q : p.k;
+  const int per = is_q ? p.hq_run : p.hk_run;
+  const int h0 = static_cast<int>(is_q ? run : run - p.nq) * per;
+  const int nh = min(per, in.n - h0);
+  int oa, ob;
+  quad_offsets<PAIR>(sub, p.rot, &oa, &ob);
+  const X* src = static_cast<const X*>(in.p) + b * in.sb + s * in.st + h0 * in.sh;
+  Raw<X> raw[H];
+  auto load = [&](int h) {
 #pragma unroll
     for (int i = 0; i < H; ++i) {
       raw[i].zero();
-      if (ok && i < nh) raw[i].load(src + i * in.sh, oa, ob);
+      if (ok && h + i < nh) raw[i].load(src + i * in.sh, oa, ob);
     }
-    SlotRow slot{0, false};
-    if (KF >= 0 && !is_q) slot = slot_row(p, token, ok);
-    float w[8];
-    if (p.norm) load_weights(is_q ? p.wq : p.wk, p.w_f32, p.w_offset, oa, ob, w);
-    const Turns t = load_turns(p, sub, b, s, ok);
-    const HeadsView out = is_q ? p.qo : p.ko;
-    O* dst = static_cast<O*>(out.p) + b * out.sb + s * out.st + h0 * out.sh;
+    src += H * in.sh;
+  };
+  load(0);
+  SlotRow slot{0, false};
+  if (KF >= 0 && !is_q) slot = slot_row(p, token, ok);
+  float w[8];
+  load_weights(is_q ? p.wq : p.wk, p.w_f32, p.w_offset, oa, ob, w);
+  const Turns t = load_turns(p, sub, b, s, ok);
+  const HeadsView out = is_q ? p.qo : p.ko;
+  O* dst = static_cast<O*>(out.p) + b * out.sb + s * out.st + h0 * out.sh;
+  int64_t row = slot.block_row + static_cast<int64_t>(h0) * p.slot_rows;
+  for (int h = 0; h < nh; h += H) {
 #pragma unroll
     for (int i = 0; i < H; ++i) {
-      if (i >= nh) break;
+      if (h + i >= nh) break;
       float y[8];
       raw[i].get(y);
-      if (p.norm) {
-        float ss = 0.f;
+      float ss = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = __fmaf_rn(y[e], y[e], ss);
-        const float rho = rsqrtf(__fmaf_rn(row_sum<G>(ss), 1.0f / R, p.eps));
+      for (int e = 0; e < 8; ++e) ss = __fmaf_rn(y[e], y[e], ss);
+      // without norm the row is multiplied by 1, which changes no bit
+      const float rho = p.norm ? rsqrtf(__fmaf_rn(row_sum<G>(ss), 1.0f / R, p.eps)) : 1.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = __fmul_rn(__fmul_rn(y[e], rho), w[e]);
-      }
-      rotate8(y, t, p.pair_layout, false);
+      for (int e = 0; e < 8; ++e) y[e] = __fmul_rn(__fmul_rn(y[e], rho), w[e]);
+      rotate8<PAIR, false>(y, t);
       if (KF < 0 || is_q) {
-        if (ok) store_quads(dst + i * out.sh, oa, ob, y);
+        if (ok) store_quads(dst, oa, ob, y);
+        dst += out.sh;
       } else {
-        const int64_t row = slot.block_row + static_cast<int64_t>(h0 + i) * p.slot_rows;
         if constexpr (KF <= 0) {
           if (slot.ok) store_quads(static_cast<__nv_bfloat16*>(p.k_cache) + row * R, oa, ob, y);
         } else {
           store_codes<R, KF>(p, row, slot.ok, sub, oa, ob, y);
         }
+        row += p.slot_rows;
       }
     }
-    return;
-  }
-
-  // values: the group's tokens x a run of heads, as 8-element pieces
-  constexpr int log_t = T == 16 ? 4 : T == 8 ? 3 : T == 4 ? 2 : 1;
-  const int log_c = p.DV == 128 ? 4 : 3;
-  const int h0 = static_cast<int>(run - p.nq - p.nk) * p.hv_run;
-  const int nh = min(p.hv_run, p.v.n - h0);
-  const int pieces = nh << (log_t + log_c);
-  for (int c0 = lane; c0 < pieces; c0 += 32 * H) {
-    Piece<X, O> piece[H];
-#pragma unroll
-    for (int i = 0; i < H; ++i) {
-      const int c = c0 + 32 * i;
-      const uint32_t token = group * T + ((c >> log_c) & (T - 1));
-      if (c < pieces && token < p.n_tokens) {
-        uint32_t s;
-        const uint32_t b = p.div_s.divmod(token, &s);
-        piece[i].load(static_cast<const X*>(p.v.p) + b * p.v.sb + s * p.v.st +
-                      (h0 + (c >> (log_c + log_t))) * p.v.sh + 8 * (c & ((1 << log_c) - 1)));
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < H; ++i) {
-      const int c = c0 + 32 * i;
-      const uint32_t token = group * T + ((c >> log_c) & (T - 1));
-      const bool ok = c < pieces && token < p.n_tokens;
-      const int h = h0 + (c >> (log_c + log_t));
-      const int col = 8 * (c & ((1 << log_c) - 1));
-      if constexpr (KF < 0) {
-        if (ok) {
-          uint32_t s;
-          const uint32_t b = p.div_s.divmod(token, &s);
-          piece[i].store(static_cast<O*>(p.vo.p) + b * p.vo.sb + s * p.vo.st + h * p.vo.sh + col);
-        }
-      } else {
-        const SlotRow slot = slot_row(p, token, ok);
-        if (slot.ok)
-          piece[i].store(static_cast<O*>(p.v_cache) +
-                         (slot.block_row + static_cast<int64_t>(h) * p.slot_rows) * p.DV + col);
-      }
-    }
+    if (h + H < nh) load(h + H);
   }
 }
 
 template <int R, typename X, typename O, int KF>
 cudaError_t launch_t(QkParams& p, int num_sms, cudaStream_t s) {
-  if (!plan_runs(p, sizeof(X) == 2 ? 8 : 4, num_sms, 8)) return cudaErrorInvalidConfiguration;
-  return launch_pdl(norm_rope_kernel<R, X, O, KF>, dim3((p.units + kWarps - 1) / kWarps),
-                    dim3(kWarps * 32), 0, s, p);
+  if (!plan_runs(p, num_sms, 8)) return cudaErrorInvalidConfiguration;
+  const dim3 grid((p.units + kWarps - 1) / kWarps), block(kWarps * 32);
+  return p.pair_layout ? launch_pdl(norm_rope_kernel<R, true, X, O, KF>, grid, block, 0, s, p)
+                       : launch_pdl(norm_rope_kernel<R, false, X, O, KF>, grid, block, 0, s, p);
 }
 
 template <typename X, typename O, int KF>

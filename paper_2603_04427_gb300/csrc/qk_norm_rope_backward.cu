@@ -7,12 +7,14 @@
 // read once, kept in registers and written once; rho is recomputed, not
 // stored by the forward (the row is read anyway).
 //
-// Bound by HBM.  One block per SM, each warp taking an equal share of the
-// (token group, run of heads) units in order: the weight gradient then
-// gathers in registers over all the units of a warp, in shared memory over
-// the block's warps, and one partial sum per block goes to the workspace,
-// which the last block to arrive adds up in block order.  No atomics touch
-// the sums, so results repeat bit for bit on one GPU model.
+// Bound by HBM.  One block per SM; each warp takes an equal share of the (token
+// group, run of heads) units of q, of k and of v (equal shares of all units in
+// one row left SMs with values alone idle a quarter of the time).  The weight
+// gradient gathers in eight registers a lane over a warp's units of one
+// tensor, in shared memory over the block's warps, and one partial sum per
+// block goes to the workspace, which the last block to arrive adds up in
+// block order.  No atomics touch the sums, so results repeat bit for bit on
+// one GPU model.
 #include "kernels.h"
 #include "qk_row.cuh"
 
@@ -20,38 +22,48 @@ namespace tk {
 namespace {
 
 constexpr int kThreads = 512, kWarpsB = kThreads / 32;
-constexpr int kRun = 4;   // rows a lane holds at a time
 
-template <int R, typename X, typename D>
+// Rows a lane holds at a time: 96 to 128 bytes of x and g.
+template <typename X, typename D>
+constexpr int rows_held() { return sizeof(X) + sizeof(D) == 4 ? 4 : 2; }
+
+template <int R, bool PAIR, typename X, typename D>
 __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const __grid_constant__ QkParams p) {
-  constexpr int G = R / 8, T = 32 / G;
-  constexpr int log_t = T == 16 ? 4 : T == 8 ? 3 : T == 4 ? 2 : 1;
+  constexpr int G = R / 8, T = 32 / G, kRun = rows_held<X, D>();
   __shared__ float sums[kWarpsB][2][R];
   __shared__ int last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sub = lane % G;
   int oa, ob;
-  quad_offsets(sub, p.rot, p.pair_layout, &oa, &ob);
-  float dw[2][8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) dw[0][e] = dw[1][e] = 0.f;
+  quad_offsets<PAIR>(sub, p.rot, &oa, &ob);
 
-  // this warp's share of the units
+  // this warp's share of a tensor's units: neighbouring ones, so that a
+  // token's angles serve several
   const uint64_t n_warps = static_cast<uint64_t>(gridDim.x) * kWarpsB;
   const uint64_t w = static_cast<uint64_t>(blockIdx.x) * kWarpsB + warp;
-  const uint32_t first = static_cast<uint32_t>(w * p.units / n_warps);
-  const uint32_t end = static_cast<uint32_t>((w + 1) * p.units / n_warps);
+  auto share = [&](uint64_t at, uint64_t units) { return static_cast<uint32_t>(at * units / n_warps); };
   pdl_wait();
   pdl_trigger();
 
-  uint32_t group = 0xffffffffu, b = 0, s = 0;
-  bool ok = false;
-  Turns t;
-  for (uint32_t unit = first; unit < end; ++unit) {
-    uint32_t run;
-    const uint32_t g = p.div_runs.divmod(unit, &run);
-    if (run < static_cast<uint32_t>(p.nq + p.nk)) {
-      const bool is_q = run < static_cast<uint32_t>(p.nq);
+#pragma unroll 1
+  for (int m = 0; m < 2; ++m) {      // q, k
+    const HeadsView gin = m ? p.ko : p.qo;
+    const HeadsView xin = m ? p.k : p.q;
+    const HeadsView out = m ? p.dk : p.dq;
+    const int per = m ? p.hk_run : p.hq_run;
+    const FastDiv div = m ? p.div_nk : p.div_nq;
+    const uint64_t units = static_cast<uint64_t>(p.groups) * (m ? p.nk : p.nq);
+    const uint32_t first = share(w, units), end = share(w + 1, units);
+    float dw[8], u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[e] = 0.f;
+    uint32_t group = 0xffffffffu, b = 0, s = 0;
+    bool ok = false;
+    Turns t;
+    if (p.norm && first < end) load_weights(m ? p.wk : p.wq, p.w_f32, p.w_offset, oa, ob, u);
+    for (uint32_t unit = first; unit < end; ++unit) {
+      uint32_t run;
+      const uint32_t g = div.divmod(unit, &run);
       const bool fresh = g != group;
       if (fresh) {
         group = g;
@@ -59,107 +71,77 @@ __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const _
         ok = token < p.n_tokens;
         b = p.div_s.divmod(ok ? token : 0u, &s);
       }
-      const HeadsView gin = is_q ? p.qo : p.ko;
-      const HeadsView xin = is_q ? p.q : p.k;
-      const HeadsView out = is_q ? p.dq : p.dk;
-      const int per = is_q ? p.hq_run : p.hk_run;
-      const int h0 = static_cast<int>(is_q ? run : run - p.nq) * per;
+      const int h0 = static_cast<int>(run) * per;
       const int nh = min(per, gin.n - h0);
-      Raw<D> rg[kRun];
-      Raw<X> rx[kRun];
       const D* gsrc = static_cast<const D*>(gin.p) + b * gin.sb + s * gin.st + h0 * gin.sh;
       const X* xsrc = static_cast<const X*>(xin.p) + b * xin.sb + s * xin.st + h0 * xin.sh;
-#pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        rg[i].zero();
-        rx[i].zero();
-        if (ok && i < nh) {
-          rg[i].load(gsrc + i * gin.sh, oa, ob);
-          if (p.norm) rx[i].load(xsrc + i * xin.sh, oa, ob);
-        }
-      }
-      float u[8];
-      if (p.norm) load_weights(is_q ? p.wq : p.wk, p.w_f32, p.w_offset, oa, ob, u);
-      if (fresh) t = load_turns(p, sub, b, s, ok);
       X* dst = static_cast<X*>(out.p) + b * out.sb + s * out.st + h0 * out.sh;
+      Raw<D> rg[kRun];
+      Raw<X> rx[kRun];
+      auto load = [&](int h) {
 #pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        if (i >= nh) break;
-        float y[8];
-        rg[i].get(y);
-        rotate8(y, t, p.pair_layout, true);
-        if (p.norm) {
-          float x[8], ss = 0.f, gx = 0.f;
-          rx[i].get(x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            ss = fmaf(x[e], x[e], ss);
-            gx = fmaf(y[e] * u[e], x[e], gx);
-          }
-          ss = row_sum<G>(ss);
-          gx = row_sum<G>(gx);
-          const float rho = rsqrtf(ss * (1.0f / R) + p.eps);
-          const float m = rho * rho * (gx * (1.0f / R));
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float d = y[e] * (x[e] * rho);
-            if (is_q) dw[0][e] += d;
-            else dw[1][e] += d;
-            y[e] = rho * (y[e] * u[e] - x[e] * m);
+        for (int i = 0; i < kRun; ++i) {
+          rg[i].zero();
+          rx[i].zero();
+          if (ok && h + i < nh) {
+            rg[i].load(gsrc + i * gin.sh, oa, ob);
+            if (p.norm) rx[i].load(xsrc + i * xin.sh, oa, ob);
           }
         }
-        if (ok) store_quads(dst + i * out.sh, oa, ob, y);
-      }
-      continue;
-    }
-    // value gradients: converted and laid out, 8-element pieces
-    const int log_c = p.DV == 128 ? 4 : 3;
-    const int h0 = static_cast<int>(run - p.nq - p.nk) * p.hv_run;
-    const int nh = min(p.hv_run, p.vo.n - h0);
-    const int pieces = nh << (log_t + log_c);
-    for (int c0 = lane; c0 < pieces; c0 += 32 * kRun) {
-      Raw<D> r[kRun];
+        gsrc += kRun * gin.sh;
+        xsrc += kRun * xin.sh;
+      };
+      load(0);
+      if (fresh) t = load_turns(p, sub, b, s, ok);
+      for (int h = 0; h < nh; h += kRun) {
 #pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        const int c = c0 + 32 * i;
-        const uint32_t token = g * T + ((c >> log_c) & (T - 1));
-        if (c < pieces && token < p.n_tokens) {
-          uint32_t vs;
-          const uint32_t vb = p.div_s.divmod(token, &vs);
-          r[i].load(static_cast<const D*>(p.vo.p) + vb * p.vo.sb + vs * p.vo.st +
-                        (h0 + (c >> (log_c + log_t))) * p.vo.sh,
-                    8 * (c & ((1 << log_c) - 1)), 8 * (c & ((1 << log_c) - 1)) + 4);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        const int c = c0 + 32 * i;
-        const uint32_t token = g * T + ((c >> log_c) & (T - 1));
-        if (c < pieces && token < p.n_tokens) {
-          uint32_t vs;
-          const uint32_t vb = p.div_s.divmod(token, &vs);
+        for (int i = 0; i < kRun; ++i) {
+          if (h + i >= nh) break;
           float y[8];
-          r[i].get(y);
-          store_quads(static_cast<X*>(p.dv.p) + vb * p.dv.sb + vs * p.dv.st +
-                          (h0 + (c >> (log_c + log_t))) * p.dv.sh,
-                      8 * (c & ((1 << log_c) - 1)), 8 * (c & ((1 << log_c) - 1)) + 4, y);
+          rg[i].get(y);
+          rotate8<PAIR, true>(y, t);
+          if (p.norm) {
+            float x[8], ss = 0.f, gx = 0.f;
+            rx[i].get(x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              ss = fmaf(x[e], x[e], ss);
+              gx = fmaf(y[e] * u[e], x[e], gx);
+            }
+            ss = row_sum<G>(ss);
+            gx = row_sum<G>(gx);
+            const float rho = rsqrtf(ss * (1.0f / R) + p.eps);
+            const float mean = rho * rho * (gx * (1.0f / R));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              dw[e] = fmaf(y[e], x[e] * rho, dw[e]);
+              y[e] = rho * (y[e] * u[e] - x[e] * mean);
+            }
+          }
+          if (ok) store_quads(dst, oa, ob, y);
+          dst += out.sh;
         }
+        if (h + kRun < nh) load(h + kRun);
       }
     }
-  }
-  if (p.dwq == nullptr && p.dwk == nullptr) return;
-
-  // weight gradients: over the lanes that hold the same elements, the block's
-  // warps, then the blocks
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
+    // over the lanes that hold the same elements
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
 #pragma unroll
-      for (int o = 16; o >= G; o >>= 1) dw[m][e] += __shfl_xor_sync(0xffffffffu, dw[m][e], o);
-      if (lane < G) sums[warp][m][(e < 4 ? oa : ob - 4) + e] = dw[m][e];
+      for (int o = 16; o >= G; o >>= 1) dw[e] += __shfl_xor_sync(0xffffffffu, dw[e], o);
+      if (lane < G) sums[warp][m][(e < 4 ? oa : ob - 4) + e] = dw[e];
     }
   }
+  // value gradients: converted and laid out
+  const uint32_t v_units = p.units - p.units_qk, v_end = share(w + 1, v_units);
+  for (uint32_t unit = share(w, v_units); unit < v_end; ++unit)
+    copy_values<4, D, X>(
+        p, unit, p.vo.n, p.vo.sh, p.dv.sh, lane,
+        [&](uint32_t b, uint32_t s) { return static_cast<const D*>(p.vo.p) + b * p.vo.sb + s * p.vo.st; },
+        [&](uint32_t b, uint32_t s, uint32_t) { return static_cast<X*>(p.dv.p) + b * p.dv.sb + s * p.dv.st; });
+  if (p.dwq == nullptr && p.dwk == nullptr) return;
+
+  // weight gradients: over the block's warps, then the blocks
   __syncthreads();
   for (int c = threadIdx.x; c < 2 * R; c += kThreads) {
     float a = 0.f;
@@ -173,23 +155,30 @@ __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const _
   __syncthreads();
   if (!last) return;
   __threadfence();
-  // kThreads / 2R threads per column, each over every such block, then joined
-  constexpr int P = kThreads / (2 * R);
-  float* join = &sums[0][0][0];          // [P][2R], no larger than sums
-  static_assert(P <= kWarpsB, "the join fits the block's sums");
-  const int c = threadIdx.x % (2 * R), part = threadIdx.x / (2 * R);
-  float a = 0.f;
-#pragma unroll 8
-  for (unsigned k = part; k < gridDim.x; k += P) a += __ldcg(p.part + static_cast<size_t>(k) * 2 * R + c);
-  join[part * 2 * R + c] = a;
+  // four columns a thread and up to 16 threads a column group, so that a
+  // thread adds some ten blocks' sums, loaded at once (a thread a column and
+  // 76 loads in chains of 8 took 7 us of a 16 us call)
+  constexpr int kCols = 2 * R / 4, P = kThreads / kCols < kWarpsB ? kThreads / kCols : kWarpsB;
+  float4* join = reinterpret_cast<float4*>(&sums[0][0][0]);   // [P][kCols], at most all of sums
+  const int c = threadIdx.x % kCols, part = threadIdx.x / kCols;
+  if (part < P) {
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 10
+    for (unsigned k = part; k < gridDim.x; k += P) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part) + static_cast<size_t>(k) * kCols + c);
+      a.x += x.x, a.y += x.y, a.z += x.z, a.w += x.w;
+    }
+    join[part * kCols + c] = a;
+  }
   __syncthreads();
-  if (part == 0) {
+  for (int e = threadIdx.x; e < 2 * R; e += kThreads) {
+    float a = 0.f;
 #pragma unroll
-    for (int k = 1; k < P; ++k) a += join[k * 2 * R + c];
-    if (c < R) {
-      if (p.dwq) p.dwq[c] = a;
+    for (int k = 0; k < P; ++k) a += (&sums[0][0][0])[k * 2 * R + e];
+    if (e < R) {
+      if (p.dwq) p.dwq[e] = a;
     } else if (p.dwk) {
-      p.dwk[c - R] = a;
+      p.dwk[e - R] = a;
     }
   }
   if (threadIdx.x == 0) *p.counter = 0;   // ready for the next call
@@ -197,10 +186,12 @@ __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const _
 
 template <int R, typename X, typename D>
 cudaError_t launch_t(QkParams& p, int num_sms, cudaStream_t s) {
-  if (!plan_runs(p, kRun, num_sms, kWarpsB)) return cudaErrorInvalidConfiguration;
+  if (!plan_runs(p, num_sms, kWarpsB)) return cudaErrorInvalidConfiguration;
   const uint32_t blocks = (p.units + kWarpsB - 1) / kWarpsB;
   const uint32_t grid = blocks < static_cast<uint32_t>(num_sms) ? blocks : static_cast<uint32_t>(num_sms);
-  return launch_pdl(norm_rope_backward_kernel<R, X, D>, dim3(grid), dim3(kThreads), 0, s, p);
+  return p.pair_layout
+             ? launch_pdl(norm_rope_backward_kernel<R, true, X, D>, dim3(grid), dim3(kThreads), 0, s, p)
+             : launch_pdl(norm_rope_backward_kernel<R, false, X, D>, dim3(grid), dim3(kThreads), 0, s, p);
 }
 
 template <typename X, typename D>

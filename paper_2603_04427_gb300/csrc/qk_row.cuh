@@ -12,6 +12,8 @@
 // that are not rotated.
 #pragma once
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "qk.h"
 
@@ -45,8 +47,9 @@ __device__ __forceinline__ void turn(int p, float f, float* c, float* s) {
 }
 
 // Where lane `sub` of a row's R / 8 lanes finds its quads.
-__device__ __forceinline__ void quad_offsets(int sub, int rot, int pair_layout, int* a, int* b) {
-  const bool split = !pair_layout && sub < rot / 8;
+template <bool PAIR>
+__device__ __forceinline__ void quad_offsets(int sub, int rot, int* a, int* b) {
+  const bool split = !PAIR && sub < rot / 8;
   *a = split ? 4 * sub : 8 * sub;
   *b = split ? rot / 2 + 4 * sub : 8 * sub + 4;
 }
@@ -151,22 +154,19 @@ __device__ __forceinline__ void load_weights(const void* w, int w_f32, float off
 
 // Pairs of a lane's eight elements: (i, i + 4) in the half layout,
 // (2i, 2i + 1) in the pair layout; y is turned by +angle, or by -angle when
-// `back`.  Elements outside rot_dim are left alone, not multiplied by 1 and 0:
-// an infinity among them stays where it is.
-__device__ __forceinline__ void rotate8(float* y, const Turns& t, int pair_layout, bool back) {
-  if (!t.on) return;
+// BACK.  Elements outside rot_dim are selected, not multiplied by 1 and 0: an
+// infinity among them stays where it is.
+template <bool PAIR, bool BACK>
+__device__ __forceinline__ void rotate8(float* y, const Turns& t) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float s = back ? -t.s[i] : t.s[i];
-    if (pair_layout) {
-      const float a = y[2 * i], b = y[2 * i + 1];
-      y[2 * i] = __fmaf_rn(a, t.c[i], -__fmul_rn(b, s));
-      y[2 * i + 1] = __fmaf_rn(a, s, __fmul_rn(b, t.c[i]));
-    } else {
-      const float a = y[i], b = y[i + 4];
-      y[i] = __fmaf_rn(a, t.c[i], -__fmul_rn(b, s));
-      y[i + 4] = __fmaf_rn(a, s, __fmul_rn(b, t.c[i]));
-    }
+    const int ia = PAIR ? 2 * i : i, ib = PAIR ? 2 * i + 1 : i + 4;
+    const float s = BACK ? -t.s[i] : t.s[i];
+    const float a = y[ia], b = y[ib];
+    const float ra = __fmaf_rn(a, t.c[i], -__fmul_rn(b, s));
+    const float rb = __fmaf_rn(a, s, __fmul_rn(b, t.c[i]));
+    y[ia] = t.on ? ra : a;
+    y[ib] = t.on ? rb : b;
   }
 }
 
@@ -184,36 +184,97 @@ __device__ __forceinline__ float row_max(float x) {
   return x;
 }
 
+// Eight neighbouring elements, converted from X to O; equal types are copied bit for bit.
+template <typename X, typename O>
+struct Piece {
+  Raw<X> r;
+  __device__ __forceinline__ void load(const X* s) {
+    if constexpr (sizeof(X) == 2) {
+      const uint4 w = *reinterpret_cast<const uint4*>(s);
+      r.a = make_uint2(w.x, w.y);
+      r.b = make_uint2(w.z, w.w);
+    } else {
+      r.load(s, 0, 4);
+    }
+  }
+  __device__ __forceinline__ void store(O* d) const {
+    if constexpr (std::is_same<X, O>::value && sizeof(X) == 2) {
+      *reinterpret_cast<uint4*>(d) = make_uint4(r.a.x, r.a.y, r.b.x, r.b.y);
+    } else {
+      float y[8];
+      r.get(y);
+      if constexpr (sizeof(O) == 2)
+        *reinterpret_cast<uint4*>(d) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]),
+                                                  pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+      else
+        store_quads(d, 0, 4, y);
+    }
+  }
+};
+
+// Value rows: DV / 8 lanes a row, so 256 / DV tokens a warp, and a run of heads
+// of which N are in flight.  src(b, s) and dst(b, s, token) give the lane's
+// address in head h0 (null: nothing is stored), heads are src_sh and dst_sh apart.
+template <int N, typename X, typename O, typename Src, typename Dst>
+__device__ __forceinline__ void copy_values(const QkParams& p, uint32_t unit, int n_heads, int64_t src_sh,
+                                            int64_t dst_sh, int lane, Src src, Dst dst) {
+  uint32_t run, s;
+  const uint32_t group = p.div_nv.divmod(unit, &run);
+  const int log_l = p.DV == 128 ? 4 : 3;
+  const uint32_t token = (group << (5 - log_l)) + (lane >> log_l);
+  if (token >= p.n_tokens) return;
+  const uint32_t b = p.div_s.divmod(token, &s);
+  const int h0 = static_cast<int>(run) * p.hv_run;
+  const int nh = min(p.hv_run, n_heads - h0);
+  const int col = 8 * (lane & ((1 << log_l) - 1));
+  const X* in = src(b, s) + h0 * src_sh + col;
+  O* out = dst(b, s, token);
+  if (out) out += h0 * dst_sh + col;
+  for (int h = 0; h < nh; h += N) {
+    Piece<X, O> piece[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (h + i < nh) piece[i].load(in + i * src_sh);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (h + i < nh && out) piece[i].store(out + i * dst_sh);
+    in += N * src_sh;
+    if (out) out += N * dst_sh;
+  }
+}
+
 // How a launch cuts its heads: a warp takes the tokens that fit its lanes
-// (256 / r) and a run of at most `most` heads of q or of k, or as many value
-// elements.  Long runs amortise the angles and keep more loads in flight;
-// while the launch is too small to give every SM `want_warps` warps, the runs
-// are halved, down to single heads.
-// False if there are too many units for one launch.
-inline bool plan_runs(QkParams& p, int most, int num_sms, int want_warps) {
-  const uint32_t per_group = 256 / p.R;
-  const uint32_t groups = (p.n_tokens + per_group - 1) / per_group;
-  const int nq = p.q.p || p.qo.p ? (p.q.p ? p.q.n : p.qo.n) : 0;
-  const int nk = p.k.p || p.ko.p ? (p.k.p ? p.k.n : p.ko.n) : 0;
-  const int nv = p.v.p || p.vo.p ? (p.v.p ? p.v.n : p.vo.n) : 0;
-  auto runs = [](int heads, int run) { return (heads + run - 1) / run; };
-  for (int m = most;; m /= 2) {
+// (256 / r of q and k, 256 / d_v of v) and a run of up to 8 heads.  Long runs
+// amortise the angles; while the launch is too small to give every SM
+// `want_warps` warps, the runs are halved, down to single heads.  False if
+// there are too many units for one launch.
+inline bool plan_runs(QkParams& p, int num_sms, int want_warps) {
+  auto up = [](uint64_t a, uint64_t b) { return (a + b - 1) / b; };
+  auto heads = [](const HeadsView& a, const HeadsView& b) { return a.p ? a.n : b.p ? b.n : 0; };
+  const int nq = heads(p.q, p.qo), nk = heads(p.k, p.ko), nv = heads(p.v, p.vo);
+  p.groups = static_cast<uint32_t>(up(p.n_tokens, 256 / p.R));
+  p.groups_v = static_cast<uint32_t>(up(p.n_tokens, 256 / p.DV));
+  for (int m = 8;; m /= 2) {
     // even runs: 12 heads at most 8 at a time go as 6 + 6
-    auto even = [&](int heads, int run) {
-      return heads ? (heads + runs(heads, run) - 1) / runs(heads, run) : 1;
+    auto cut = [&](int n, int* run) {
+      const int runs = static_cast<int>(up(n, m));
+      *run = runs ? static_cast<int>(up(n, runs)) : 1;
+      return static_cast<int>(up(n, *run));
     };
-    const int mv = (m * p.R / p.DV) > 0 ? m * p.R / p.DV : 1;
-    p.hq_run = even(nq, m);
-    p.hk_run = even(nk, m);
-    p.hv_run = even(nv, mv);
-    p.nq = runs(nq, p.hq_run);
-    p.nk = runs(nk, p.hk_run);
-    p.nv = runs(nv, p.hv_run);
-    const uint64_t units = static_cast<uint64_t>(groups) * (p.nq + p.nk + p.nv);
+    p.nq = cut(nq, &p.hq_run);
+    p.nk = cut(nk, &p.hk_run);
+    p.nv = cut(nv, &p.hv_run);
+    const uint64_t qk = static_cast<uint64_t>(p.groups) * (p.nq + p.nk);
+    const uint64_t units = qk + static_cast<uint64_t>(p.groups_v) * p.nv;
     if (m > 1 && units < static_cast<uint64_t>(num_sms) * want_warps) continue;
     if (units >= (1ull << 31)) return false;
+    p.units_qk = static_cast<uint32_t>(qk);
     p.units = static_cast<uint32_t>(units);
-    p.div_runs = FastDiv(static_cast<uint32_t>(p.nq + p.nk + p.nv));
+    auto div = [](int n) { return FastDiv(static_cast<uint32_t>(n > 0 ? n : 1)); };
+    p.div_qk = div(p.nq + p.nk);
+    p.div_nq = div(p.nq);
+    p.div_nk = div(p.nk);
+    p.div_nv = div(p.nv);
     return true;
   }
 }

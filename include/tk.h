@@ -320,7 +320,8 @@ typedef enum tk_rope_layout {
  *   n_axes   : position axes, 1 .. TK_ROPE_MAX_AXES (1 for text; e.g. row and
  *              column for images; frame, row and column for video)
  *   norm     : nonzero = RMS norm of each head's row before the rotation
- *   eps      : added to the mean square (finite, > 0; unused without norm)
+ *   eps      : added to the mean square (a positive normal number; unused
+ *              without norm)
  *   w_offset : added to the norm weights (1 for weights stored as w - 1)
  *   inv_freq : angle of pair j = position[pair_axis[j]] * inv_freq[j];
  *              finite, magnitude at most 4; the first rot_dim / 2 are used

@@ -10,7 +10,6 @@ kernels; there is no CPU or PyTorch fallback, and a missing library raises.
 from __future__ import annotations
 
 import ctypes
-import itertools
 import math
 import os
 import struct
@@ -556,15 +555,14 @@ def rope_plan(r: int, rot_dim: int | None = None, layout: str = "half", base: fl
 
 
 _HEADS_DTYPE = {torch.bfloat16: TK_BF16, torch.float32: TK_F32}
-_HEADS_SIZE = ctypes.sizeof(tk_heads)
-_HEADS_PACK = {n: struct.Struct("Piiqqq" * n) for n in (4, 6, 8)}
+_pack_heads = struct.Struct("Piiqqq").pack     # the layout of tk_heads
 
 
 def _heads(t, name, shape, device):
-    """The fields of tk_heads for a tensor of logical shape [B, H, S, width], any strides with the
-    width contiguous; zeros for None."""
+    """A tk_heads, as bytes, for a tensor of logical shape [B, H, S, width], any strides with the
+    width contiguous; None for None."""
     if t is None:
-        return 0, 0, 0, 0, 0, 0
+        return None
     dt = _HEADS_DTYPE.get(t.dtype)
     if dt is None:
         raise TypeError(f"{name} must be float32 or bfloat16")
@@ -575,30 +573,22 @@ def _heads(t, name, shape, device):
     sb, sh, st, sw = t.stride()
     if sw != 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
-    return t.data_ptr(), shape[1], dt, sb, st, sh
-
-
-def _pack_heads(*fields):
-    """A buffer of tk_heads (keep it alive during the call) and the address of each, None if absent."""
-    n = len(fields)
-    buf = (tk_heads * n)()
-    _HEADS_PACK[n].pack_into(buf, 0, *itertools.chain.from_iterable(fields))
-    at = ctypes.addressof(buf)
-    return buf, [at + i * _HEADS_SIZE if f[1] else None for i, f in enumerate(fields)]
+    return _pack_heads(t.data_ptr(), shape[1], dt, sb, st, sh)
 
 
 def _weights(plan, q_weight, k_weight, device):
-    """The weights' type, checked, and their addresses."""
-    given = [(t, n) for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")) if t is not None]
-    kinds = {_HEADS_DTYPE.get(t.dtype) for t, _ in given}
+    """The weights' addresses and type, checked."""
+    kinds = {_HEADS_DTYPE.get(t.dtype) for t in (q_weight, k_weight) if t is not None}
     if None in kinds or len(kinds) > 1:
         raise TypeError("norm weights must be float32 or bfloat16, both alike")
-    for t, n in given:
-        _need(t, t.dtype, n, device)
-        if t.numel() != plan.r:
-            raise ValueError(f"{n} has {t.numel()} elements, expected {plan.r}")
-    return (None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
-            kinds.pop() if kinds else TK_F32)
+    at = [None, None]
+    for i, t in enumerate((q_weight, k_weight)):
+        if t is None:
+            continue
+        if not t.is_cuda or t.device != device or not t.is_contiguous() or t.numel() != plan.r:
+            raise ValueError(f"a norm weight must be {plan.r} contiguous elements on {device} (CUDA)")
+        at[i] = t.data_ptr()
+    return at[0], at[1], kinds.pop() if kinds else TK_F32
 
 
 def _positions(plan, positions, B, S, device):
@@ -617,12 +607,14 @@ def _positions(plan, positions, B, S, device):
     return positions.data_ptr(), stride[0], stride[1]
 
 
-def _dims(*tensors):
+def _first(*tensors):
+    """(batch, tokens, device) by the first tensor that is there."""
     for t in tensors:
         if t is not None:
             if t.dim() != 4:
                 raise ValueError(f"expected [B, H, S, width] tensors, got {tuple(t.shape)}")
-            return t.shape[0], t.shape[2], t.device
+            B, _, S, _ = t.shape
+            return B, S, t.device
     raise ValueError("q, k and v are all None")
 
 
@@ -636,15 +628,14 @@ def tk_qk_norm_rope(plan: tk_rope_desc, q, k, v, positions, q_out, k_out, v_out,
     change of v [B, H_kv, S, d_v], in one launch.  Tensors are [B, H, S, width] with any strides
     (a transposed slice of a packed projection, say); bf16 or fp32 in and out.  positions int32
     [B, S] or [n_axes, B, S].  Any of the three may be None together with its output."""
-    B, S, dev = _dims(q, k, v)
-    dv = 0 if v is None else v.shape[3]
-    sq, sk, sv = _shape(q, B, S, plan.r), _shape(k, B, S, plan.r), _shape(v, B, S, dv)
-    _buf, h = _pack_heads(
-        _heads(q, "q", sq, dev), _heads(k, "k", sk, dev), _heads(v, "v", sv, dev),
-        _heads(q_out, "q_out", sq, dev), _heads(k_out, "k_out", sk, dev), _heads(v_out, "v_out", sv, dev))
+    B, S, dev = _first(q, k, v)
+    r, dv = plan.r, 0 if v is None else v.shape[3]
+    sq, sk, sv = _shape(q, B, S, r), _shape(k, B, S, r), _shape(v, B, S, dv)
     st = load_library().tk_qk_norm_rope(
-        ctypes.byref(plan), B, S, dv, h[0], h[1], h[2], *_weights(plan, q_weight, k_weight, dev),
-        *_positions(plan, positions, B, S, dev), h[3], h[4], h[5], _raw_stream(stream))
+        ctypes.byref(plan), B, S, dv, _heads(q, "q", sq, dev), _heads(k, "k", sk, dev), _heads(v, "v", sv, dev),
+        *_weights(plan, q_weight, k_weight, dev), *_positions(plan, positions, B, S, dev),
+        _heads(q_out, "q_out", sq, dev), _heads(k_out, "k_out", sk, dev), _heads(v_out, "v_out", sv, dev),
+        _raw_stream(stream))
     if st != TK_OK:
         _check(st, "tk_qk_norm_rope")
     return q_out, k_out, v_out
@@ -653,22 +644,21 @@ def tk_qk_norm_rope(plan: tk_rope_desc, q, k, v, positions, q_out, k_out, v_out,
 def _append_args(cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight, stream):
     """Checked and marshalled arguments of tk_qk_norm_rope_append, and what they point into."""
     d = cache.desc
-    B, S, dev = _dims(k)
+    B, S, dev = _first(k)
     if v is None or v.dim() != 4:
         raise ValueError("k and v are required")
     sq, sk = (B, d.h_q, S, plan.r), (B, d.h_kv, S, plan.r)
-    buf, h = _pack_heads(_heads(q, "q", sq, dev), _heads(k, "k", sk, dev),
-                         _heads(v, "v", (B, d.h_kv, S, d.d_v), dev), _heads(q_out, "q_out", sq, dev))
     _need(slots, torch.int32, "slots", dev)
     if slots.numel() != B * S:
         raise ValueError(f"slots has {slots.numel()} entries for {B * S} tokens")
     for t, n in ((cache.k, "cache.k"), (cache.v, "cache.v"), (cache.k_scale, "cache.k_scale")):
         if t is not None and t.device != dev:
             raise ValueError(f"{n} is on {t.device}, expected {dev}")
-    args = (ctypes.byref(d), ctypes.byref(plan), B, S, h[0], h[1], h[2],
-            *_weights(plan, q_weight, k_weight, dev), *_positions(plan, positions, B, S, dev), _ptr(slots),
-            h[3], _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_scale), _stream(stream))
-    return args, (cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight, buf)
+    args = (ctypes.byref(d), ctypes.byref(plan), B, S, _heads(q, "q", sq, dev), _heads(k, "k", sk, dev),
+            _heads(v, "v", (B, d.h_kv, S, d.d_v), dev), *_weights(plan, q_weight, k_weight, dev),
+            *_positions(plan, positions, B, S, dev), _ptr(slots), _heads(q_out, "q_out", sq, dev),
+            _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_scale), _stream(stream))
+    return args, (cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight)
 
 
 def tk_qk_norm_rope_append(cache: ThinKeyCache, plan: tk_rope_desc, q, k, v, positions, slots, q_out,
@@ -704,28 +694,28 @@ def tk_qk_norm_rope_backward(plan: tk_rope_desc, q, k, positions, dq_out, dk_out
     a packed gradient, say) and the weights' dq_weight, dk_weight [r] fp32.  q and k (the
     forward's inputs) may be None for a plan without norm.  Weight gradients need a workspace
     (qk_norm_rope_workspace; allocated here if None)."""
-    B, S, dev = _dims(dq_out, dk_out, dv_out)
-    width = 0 if dv_out is None else dv_out.shape[3]
-    sq, sk, sv = _shape(dq_out, B, S, plan.r), _shape(dk_out, B, S, plan.r), _shape(dv_out, B, S, width)
+    B, S, dev = _first(dq_out, dk_out, dv_out)
+    r, width = plan.r, 0 if dv_out is None else dv_out.shape[3]
+    sq, sk, sv = _shape(dq_out, B, S, r), _shape(dk_out, B, S, r), _shape(dv_out, B, S, width)
     if not plan.norm:
         q = k = None
-    _buf, h = _pack_heads(
-        _heads(q, "q", sq, dev), _heads(k, "k", sk, dev), _heads(dq_out, "dq_out", sq, dev),
-        _heads(dk_out, "dk_out", sk, dev), _heads(dv_out, "dv_out", sv, dev), _heads(dq, "dq", sq, dev),
-        _heads(dk, "dk", sk, dev), _heads(dv, "dv", sv, dev))
     for t, n in ((dq_weight, "dq_weight"), (dk_weight, "dk_weight")):
-        _need(t, torch.float32, n, dev)
-        if t is not None and t.numel() != plan.r:
-            raise ValueError(f"{n} has {t.numel()} elements, expected {plan.r}")
-    if workspace is None and (dq_weight is not None or dk_weight is not None):
-        workspace = qk_norm_rope_workspace(plan, dev)
-    _need(workspace, torch.uint8, "workspace", dev)
+        if t is not None:
+            _need(t, torch.float32, n, dev)
+            if t.numel() != r:
+                raise ValueError(f"{n} has {t.numel()} elements, expected {r}")
+    if workspace is None:
+        if dq_weight is not None or dk_weight is not None:
+            workspace = qk_norm_rope_workspace(plan, dev)
+    else:
+        _need(workspace, torch.uint8, "workspace", dev)
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     st = load_library().tk_qk_norm_rope_backward(
-        ctypes.byref(plan), B, S, width, h[0], h[1], *_weights(plan, q_weight, k_weight, dev),
-        *_positions(plan, positions, B, S, dev), *h[2:], None if dq_weight is None else dq_weight.data_ptr(),
-        None if dk_weight is None else dk_weight.data_ptr(),
-        None if workspace is None else workspace.data_ptr(),
-        0 if workspace is None else workspace.numel(), _raw_stream(stream))
+        ctypes.byref(plan), B, S, width, _heads(q, "q", sq, dev), _heads(k, "k", sk, dev),
+        *_weights(plan, q_weight, k_weight, dev), *_positions(plan, positions, B, S, dev),
+        _heads(dq_out, "dq_out", sq, dev), _heads(dk_out, "dk_out", sk, dev), _heads(dv_out, "dv_out", sv, dev),
+        _heads(dq, "dq", sq, dev), _heads(dk, "dk", sk, dev), _heads(dv, "dv", sv, dev), at(dq_weight),
+        at(dk_weight), at(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(stream))
     if st != TK_OK:
         _check(st, "tk_qk_norm_rope_backward")
     return dq, dk, dv

@@ -5,19 +5,22 @@
 //
 // Everything follows from prefix sums over the sequences (wanted tokens,
 // needed pages, returned pages, granted tokens).  Each block computes them for
-// the whole batch in shared memory (a few microseconds' worth of latency, no
-// matter how many blocks do it), then fills its share of the slot map,
+// the whole batch in shared memory, then fills its share of the slot map,
 // looking up a row's sequence by binary search.  No block waits for another:
 // a page taken by this call is found from the prefix sums and the free stack,
 // never from the page-table entry another block may not have written yet.
 // Entries written (pages past a sequence's old ones, stack entries from the
 // old top upwards) are never read by the call that writes them, so lengths and
 // the free count are the only values read by all and changed: the last block
-// to arrive writes those, which lets the caller pass the same arrays in and
-// out.
+// to have read them writes those, which lets the caller pass the same arrays
+// in and out.
 //
-// Bound by latency: one launch, two dependent loads and the scans; for large
-// prompts by the 8 bytes a token written.
+// Bound by latency: one launch, two dependent loads and one scan (three where
+// a request is refused); for large prompts by the 8 bytes a token written.
+// The second load (each sequence's partly filled page, the stack's top) is
+// issued before the scan and lands behind it.
+#include <algorithm>
+
 #include "common.cuh"
 #include "kernels.h"
 #include "qk.h"
@@ -25,144 +28,165 @@
 namespace tk {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+using int64 = long long;
 
-// Exclusive prefix sums over the block of one value a thread each, two at a
-// time; *ta and *tb: their totals.
-template <typename A, typename B>
-__device__ __forceinline__ void block_scan2(A& a, B& b, A* ta, B* tb, A* sa, B* sb) {
+constexpr int kBack = 4;   // returned pages a thread copies at a time
+
+// Exclusive prefix sums over the block of two values a thread each, and their
+// totals.  sm: 2 * kWarps values.
+template <int kWarps>
+__device__ __forceinline__ void block_scan(int64& a, int64& b, int64* total_a, int64* total_b, int64* sm) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  A ia = a;
-  B ib = b;
+  int64 ia = a, ib = b;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const A ya = __shfl_up_sync(0xffffffffu, ia, o);
-    const B yb = __shfl_up_sync(0xffffffffu, ib, o);
+    const int64 ya = __shfl_up_sync(0xffffffffu, ia, o), yb = __shfl_up_sync(0xffffffffu, ib, o);
     if (lane >= o) ia += ya, ib += yb;
   }
-  __syncthreads();           // the arrays' previous use is over
-  if (lane == 31) sa[warp] = ia, sb[warp] = ib;
+  __syncthreads();           // the array's previous use is over
+  if (lane == 31) sm[warp] = ia, sm[kWarps + warp] = ib;
   __syncthreads();
-  A pa = 0, xa = 0;
-  B pb = 0, xb = 0;
+  int64 wa = lane < kWarps ? sm[lane] : 0, wb = lane < kWarps ? sm[kWarps + lane] : 0;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) pa += sa[w], pb += sb[w];
-    xa += sa[w], xb += sb[w];
+  for (int o = 1; o < kWarps; o <<= 1) {
+    const int64 ya = __shfl_up_sync(0xffffffffu, wa, o), yb = __shfl_up_sync(0xffffffffu, wb, o);
+    if (lane >= o) wa += ya, wb += yb;
   }
-  a = pa + ia - a;
-  b = pb + ib - b;
-  *ta = xa;
-  *tb = xb;
+  const int64 pa = __shfl_sync(0xffffffffu, wa, warp > 0 ? warp - 1 : 0);
+  const int64 pb = __shfl_sync(0xffffffffu, wb, warp > 0 ? warp - 1 : 0);
+  *total_a = __shfl_sync(0xffffffffu, wa, kWarps - 1);
+  *total_b = __shfl_sync(0xffffffffu, wb, kWarps - 1);
+  a = ia - a + (warp > 0 ? pa : 0);
+  b = ib - b + (warp > 0 ? pb : 0);
 }
 
-struct Shared {
-  long long sa[kWarps];
-  int sb[kWarps];
-  int last;
-};
+// Two counts below 2^31 in one value to scan.
+__device__ __forceinline__ int64 pair_of(int64 hi, int64 lo) { return (hi << 32) + lo; }
+__device__ __forceinline__ int high(int64 x) { return static_cast<int>(x >> 32); }
+__device__ __forceinline__ int low(int64 x) { return static_cast<int>(x & 0xffffffffll); }
 
-// K: sequences of one thread; kPer: rows of the slot map that it fills at a
-// time.
-template <int K, int kPer>
+// kThreads: of a block; K: sequences of one thread; kPer: rows of the slot map
+// that it fills at a time.
+template <int kThreads, int K, int kPer>
 __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_constant__ BlockTableParams p) {
+  constexpr int kWarps = kThreads / 32;
   extern __shared__ int dyn[];
-  __shared__ Shared sh;
+  __shared__ int64 scan[2 * kWarps];
+  __shared__ int top[kThreads];         // the stack's first kThreads entries from the old top
+  __shared__ int last;
   int* tok = dyn;                       // [B + 1] first granted token (exclusive prefix)
-  int* len = dyn + (p.B + 1);           // [B] cached tokens
-  int* pop = dyn + (2 * p.B + 1);       // [B] pages taken before the sequence's - its old pages
-  int* ret = dyn + (3 * p.B + 1);       // [B + 1] pages returned before the sequence's
+  int* ret = tok + p.B + 1;             // [B + 1] pages returned before the sequence's
+  int* len = ret + p.B + 1;             // [B] cached tokens
+  int* pop = len + p.B;                 // [B] pages taken before the sequence's - its old pages
+  int* cur = pop + p.B;                 // [B] its partly filled page
   const int ps = p.page_size;
+  const int64 row_tokens = static_cast<int64>(p.max_pages) * ps;     // at most 2^30
   pdl_wait();
   pdl_trigger();
 
   const int b0 = threadIdx.x * K;
-  int L[K], want[K], held[K];
-  bool done[K], valid[K];
+  int L[K], n[K];
   int f = *p.free_count;
-  bool bad = f < 0 || f > p.num_pages;
-  f = min(max(f, 0), p.num_pages);
 #pragma unroll
   for (int i = 0; i < K; ++i) {
     const bool in = b0 + i < p.B;
     L[i] = in ? p.seq_lens[b0 + i] : 0;
-    const int n = in ? p.new_lens[b0 + i] : 0;
-    valid[i] = L[i] >= 0 && n >= -1 && L[i] <= static_cast<long long>(p.max_pages) * ps;
-    bad |= !valid[i];
-    if (!valid[i]) L[i] = max(0, static_cast<int>(min(static_cast<long long>(L[i]), static_cast<long long>(p.max_pages) * ps)));
-    done[i] = n == -1 && valid[i];
-    want[i] = max(n, 0);
+    n[i] = in ? p.new_lens[b0 + i] : 0;
+  }
+  bool bad = f < 0 || f > p.num_pages;
+  f = min(max(f, 0), p.num_pages);
+  const int my_top = static_cast<int>(threadIdx.x) < f ? p.free_pages[f - 1 - static_cast<int>(threadIdx.x)] : -1;
+
+  // Pages held, tokens wanted and pages needed, by what a request's own numbers
+  // say; `odd`: one that cannot be served whatever the others are.
+  int want[K], held[K], need[K], page[K];
+  bool done[K], fits[K], odd = false;
+  int64 wanted = 0, pages = 0;          // pages: needed, returned
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const bool valid = L[i] >= 0 && n[i] >= -1 && L[i] <= row_tokens;
+    bad |= !valid;
+    L[i] = static_cast<int>(min(max(static_cast<int64>(L[i]), 0ll), row_tokens));
+    done[i] = valid && n[i] == -1;
+    want[i] = max(n[i], 0);
     held[i] = (L[i] + (ps - 1)) >> p.page_shift;
+    page[i] = -1;
+    if (b0 + i < p.B && (L[i] & (ps - 1)) != 0)
+      page[i] = p.page_table[static_cast<size_t>(b0 + i) * p.max_pages + (L[i] >> p.page_shift)];
+    const int64 to = static_cast<int64>(L[i]) + want[i];
+    fits[i] = valid && !done[i] && to <= row_tokens && (!p.per_seq || want[i] <= p.per_seq);
+    odd |= !fits[i] && !done[i];
+    need[i] = fits[i] ? static_cast<int>((to + ps - 1) >> p.page_shift) - held[i] : 0;
+    wanted += want[i];
+    pages += pair_of(need[i], done[i] ? held[i] : 0);
   }
   if (bad && blockIdx.x == 0) record_error(p.err, TK_DEVERR_INDEX);
-
-  // 1. tokens wanted up to each sequence (64 bits: nothing bounds them) and pages returned
-  long long a = 0, ta;
-  int r = 0, total_ret;
+  int64 total_wanted, total_pages;
+  block_scan<kWarps>(wanted, pages, &total_wanted, &total_pages, scan);
+  // the whole block has read the lengths and the free count
+  if (threadIdx.x == 0 && gridDim.x > 1)
+    last = atomicAdd(p.counter, 1) == static_cast<int>(gridDim.x) - 1;
+  const int total_ret = low(total_pages);
+  const int64 avail = static_cast<int64>(f) + total_ret;
+  int first_ret = low(pages);
+  int m[K], first, total_tokens, total_taken, total_refused = 0;
+  int64 taken0;                         // pages needed before the thread's first sequence
+  const bool all = !__syncthreads_or(odd || (!p.per_seq && total_wanted > p.rows) || high(total_pages) > avail);
+  if (all) {                            // every request is granted
 #pragma unroll
-  for (int i = 0; i < K; ++i) a += want[i], r += done[i] ? held[i] : 0;
-  block_scan2(a, r, &ta, &total_ret, sh.sa, sh.sb);
-  const int ret0 = r;
-  // 2. pages needed by the requests that fit the table and the slot map
-  long long need_sum = 0;
-  int need[K];
-  bool fits[K];
-#pragma unroll
-  for (int i = 0; i < K; ++i) {
-    a += want[i];
-    const long long to = static_cast<long long>(L[i]) + want[i];
-    fits[i] = valid[i] && !done[i] && to <= static_cast<long long>(p.max_pages) * ps &&
-              (p.per_seq ? want[i] <= p.per_seq : a <= p.rows);
-    need[i] = fits[i] ? static_cast<int>((to + ps - 1) >> p.page_shift) - held[i] : 0;
-    need_sum += need[i];
-  }
-  int unused = 0, tu;
-  block_scan2(need_sum, unused, &ta, &tu, sh.sa, sh.sb);
-  // 3. requests granted, in order; their tokens, pages taken, requests refused
-  const long long avail = static_cast<long long>(f) + total_ret;
-  int m[K], tokens = 0, refused = 0;
-  long long taken = 0;
-  long long upto = need_sum;
-#pragma unroll
-  for (int i = 0; i < K; ++i) {
-    const bool in = b0 + i < p.B;
-    const long long before = upto;
-    upto += need[i];
-    const bool given = fits[i] && (need[i] == 0 || upto <= avail);
-    m[i] = given ? want[i] : 0;
-    tokens += m[i];
-    refused += in && !done[i] && !given;
-    taken += given ? need[i] : 0;
-    if (in) {
-      len[b0 + i] = L[i];
-      pop[b0 + i] = static_cast<int>(before) - held[i];
-    }
-  }
-  int first = tokens, total_tokens;
-  // the granted pages are a prefix of the needed ones, so their count is also
-  // the position the stack has been popped to
-  long long refused_taken = (static_cast<long long>(refused) << 40) + taken;
-  long long total_rt;
-  block_scan2(refused_taken, first, &total_rt, &total_tokens, sh.sa, sh.sb);
-  const int total_taken = static_cast<int>(total_rt & ((1ll << 40) - 1));
-  const int total_refused = static_cast<int>(total_rt >> 40);
-  {
-    int t = first, rr = ret0;
+    for (int i = 0; i < K; ++i) m[i] = want[i];
+    first = static_cast<int>(wanted);
+    total_tokens = static_cast<int>(total_wanted);
+    taken0 = high(pages);
+    total_taken = high(total_pages);
+  } else {
+    // pages needed by the requests that also fit the slot map
+    int64 upto = wanted, needed = 0, unused = 0, t0, t1;
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-      if (b0 + i < p.B) {
-        tok[b0 + i] = t;
-        ret[b0 + i] = rr;
-        if (p.offsets && blockIdx.x == 0) p.offsets[b0 + i] = t;
-      }
-      t += m[i];
-      rr += done[i] ? held[i] : 0;
+      upto += want[i];
+      if (!p.per_seq && upto > p.rows) fits[i] = false;
+      if (!fits[i]) need[i] = 0;
+      needed += need[i];
     }
-    if (threadIdx.x == 0) {
-      tok[p.B] = total_tokens;
-      ret[p.B] = total_ret;
-      if (p.offsets && blockIdx.x == 0) p.offsets[p.B] = total_tokens;
+    block_scan<kWarps>(needed, unused, &t0, &t1, scan);
+    taken0 = needed;
+    // requests granted, in order; the granted pages are a prefix of the needed
+    // ones, so their count is where the stack has been popped to
+    int64 counts = 0, tokens_taken = 0;   // refused; tokens, pages taken
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      needed += need[i];
+      const bool given = fits[i] && (need[i] == 0 || needed <= avail);
+      m[i] = given ? want[i] : 0;
+      counts += b0 + i < p.B && !done[i] && !given;
+      tokens_taken += pair_of(m[i], given ? need[i] : 0);
     }
+    block_scan<kWarps>(counts, tokens_taken, &t0, &t1, scan);
+    total_refused = static_cast<int>(t0);
+    first = high(tokens_taken);
+    total_tokens = high(t1);
+    total_taken = low(t1);
+  }
+  top[threadIdx.x] = my_top;
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    if (b0 + i < p.B) {
+      tok[b0 + i] = first;
+      ret[b0 + i] = first_ret;
+      len[b0 + i] = L[i];
+      pop[b0 + i] = static_cast<int>(taken0) - held[i];     // used for granted requests only
+      cur[b0 + i] = page[i];
+      if (p.offsets && blockIdx.x == 0) p.offsets[b0 + i] = first;
+    }
+    first += m[i];
+    first_ret += done[i] ? held[i] : 0;
+    taken0 += need[i];
+  }
+  if (threadIdx.x == 0) {
+    tok[p.B] = total_tokens;
+    ret[p.B] = total_ret;
+    if (p.offsets && blockIdx.x == 0) p.offsets[p.B] = total_tokens;
   }
   __syncthreads();
 
@@ -181,25 +205,46 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
     const int b = owner(ret, i);
     return p.page_table[static_cast<size_t>(b) * p.max_pages + (i - ret[b])];
   };
-  auto checked = [&](int page) {
-    if (page >= 0 && page < p.num_pages) return page;
+  auto checked = [&](int id) {
+    if (id >= 0 && id < p.num_pages) return id;
     record_error(p.err, TK_DEVERR_INDEX);
     return -1;
   };
+  // the j-th page popped: first the returned pages, last one first, then the
+  // stack from its old top
+  auto popped = [&](int j) {
+    if (j < total_ret) return returned(total_ret - 1 - j);
+    const int down = j - total_ret;
+    return down < kThreads ? top[down] : p.free_pages[f - 1 - down];
+  };
 
-  // the stack's new top entries: the returned pages that were not taken again
+  // the stack's new top entries: the returned pages that were not taken again,
+  // kBack neighbours a thread (their loads overlap; mostly one sequence's row)
   const int stride = static_cast<int>(gridDim.x) * kThreads;
-  const int tid = blockIdx.x * kThreads + threadIdx.x;
+  const int tid = static_cast<int>(blockIdx.x) * kThreads + static_cast<int>(threadIdx.x);
   const int left = total_ret - total_taken;
-  for (int i = tid; i < left; i += stride) {
-    if (f + i < p.num_pages) p.free_pages[f + i] = returned(i);
-    else record_error(p.err, TK_DEVERR_INDEX);     // more free pages than the pool has
+  for (int64 i0 = static_cast<int64>(tid) * kBack; i0 < left; i0 += static_cast<int64>(stride) * kBack) {
+    int b = owner(ret, static_cast<int>(i0)), id[kBack];
+#pragma unroll
+    for (int k = 0; k < kBack; ++k) {
+      const int i = static_cast<int>(i0) + k;
+      if (i0 + k >= left) continue;
+      while (i >= ret[b + 1]) ++b;
+      id[k] = p.page_table[static_cast<size_t>(b) * p.max_pages + (i - ret[b])];
+    }
+#pragma unroll
+    for (int k = 0; k < kBack; ++k) {
+      if (i0 + k >= left) continue;
+      const int64 to = f + i0 + k;
+      if (to < p.num_pages) p.free_pages[to] = id[k];
+      else record_error(p.err, TK_DEVERR_INDEX);     // more free pages than the pool has
+    }
   }
 
   // the slot map
-  for (int64_t row0 = static_cast<int64_t>(tid) * kPer; row0 < p.rows; row0 += static_cast<int64_t>(stride) * kPer) {
+  for (int64 row0 = static_cast<int64>(tid) * kPer; row0 < p.rows; row0 += static_cast<int64>(stride) * kPer) {
     int slot[kPer], pos[kPer];
-    int b = -1, page_of = -1, page = -1;
+    int b = -1, page_of = -1, id = -1;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int row = static_cast<int>(row0) + i;
@@ -224,17 +269,15 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
       const int pi = pos[i] >> p.page_shift;
       if (pi != page_of) {
         page_of = pi;
-        const int old = (len[b] + (ps - 1)) >> p.page_shift;
-        int32_t* entry = p.page_table + static_cast<size_t>(b) * p.max_pages + pi;
-        if (pi < old) {
-          page = checked(*entry);
+        if (pi < (len[b] + (ps - 1)) >> p.page_shift) {
+          id = checked(cur[b]);
         } else {
-          const int s = f + total_ret - 1 - (pop[b] + pi);     // entry of the stack
-          page = checked(s < f ? p.free_pages[s] : returned(s - f));
-          if ((pos[i] & (ps - 1)) == 0) *entry = page;        // its first token writes it
+          id = checked(popped(pop[b] + pi));
+          if ((pos[i] & (ps - 1)) == 0)                    // its first token writes the entry
+            p.page_table[static_cast<size_t>(b) * p.max_pages + pi] = id;
         }
       }
-      if (page >= 0) slot[i] = (page << p.page_shift) + (pos[i] & (ps - 1));
+      if (id >= 0) slot[i] = (id << p.page_shift) + (pos[i] & (ps - 1));
     }
     if (kPer == 4 && row0 + kPer <= p.rows) {
       *reinterpret_cast<int4*>(p.slots + row0) = make_int4(slot[0], slot[1 % kPer], slot[2 % kPer], slot[3 % kPer]);
@@ -246,13 +289,9 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
     }
   }
 
-  // lengths and the free count, once every block has read them
+  // lengths and the free count, by the block that was the last to read them
   if (gridDim.x > 1) {
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) sh.last = atomicAdd(p.counter, 1) == static_cast<int>(gridDim.x) - 1;
-    __syncthreads();
-    if (!sh.last) return;
+    if (!last) return;
     if (threadIdx.x == 0) *p.counter = 0;
   }
 #pragma unroll
@@ -264,35 +303,44 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
   }
 }
 
-template <int K, int kPer>
+template <int kThreads, int K, int kPer>
 cudaError_t launch_t(const BlockTableParams& p, int num_sms, cudaStream_t s) {
-  const size_t smem = (4 * static_cast<size_t>(p.B) + 2) * sizeof(int);
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(block_tables_kernel<K, kPer>,
+  const size_t smem = (5 * static_cast<size_t>(p.B) + 2) * sizeof(int);
+  if (smem > 32 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(block_tables_kernel<kThreads, K, kPer>,
                                                cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                static_cast<int>(smem));
     if (e != cudaSuccess) return e;
   }
-  const int64_t want = (static_cast<int64_t>(p.rows) + kThreads * kPer - 1) / (kThreads * kPer);
-  const unsigned grid = static_cast<unsigned>(want < 1 ? 1 : want > num_sms ? num_sms : want);
-  return launch_pdl(block_tables_kernel<K, kPer>, dim3(grid), dim3(kThreads), smem, s, p);
+  // Blocks for the rows, and for an eighth of the pages that finished requests
+  // could hold: how many they do hold only the device knows (one block took 16
+  // us to put back the 2400 pages of three long requests).
+  const int64_t held = std::min(static_cast<int64_t>(p.num_pages), static_cast<int64_t>(p.B) * p.max_pages);
+  auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  const int64_t want = std::max(up(p.rows, kThreads * kPer),
+                                std::min(up(held, 8 * kThreads * kBack), static_cast<int64_t>(num_sms)));
+  const unsigned grid = static_cast<unsigned>(
+      std::min(std::max(want, static_cast<int64_t>(1)), 2 * static_cast<int64_t>(num_sms)));
+  return launch_pdl(block_tables_kernel<kThreads, K, kPer>, dim3(grid), dim3(kThreads), smem, s, p);
 }
 
 // Four rows a thread share a search and a page and store 16 bytes, but their
 // page loads follow one another; one row a thread does while that fills no
 // more than one block per SM.
-template <int K>
+template <int kThreads, int K>
 cudaError_t launch_k(const BlockTableParams& p, int num_sms, cudaStream_t s) {
-  if (p.rows <= num_sms * kThreads) return launch_t<K, 1>(p, num_sms, s);
-  return launch_t<K, 4>(p, num_sms, s);
+  if (p.rows <= num_sms * kThreads) return launch_t<kThreads, K, 1>(p, num_sms, s);
+  return launch_t<kThreads, K, 4>(p, num_sms, s);
 }
 
 }  // namespace
 
+// Small batches take small blocks, whose scan is shorter.
 cudaError_t launch_block_tables(const BlockTableParams& p, int num_sms, cudaStream_t s) {
-  if (p.B <= kThreads) return launch_k<1>(p, num_sms, s);
-  if (p.B <= 2 * kThreads) return launch_k<2>(p, num_sms, s);
-  return launch_k<kMaxTableBatch / kThreads>(p, num_sms, s);
+  if (p.B <= 128) return launch_k<128, 1>(p, num_sms, s);
+  if (p.B <= 512) return launch_k<512, 1>(p, num_sms, s);
+  if (p.B <= 1024) return launch_k<512, 2>(p, num_sms, s);
+  return launch_k<512, kMaxTableBatch / 512>(p, num_sms, s);
 }
 
 }  // namespace tk

@@ -53,11 +53,18 @@ struct QkParams {
   int x_f32, o_f32;         // type of q, k, v; type of qo, ko, vo
   uint32_t n_tokens;        // B * S
   FastDiv div_s;
-  // set by the launchers (plan_runs): heads a warp takes, how many such runs
-  // q, k and v have, groups of tokens, and units = groups x runs
+  // Set by the launchers.  Heads are taken in runs (heads of a run, number of
+  // runs of q, k and v) for groups of tokens (256 / r for q and k, 256 / d_v
+  // for v).
   int hq_run, hk_run, hv_run, nq, nk, nv;
-  uint32_t groups, groups_v, units_qk, units;
-  FastDiv div_qk, div_nq, div_nk, div_nv;   // by nq + nk, nq, nk, nv
+  FastDiv div_nq, div_nk, div_nqk, div_nv;
+  // forward: units = blocks of tokens x units of a block, which has block_qk
+  // groups of q and k and block_v of v
+  uint32_t units, block_qk, block_v;
+  FastDiv div_block, div_block_v;   // by the units of a block, by block_v
+  // backward: each warp's share of the units of q, k and v, how many warps take
+  // one more, and the warp that is the first of them
+  uint32_t share[3], more[3], turn[3];
   // append: k and v go to the cache at slots[token]
   const int32_t* slots;
   void* k_cache;

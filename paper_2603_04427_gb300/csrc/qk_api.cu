@@ -23,8 +23,8 @@ tk_status check_rope(const tk_rope_desc* d) {
     return fail(TK_ERR_INVALID_ARG, "layout=%d", d->layout);
   if (d->n_axes < 1 || d->n_axes > TK_ROPE_MAX_AXES)
     return fail(TK_ERR_INVALID_ARG, "n_axes=%d (1 .. %d)", d->n_axes, TK_ROPE_MAX_AXES);
-  if (d->norm && (!std::isfinite(d->eps) || !(d->eps > 0.f) || !std::isfinite(d->w_offset)))
-    return fail(TK_ERR_INVALID_ARG, "eps must be finite and positive, w_offset finite");
+  if (d->norm && (!std::isnormal(d->eps) || !(d->eps > 0.f) || !std::isfinite(d->w_offset)))
+    return fail(TK_ERR_INVALID_ARG, "eps must be a positive normal number, w_offset finite");
   for (int j = 0; j < d->rot_dim / 2; ++j) {
     if (!(std::fabs(d->inv_freq[j]) <= 4.f))
       return fail(TK_ERR_INVALID_ARG, "inv_freq[%d]=%g (finite, magnitude at most 4)", j,

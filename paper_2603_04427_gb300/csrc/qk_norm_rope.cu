@@ -1,225 +1,7 @@
-// Per-head RMS norm and rotation of queries and keys in one pass, from the
-// projection's token-major rows to the layout the attention reads, or (k and
-// v) straight into the cache.
-//
-//   y = x (mean(x^2) + eps)^(-1/2) (w + w_offset),
-//   (a, b) of pair j -> (a cos t - b sin t, a sin t + b cos t),
-//   t = position[axis j] * inv_freq[j]
-//
-// Nothing is computed twice and every element is read and written once, so
-// the bound is HBM for long prompts and the launch for single tokens.
-//
-// A warp takes the 256 / r tokens that fit its lanes (qk_row.cuh) and a run
-// of up to 8 heads, whose angles it computes once: four rows (two of fp32) are
-// loaded before the first is used, 64 bytes a lane, which with 32 warps an SM
-// covers HBM's latency.  Lanes of one store instruction hold neighbouring
-// tokens of one head, the contiguous direction of the head-major output.
-// Values are copied by further units of the same launch.
-#include "kernels.h"
-#include "qk_row.cuh"
+// Norm and rotation into strided tensors (the kernel is in qk_norm_rope.cuh).
+#include "qk_norm_rope.cuh"
 
 namespace tk {
-namespace {
-
-constexpr int kWarps = 4;
-
-// The cache row of kv head g for a slot: block = page or sequence.
-struct SlotRow {
-  int64_t block_row;   // block * h_kv * rows + offset
-  bool ok;
-};
-__device__ __forceinline__ SlotRow slot_row(const QkParams& p, uint32_t token, bool token_ok) {
-  SlotRow r{0, false};
-  if (!token_ok) return r;
-  const int slot = p.slots[token];
-  if (slot < 0) return r;              // no slot: the token is not cached
-  if (slot >= p.slot_limit) {
-    record_error(p.err, TK_DEVERR_INDEX);
-    return r;
-  }
-  uint32_t off;
-  const uint32_t block = p.div_rows.divmod(static_cast<uint32_t>(slot), &off);
-  r.block_row = static_cast<int64_t>(block) * p.k.n * p.slot_rows + off;
-  r.ok = true;
-  return r;
-}
-
-// A lane's eight key elements as codes: symmetric absmax per (token, kv head),
-// scale = amax / Q, code = clamp(rint(y / scale), -Q, Q), both quotients as
-// binary32 division rounds them, amax 0 storing scale 0 and zero codes.  y is
-// the fp32 result of the rotation, not rounded to bf16 first: one rounding
-// less than an append of bf16 keys makes.
-// y / scale takes the row's one reciprocal and two corrections by the FMA
-// remainder; after the first the quotient is off by less than a unit, and the
-// second then rounds as division does (Markstein, 1990).  Both operands are
-// scaled by a power of two where the remainder could underflow.  Eight
-// divisions a lane instead made the unrolled kernel miss the instruction
-// cache (5.6 of 12 stall cycles an instruction).
-template <int R, int KF>
-__device__ __forceinline__ void store_codes(const QkParams& p, int64_t row, bool ok, int sub, int oa,
-                                            int ob, const float* y) {
-  float amax = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[e]));
-  amax = row_max<R / 8>(amax);
-  if (!ok) return;
-  constexpr float Q = KF == 1 ? 127.0f : 7.0f;
-  const float scale = amax / Q;
-  const float up = scale < 1e-25f ? 0x1p100f : scale > 1e25f ? 0x1p-60f : 1.0f;
-  const bool plain = scale > 0.f && scale < INFINITY;
-  const float s = plain ? scale * up : 0.f;
-  const float inv = plain ? 1.0f / s : 0.f;
-  int code[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float a = y[e] * up;
-    float x = __fmul_rn(a, inv);
-    x = __fmaf_rn(__fmaf_rn(-x, s, a), inv, x);
-    x = __fmaf_rn(__fmaf_rn(-x, s, a), inv, x);
-    code[e] = static_cast<int>(fminf(fmaxf(rintf(x), -Q), Q));
-  }
-  unsigned char* k = static_cast<unsigned char*>(p.k_cache);
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int* c = code + 4 * half;
-    const int o = half ? ob : oa;      // a multiple of 4
-    if constexpr (KF == 1) {
-      *reinterpret_cast<uint32_t*>(k + row * R + o) =
-          (c[0] & 0xFF) | (c[1] & 0xFF) << 8 | (c[2] & 0xFF) << 16 | static_cast<uint32_t>(c[3] & 0xFF) << 24;
-    } else {
-      *reinterpret_cast<uint16_t*>(k + row * (R / 2) + o / 2) = static_cast<uint16_t>(
-          (c[0] & 0xF) | (c[1] & 0xF) << 4 | (c[2] & 0xF) << 8 | (c[3] & 0xF) << 12);
-    }
-  }
-  if (sub == 0) p.k_scale[row] = scale;
-}
-
-// KF: -1 = k and v go to strided tensors of type O, else to the cache with key
-// format KF (0 bf16, 1 int8, 2 int4).
-template <int R, bool PAIR, typename X, typename O, int KF>
-__global__ void __launch_bounds__(kWarps * 32, 7) norm_rope_kernel(const __grid_constant__ QkParams p) {
-  constexpr int G = R / 8, T = 32 / G;
-  constexpr int H = sizeof(X) == 2 ? 4 : 2;      // rows a lane holds at a time
-  const int lane = threadIdx.x & 31;
-  const uint32_t unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
-  if (unit >= p.units) return;
-  pdl_wait();
-  pdl_trigger();
-
-  if (unit >= p.units_qk) {
-    auto src = [&](uint32_t b, uint32_t s) {
-      return static_cast<const X*>(p.v.p) + b * p.v.sb + s * p.v.st;
-    };
-    if constexpr (KF < 0) {
-      copy_values<2 * H, X, O>(p, unit - p.units_qk, p.v.n, p.v.sh, p.vo.sh, lane, src,
-                               [&](uint32_t b, uint32_t s, uint32_t) {
-                                 return static_cast<O*>(p.vo.p) + b * p.vo.sb + s * p.vo.st;
-                               });
-    } else {
-      copy_values<2 * H, X, O>(p, unit - p.units_qk, p.v.n, p.v.sh,
-                               static_cast<int64_t>(p.slot_rows) * p.DV, lane, src,
-                               [&](uint32_t, uint32_t, uint32_t token) -> O* {
-                                 const SlotRow slot = slot_row(p, token, true);
-                                 return slot.ok ? static_cast<O*>(p.v_cache) + slot.block_row * p.DV : nullptr;
-                               });
-    }
-    return;
-  }
-
-  uint32_t run, s;
-  const uint32_t group = p.div_qk.divmod(unit, &run);
-  const int sub = lane % G;
-  const uint32_t token = group * T + lane / G;
-  const bool ok = token < p.n_tokens;
-  const uint32_t b = p.div_s.divmod(ok ? token : 0u, &s);
-  const bool is_q = run < static_cast<uint32_t>(p.nq);
-  const HeadsView in = is_q ? p.q : p.k;
-  const int per = is_q ? p.hq_run : p.hk_run;
-  const int h0 = static_cast<int>(is_q ? run : run - p.nq) * per;
-  const int nh = min(per, in.n - h0);
-  int oa, ob;
-  quad_offsets<PAIR>(sub, p.rot, &oa, &ob);
-  const X* src = static_cast<const X*>(in.p) + b * in.sb + s * in.st + h0 * in.sh;
-  Raw<X> raw[H];
-  auto load = [&](int h) {
-#pragma unroll
-    for (int i = 0; i < H; ++i) {
-      raw[i].zero();
-      if (ok && h + i < nh) raw[i].load(src + i * in.sh, oa, ob);
-    }
-    src += H * in.sh;
-  };
-  load(0);
-  SlotRow slot{0, false};
-  if (KF >= 0 && !is_q) slot = slot_row(p, token, ok);
-  float w[8];
-  load_weights(is_q ? p.wq : p.wk, p.w_f32, p.w_offset, oa, ob, w);
-  const Turns t = load_turns(p, sub, b, s, ok);
-  const HeadsView out = is_q ? p.qo : p.ko;
-  O* dst = static_cast<O*>(out.p) + b * out.sb + s * out.st + h0 * out.sh;
-  int64_t row = slot.block_row + static_cast<int64_t>(h0) * p.slot_rows;
-  for (int h = 0; h < nh; h += H) {
-#pragma unroll
-    for (int i = 0; i < H; ++i) {
-      if (h + i >= nh) break;
-      float y[8];
-      raw[i].get(y);
-      float ss = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ss = __fmaf_rn(y[e], y[e], ss);
-      // without norm the row is multiplied by 1, which changes no bit
-      const float rho = p.norm ? rsqrtf(__fmaf_rn(row_sum<G>(ss), 1.0f / R, p.eps)) : 1.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = __fmul_rn(__fmul_rn(y[e], rho), w[e]);
-      rotate8<PAIR, false>(y, t);
-      if (KF < 0 || is_q) {
-        if (ok) store_quads(dst, oa, ob, y);
-        dst += out.sh;
-      } else {
-        if constexpr (KF <= 0) {
-          if (slot.ok) store_quads(static_cast<__nv_bfloat16*>(p.k_cache) + row * R, oa, ob, y);
-        } else {
-          store_codes<R, KF>(p, row, slot.ok, sub, oa, ob, y);
-        }
-        row += p.slot_rows;
-      }
-    }
-    if (h + H < nh) load(h + H);
-  }
-}
-
-template <int R, typename X, typename O, int KF>
-cudaError_t launch_t(QkParams& p, int num_sms, cudaStream_t s) {
-  if (!plan_runs(p, num_sms, 8)) return cudaErrorInvalidConfiguration;
-  const dim3 grid((p.units + kWarps - 1) / kWarps), block(kWarps * 32);
-  return p.pair_layout ? launch_pdl(norm_rope_kernel<R, true, X, O, KF>, grid, block, 0, s, p)
-                       : launch_pdl(norm_rope_kernel<R, false, X, O, KF>, grid, block, 0, s, p);
-}
-
-template <typename X, typename O, int KF>
-cudaError_t by_r(QkParams& p, int num_sms, cudaStream_t s) {
-  switch (p.R) {
-    case 16:
-      if constexpr (KF != 2) return launch_t<16, X, O, KF>(p, num_sms, s);
-      break;  // int4 keys need r >= 32
-    case 32: return launch_t<32, X, O, KF>(p, num_sms, s);
-    case 64: return launch_t<64, X, O, KF>(p, num_sms, s);
-    case 128: return launch_t<128, X, O, KF>(p, num_sms, s);
-  }
-  return cudaErrorInvalidValue;
-}
-
-template <typename X>
-cudaError_t by_format(QkParams& p, int num_sms, cudaStream_t s) {
-  switch (p.k_fmt) {
-    case 0: return by_r<X, __nv_bfloat16, 0>(p, num_sms, s);
-    case 1: return by_r<X, __nv_bfloat16, 1>(p, num_sms, s);
-    case 2: return by_r<X, __nv_bfloat16, 2>(p, num_sms, s);
-  }
-  return cudaErrorInvalidValue;
-}
-
-}  // namespace
 
 cudaError_t launch_qk_norm_rope(const QkParams& params, int num_sms, cudaStream_t s) {
   QkParams p = params;
@@ -227,11 +9,6 @@ cudaError_t launch_qk_norm_rope(const QkParams& params, int num_sms, cudaStream_
     return p.o_f32 ? by_r<float, float, -1>(p, num_sms, s) : by_r<float, __nv_bfloat16, -1>(p, num_sms, s);
   return p.o_f32 ? by_r<__nv_bfloat16, float, -1>(p, num_sms, s)
                  : by_r<__nv_bfloat16, __nv_bfloat16, -1>(p, num_sms, s);
-}
-
-cudaError_t launch_qk_norm_rope_append(const QkParams& params, int num_sms, cudaStream_t s) {
-  QkParams p = params;
-  return p.x_f32 ? by_format<float>(p, num_sms, s) : by_format<__nv_bfloat16>(p, num_sms, s);
 }
 
 }  // namespace tk

@@ -7,9 +7,12 @@
 //   pair layout (pairs (2j, 2j + 1)):   A = elements 8l.., B = 8l + 4..
 // Either way lane l < rot/8 turns pairs 4l .. 4l+3, its angles are computed
 // once per token and stay in registers for all the heads it visits, and no
-// rotation crosses lanes.  The roundings are written out (__fmul_rn, __fmaf_rn)
-// so that every kernel built from these pieces gives the same bits.  Lanes past rot/8 hold eight neighbouring elements
+// rotation crosses lanes.  Lanes past rot/8 hold eight neighbouring elements
 // that are not rotated.
+// In registers the eight are a_0..a_3 and b_0..b_3, pair i = (a_i, b_i), packed
+// two to a 64-bit operand for Blackwell's two-wide fp32 instructions.  Every
+// rounding is written out, so all kernels built from these pieces give the
+// same bits.
 #pragma once
 
 #include <type_traits>
@@ -18,6 +21,9 @@
 #include "qk.h"
 
 namespace tk {
+
+// How a kernel finds its pairs: bit 0 = pair layout, bit 1 = rot_dim < R.
+constexpr int kModePair = 1, kModePart = 2;
 
 // Largest |position|: such integers are exact in binary32.
 constexpr int kMaxPosition = TK_ROPE_MAX_POSITION;
@@ -47,45 +53,68 @@ __device__ __forceinline__ void turn(int p, float f, float* c, float* s) {
 }
 
 // Where lane `sub` of a row's R / 8 lanes finds its quads.
-template <bool PAIR>
+template <int MODE>
 __device__ __forceinline__ void quad_offsets(int sub, int rot, int* a, int* b) {
-  const bool split = !PAIR && sub < rot / 8;
+  const bool split = !(MODE & kModePair) && (!(MODE & kModePart) || sub < rot / 8);
   *a = split ? 4 * sub : 8 * sub;
   *b = split ? rot / 2 + 4 * sub : 8 * sub + 4;
 }
+// The element that slot k of a lane (a_0..a_3, b_0..b_3) holds.
+template <int MODE>
+__device__ __forceinline__ int slot_element(int k, int oa, int ob) {
+  if (MODE & kModePair) return oa + (k < 4 ? 2 * k : 2 * (k - 4) + 1);
+  return k < 4 ? oa + k : ob + k - 4;
+}
 
-// The four angles of lane `sub` for the token at (b, s); token_ok = false
-// loads nothing.
-struct Turns {
-  float c[4], s[4];
-  bool on;   // the lane's elements are rotated
+// The positions of a lane's four pairs for the token at (b, s).
+struct Places {
+  int p[4];
 };
-__device__ __forceinline__ Turns load_turns(const QkParams& p, int sub, int b, int s, bool token_ok) {
-  Turns t;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) t.c[i] = 1.f, t.s[i] = 0.f;
-  t.on = sub < p.rot / 8 && token_ok;
-  if (t.on) {
+__device__ __forceinline__ Places load_places(const QkParams& p, int sub, int b, int s) {
+  Places r{{0, 0, 0, 0}};
+  if (sub < p.rot / 8) {
     const int32_t* row = p.pos + static_cast<int64_t>(b) * p.pos_sb + s;
-    int pos[4];
     if (p.n_axes == 1) {
-      pos[0] = row[0];
-      pos[1] = pos[2] = pos[3] = pos[0];
+      r.p[0] = row[0];
+      r.p[1] = r.p[2] = r.p[3] = r.p[0];
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pos[i] = row[p.pair_axis[4 * sub + i] * p.pos_sa];
+      for (int i = 0; i < 4; ++i) r.p[i] = row[p.pair_axis[4 * sub + i] * p.pos_sa];
     }
+  }
+  return r;
+}
+
+// cos, sin and -sin of a lane's four pairs.
+struct Turns {
+  float2 c[2], s[2], n[2];
+  bool on;   // the lane's elements are rotated
+};
+__device__ __forceinline__ Turns make_turns(const QkParams& p, int sub, const Places& at) {
+  float c[4] = {1.f, 1.f, 1.f, 1.f}, si[4] = {0.f, 0.f, 0.f, 0.f};
+  Turns t;
+  t.on = sub < p.rot / 8;
+  if (t.on) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (pos[i] > kMaxPosition || pos[i] < -kMaxPosition) {
-        record_error(p.err, TK_DEVERR_INDEX);
-        pos[i] = pos[i] > 0 ? kMaxPosition : -kMaxPosition;
-      }
-      turn(pos[i], p.inv_freq[4 * sub + i], &t.c[i], &t.s[i]);
+      const int q = min(max(at.p[i], -kMaxPosition), kMaxPosition);
+      if (q != at.p[i]) record_error(p.err, TK_DEVERR_INDEX);
+      turn(q, p.inv_freq[4 * sub + i], &c[i], &si[i]);
     }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    t.c[i] = make_float2(c[2 * i], c[2 * i + 1]);
+    t.s[i] = make_float2(si[2 * i], si[2 * i + 1]);
+    t.n[i] = make_float2(-si[2 * i], -si[2 * i + 1]);
   }
   return t;
 }
+
+// A lane's eight elements in slots: v[0], v[1] = a_0..a_3, v[2], v[3] = b_0..b_3.
+struct Row8 {
+  float2 v[4];
+};
 
 // Eight elements of a row as loaded: quads A and B, bf16 or fp32.
 template <typename X>
@@ -93,11 +122,11 @@ struct Raw;
 template <>
 struct Raw<__nv_bfloat16> {
   uint2 a, b;
-  __device__ __forceinline__ void zero() { a = b = make_uint2(0u, 0u); }
   __device__ __forceinline__ void load(const __nv_bfloat16* row, int oa, int ob) {
     a = *reinterpret_cast<const uint2*>(row + oa);
     b = *reinterpret_cast<const uint2*>(row + ob);
   }
+  // in the order of memory: quad A, quad B
   __device__ __forceinline__ void get(float* x) const {
     x[0] = bf16lo(a.x), x[1] = bf16hi(a.x), x[2] = bf16lo(a.y), x[3] = bf16hi(a.y);
     x[4] = bf16lo(b.x), x[5] = bf16hi(b.x), x[6] = bf16lo(b.y), x[7] = bf16hi(b.y);
@@ -106,7 +135,6 @@ struct Raw<__nv_bfloat16> {
 template <>
 struct Raw<float> {
   float4 a, b;
-  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
   __device__ __forceinline__ void load(const float* row, int oa, int ob) {
     a = *reinterpret_cast<const float4*>(row + oa);
     b = *reinterpret_cast<const float4*>(row + ob);
@@ -116,6 +144,42 @@ struct Raw<float> {
     x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
   }
 };
+
+// Between the order of memory and the slots.
+template <int MODE>
+__device__ __forceinline__ Row8 to_slots(const float* x) {
+  Row8 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (MODE & kModePair) {
+      r.v[i] = make_float2(x[4 * i], x[4 * i + 2]);
+      r.v[2 + i] = make_float2(x[4 * i + 1], x[4 * i + 3]);
+    } else {
+      r.v[i] = make_float2(x[2 * i], x[2 * i + 1]);
+      r.v[2 + i] = make_float2(x[4 + 2 * i], x[4 + 2 * i + 1]);
+    }
+  }
+  return r;
+}
+template <int MODE>
+__device__ __forceinline__ void to_memory(const Row8& r, float* x) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (MODE & kModePair) {
+      x[4 * i] = r.v[i].x, x[4 * i + 2] = r.v[i].y;
+      x[4 * i + 1] = r.v[2 + i].x, x[4 * i + 3] = r.v[2 + i].y;
+    } else {
+      x[2 * i] = r.v[i].x, x[2 * i + 1] = r.v[i].y;
+      x[4 + 2 * i] = r.v[2 + i].x, x[4 + 2 * i + 1] = r.v[2 + i].y;
+    }
+  }
+}
+template <int MODE, typename X>
+__device__ __forceinline__ Row8 slots_of(const Raw<X>& raw) {
+  float x[8];
+  raw.get(x);
+  return to_slots<MODE>(x);
+}
 
 // Two floats rounded to bf16 (nearest even), `lo` in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -130,47 +194,72 @@ __device__ __forceinline__ void store_quads(float* row, int oa, int ob, const fl
   *reinterpret_cast<float4*>(row + oa) = make_float4(y[0], y[1], y[2], y[3]);
   *reinterpret_cast<float4*>(row + ob) = make_float4(y[4], y[5], y[6], y[7]);
 }
+template <int MODE, typename O>
+__device__ __forceinline__ void store_row(O* row, int oa, int ob, const Row8& r) {
+  float y[8];
+  to_memory<MODE>(r, y);
+  store_quads(row, oa, ob, y);
+}
 
-// The lane's eight norm weights, offset added.
-__device__ __forceinline__ void load_weights(const void* w, int w_f32, float offset, int oa, int ob,
-                                             float* out) {
+// The lane's eight norm weights, offset added; 1 without weights.
+template <int MODE>
+__device__ __forceinline__ Row8 load_weights(const void* w, int w_f32, float offset, int oa, int ob) {
+  float x[8];
   if (w == nullptr) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] = 1.f;
-    return;
-  }
-  if (w_f32) {
-    Raw<float> t;
-    t.load(static_cast<const float*>(w), oa, ob);
-    t.get(out);
+    for (int e = 0; e < 8; ++e) x[e] = 1.f;
   } else {
-    Raw<__nv_bfloat16> t;
-    t.load(static_cast<const __nv_bfloat16*>(w), oa, ob);
-    t.get(out);
-  }
+    if (w_f32) {
+      Raw<float> t;
+      t.load(static_cast<const float*>(w), oa, ob);
+      t.get(x);
+    } else {
+      Raw<__nv_bfloat16> t;
+      t.load(static_cast<const __nv_bfloat16*>(w), oa, ob);
+      t.get(x);
+    }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) out[e] += offset;
+    for (int e = 0; e < 8; ++e) x[e] += offset;
+  }
+  return to_slots<MODE>(x);
 }
 
-// Pairs of a lane's eight elements: (i, i + 4) in the half layout,
-// (2i, 2i + 1) in the pair layout; y is turned by +angle, or by -angle when
-// BACK.  Elements outside rot_dim are selected, not multiplied by 1 and 0: an
-// infinity among them stays where it is.
-template <bool PAIR, bool BACK>
-__device__ __forceinline__ void rotate8(float* y, const Turns& t) {
+// The pairs turned by +angle, or by -angle when BACK.  Elements outside rot_dim
+// are selected, not multiplied by 1 and 0: an infinity among them stays where
+// it is.
+template <int MODE, bool BACK>
+__device__ __forceinline__ void rotate8(Row8& r, const Turns& t) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int ia = PAIR ? 2 * i : i, ib = PAIR ? 2 * i + 1 : i + 4;
-    const float s = BACK ? -t.s[i] : t.s[i];
-    const float a = y[ia], b = y[ib];
-    const float ra = __fmaf_rn(a, t.c[i], -__fmul_rn(b, s));
-    const float rb = __fmaf_rn(a, s, __fmul_rn(b, t.c[i]));
-    y[ia] = t.on ? ra : a;
-    y[ib] = t.on ? rb : b;
+  for (int i = 0; i < 2; ++i) {
+    const float2 a = r.v[i], b = r.v[2 + i];
+    const float2 ra = ffma2(b, BACK ? t.s[i] : t.n[i], fmul2(a, t.c[i]));
+    const float2 rb = ffma2(a, BACK ? t.n[i] : t.s[i], fmul2(b, t.c[i]));
+    if (MODE & kModePart) {
+      r.v[i] = t.on ? ra : a;
+      r.v[2 + i] = t.on ? rb : b;
+    } else {
+      r.v[i] = ra;
+      r.v[2 + i] = rb;
+    }
   }
 }
 
-// Sum over the G lanes of one row (neighbours inside a warp).
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// Sum over a lane's eight products x y.
+__device__ __forceinline__ float dot8(const Row8& x, const Row8& y) {
+  const float2 s = ffma2(x.v[3], y.v[3], ffma2(x.v[2], y.v[2], ffma2(x.v[1], y.v[1], fmul2(x.v[0], y.v[0]))));
+  return s.x + s.y;
+}
+
+// (mean square + eps)^(-1/2); the sum is at least eps, a normal number.
+__device__ __forceinline__ float inv_rms(float sum, float inv_r, float eps) {
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(__fmaf_rn(sum, inv_r, eps)));
+  return y;
+}
+
+// Sum or maximum over the G lanes of one row (neighbours inside a warp).
 template <int G>
 __device__ __forceinline__ float row_sum(float x) {
 #pragma unroll
@@ -212,71 +301,48 @@ struct Piece {
   }
 };
 
-// Value rows: DV / 8 lanes a row, so 256 / DV tokens a warp, and a run of heads
-// of which N are in flight.  src(b, s) and dst(b, s, token) give the lane's
-// address in head h0 (null: nothing is stored), heads are src_sh and dst_sh apart.
+// Value rows: DV / 8 lanes a row, so 256 / DV tokens a warp (group), and a run
+// of heads of which N are in flight.  src(b, s) and dst(b, s, token) give the
+// lane's address in head 0 (null: nothing is stored); heads are src_sh and
+// dst_sh apart.
 template <int N, typename X, typename O, typename Src, typename Dst>
-__device__ __forceinline__ void copy_values(const QkParams& p, uint32_t unit, int n_heads, int64_t src_sh,
-                                            int64_t dst_sh, int lane, Src src, Dst dst) {
-  uint32_t run, s;
-  const uint32_t group = p.div_nv.divmod(unit, &run);
+__device__ __forceinline__ void copy_values(const QkParams& p, uint32_t group, int run, int n_heads,
+                                            int64_t src_sh, int64_t dst_sh, int lane, Src src, Dst dst) {
   const int log_l = p.DV == 128 ? 4 : 3;
   const uint32_t token = (group << (5 - log_l)) + (lane >> log_l);
   if (token >= p.n_tokens) return;
+  uint32_t s;
   const uint32_t b = p.div_s.divmod(token, &s);
-  const int h0 = static_cast<int>(run) * p.hv_run;
+  const int h0 = run * p.hv_run;
   const int nh = min(p.hv_run, n_heads - h0);
   const int col = 8 * (lane & ((1 << log_l) - 1));
   const X* in = src(b, s) + h0 * src_sh + col;
   O* out = dst(b, s, token);
-  if (out) out += h0 * dst_sh + col;
+  const bool store = out != nullptr;
+  out += h0 * dst_sh + col;
   for (int h = 0; h < nh; h += N) {
     Piece<X, O> piece[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (h + i < nh) piece[i].load(in + i * src_sh);
+    for (int i = 0; i < N; ++i) {
+      if (h + i < nh) piece[i].load(in);
+      in += src_sh;
+    }
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (h + i < nh && out) piece[i].store(out + i * dst_sh);
-    in += N * src_sh;
-    if (out) out += N * dst_sh;
+    for (int i = 0; i < N; ++i) {
+      if (h + i < nh && store) piece[i].store(out);
+      out += dst_sh;
+    }
   }
 }
 
-// How a launch cuts its heads: a warp takes the tokens that fit its lanes
-// (256 / r of q and k, 256 / d_v of v) and a run of up to 8 heads.  Long runs
-// amortise the angles; while the launch is too small to give every SM
-// `want_warps` warps, the runs are halved, down to single heads.  False if
-// there are too many units for one launch.
-inline bool plan_runs(QkParams& p, int num_sms, int want_warps) {
-  auto up = [](uint64_t a, uint64_t b) { return (a + b - 1) / b; };
-  auto heads = [](const HeadsView& a, const HeadsView& b) { return a.p ? a.n : b.p ? b.n : 0; };
-  const int nq = heads(p.q, p.qo), nk = heads(p.k, p.ko), nv = heads(p.v, p.vo);
-  p.groups = static_cast<uint32_t>(up(p.n_tokens, 256 / p.R));
-  p.groups_v = static_cast<uint32_t>(up(p.n_tokens, 256 / p.DV));
-  for (int m = 8;; m /= 2) {
-    // even runs: 12 heads at most 8 at a time go as 6 + 6
-    auto cut = [&](int n, int* run) {
-      const int runs = static_cast<int>(up(n, m));
-      *run = runs ? static_cast<int>(up(n, runs)) : 1;
-      return static_cast<int>(up(n, *run));
-    };
-    p.nq = cut(nq, &p.hq_run);
-    p.nk = cut(nk, &p.hk_run);
-    p.nv = cut(nv, &p.hv_run);
-    const uint64_t qk = static_cast<uint64_t>(p.groups) * (p.nq + p.nk);
-    const uint64_t units = qk + static_cast<uint64_t>(p.groups_v) * p.nv;
-    if (m > 1 && units < static_cast<uint64_t>(num_sms) * want_warps) continue;
-    if (units >= (1ull << 31)) return false;
-    p.units_qk = static_cast<uint32_t>(qk);
-    p.units = static_cast<uint32_t>(units);
-    auto div = [](int n) { return FastDiv(static_cast<uint32_t>(n > 0 ? n : 1)); };
-    p.div_qk = div(p.nq + p.nk);
-    p.div_nq = div(p.nq);
-    p.div_nk = div(p.nk);
-    p.div_nv = div(p.nv);
-    return true;
-  }
+inline uint32_t div_up(uint32_t a, uint32_t b) { return a / b + (a % b != 0); }
+
+// Cuts `heads` into the fewest runs of at most `most`, as even as they come
+// (12 at most 8 at a time go as 6 + 6).  Returns their number, 0 for no heads.
+inline int cut_heads(int heads, int most, int* run) {
+  const int runs = (heads + most - 1) / most;
+  *run = runs ? (heads + runs - 1) / runs : 1;
+  return (heads + *run - 1) / *run;
 }
 
 }  // namespace tk

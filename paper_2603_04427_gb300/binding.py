@@ -559,15 +559,15 @@ _pack_heads = struct.Struct("Piiqqq").pack     # the layout of tk_heads
 
 
 def _heads(t, name, shape, device):
-    """A tk_heads, as bytes, for a tensor of logical shape [B, H, S, width], any strides with the
-    width contiguous; None for None."""
+    """A tk_heads, as bytes, for a tensor of logical shape [B, H, S, width] on the GPU of index
+    `device`, any strides with the width contiguous; None for None."""
     if t is None:
         return None
     dt = _HEADS_DTYPE.get(t.dtype)
     if dt is None:
         raise TypeError(f"{name} must be float32 or bfloat16")
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device} (CUDA)")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, expected CUDA device {device}")
     if t.shape != shape:
         raise ValueError(f"{name} is {tuple(t.shape)}, expected {shape}")
     sb, sh, st, sw = t.stride()
@@ -608,13 +608,15 @@ def _positions(plan, positions, B, S, device):
 
 
 def _first(*tensors):
-    """(batch, tokens, device) by the first tensor that is there."""
+    """(batch, tokens, device, its index) by the first tensor that is there."""
     for t in tensors:
         if t is not None:
             if t.dim() != 4:
                 raise ValueError(f"expected [B, H, S, width] tensors, got {tuple(t.shape)}")
+            if not t.is_cuda:
+                raise ValueError("expected CUDA tensors")
             B, _, S, _ = t.shape
-            return B, S, t.device
+            return B, S, t.device, t.get_device()
     raise ValueError("q, k and v are all None")
 
 
@@ -628,13 +630,13 @@ def tk_qk_norm_rope(plan: tk_rope_desc, q, k, v, positions, q_out, k_out, v_out,
     change of v [B, H_kv, S, d_v], in one launch.  Tensors are [B, H, S, width] with any strides
     (a transposed slice of a packed projection, say); bf16 or fp32 in and out.  positions int32
     [B, S] or [n_axes, B, S].  Any of the three may be None together with its output."""
-    B, S, dev = _first(q, k, v)
+    B, S, dev, at = _first(q, k, v)
     r, dv = plan.r, 0 if v is None else v.shape[3]
     sq, sk, sv = _shape(q, B, S, r), _shape(k, B, S, r), _shape(v, B, S, dv)
     st = load_library().tk_qk_norm_rope(
-        ctypes.byref(plan), B, S, dv, _heads(q, "q", sq, dev), _heads(k, "k", sk, dev), _heads(v, "v", sv, dev),
+        ctypes.byref(plan), B, S, dv, _heads(q, "q", sq, at), _heads(k, "k", sk, at), _heads(v, "v", sv, at),
         *_weights(plan, q_weight, k_weight, dev), *_positions(plan, positions, B, S, dev),
-        _heads(q_out, "q_out", sq, dev), _heads(k_out, "k_out", sk, dev), _heads(v_out, "v_out", sv, dev),
+        _heads(q_out, "q_out", sq, at), _heads(k_out, "k_out", sk, at), _heads(v_out, "v_out", sv, at),
         _raw_stream(stream))
     if st != TK_OK:
         _check(st, "tk_qk_norm_rope")
@@ -644,7 +646,7 @@ def tk_qk_norm_rope(plan: tk_rope_desc, q, k, v, positions, q_out, k_out, v_out,
 def _append_args(cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight, stream):
     """Checked and marshalled arguments of tk_qk_norm_rope_append, and what they point into."""
     d = cache.desc
-    B, S, dev = _first(k)
+    B, S, dev, at = _first(k)
     if v is None or v.dim() != 4:
         raise ValueError("k and v are required")
     sq, sk = (B, d.h_q, S, plan.r), (B, d.h_kv, S, plan.r)
@@ -654,9 +656,9 @@ def _append_args(cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weig
     for t, n in ((cache.k, "cache.k"), (cache.v, "cache.v"), (cache.k_scale, "cache.k_scale")):
         if t is not None and t.device != dev:
             raise ValueError(f"{n} is on {t.device}, expected {dev}")
-    args = (ctypes.byref(d), ctypes.byref(plan), B, S, _heads(q, "q", sq, dev), _heads(k, "k", sk, dev),
-            _heads(v, "v", (B, d.h_kv, S, d.d_v), dev), *_weights(plan, q_weight, k_weight, dev),
-            *_positions(plan, positions, B, S, dev), _ptr(slots), _heads(q_out, "q_out", sq, dev),
+    args = (ctypes.byref(d), ctypes.byref(plan), B, S, _heads(q, "q", sq, at), _heads(k, "k", sk, at),
+            _heads(v, "v", (B, d.h_kv, S, d.d_v), at), *_weights(plan, q_weight, k_weight, dev),
+            *_positions(plan, positions, B, S, dev), _ptr(slots), _heads(q_out, "q_out", sq, at),
             _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_scale), _stream(stream))
     return args, (cache, plan, q, k, v, positions, slots, q_out, q_weight, k_weight)
 
@@ -694,7 +696,7 @@ def tk_qk_norm_rope_backward(plan: tk_rope_desc, q, k, positions, dq_out, dk_out
     a packed gradient, say) and the weights' dq_weight, dk_weight [r] fp32.  q and k (the
     forward's inputs) may be None for a plan without norm.  Weight gradients need a workspace
     (qk_norm_rope_workspace; allocated here if None)."""
-    B, S, dev = _first(dq_out, dk_out, dv_out)
+    B, S, dev, at = _first(dq_out, dk_out, dv_out)
     r, width = plan.r, 0 if dv_out is None else dv_out.shape[3]
     sq, sk, sv = _shape(dq_out, B, S, r), _shape(dk_out, B, S, r), _shape(dv_out, B, S, width)
     if not plan.norm:
@@ -709,13 +711,13 @@ def tk_qk_norm_rope_backward(plan: tk_rope_desc, q, k, positions, dq_out, dk_out
             workspace = qk_norm_rope_workspace(plan, dev)
     else:
         _need(workspace, torch.uint8, "workspace", dev)
-    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     st = load_library().tk_qk_norm_rope_backward(
-        ctypes.byref(plan), B, S, width, _heads(q, "q", sq, dev), _heads(k, "k", sk, dev),
+        ctypes.byref(plan), B, S, width, _heads(q, "q", sq, at), _heads(k, "k", sk, at),
         *_weights(plan, q_weight, k_weight, dev), *_positions(plan, positions, B, S, dev),
-        _heads(dq_out, "dq_out", sq, dev), _heads(dk_out, "dk_out", sk, dev), _heads(dv_out, "dv_out", sv, dev),
-        _heads(dq, "dq", sq, dev), _heads(dk, "dk", sk, dev), _heads(dv, "dv", sv, dev), at(dq_weight),
-        at(dk_weight), at(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(stream))
+        _heads(dq_out, "dq_out", sq, at), _heads(dk_out, "dk_out", sk, at), _heads(dv_out, "dv_out", sv, at),
+        _heads(dq, "dq", sq, at), _heads(dk, "dk", sk, at), _heads(dv, "dv", sv, at), ptr(dq_weight),
+        ptr(dk_weight), ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(stream))
     if st != TK_OK:
         _check(st, "tk_qk_norm_rope_backward")
     return dq, dk, dv

@@ -28,11 +28,12 @@ constexpr int kWarps = 4;
 // Rows a lane holds at a time and blocks an SM holds.  With many waves, 128
 // bytes a lane and 20 warps an SM beat 64 bytes and 28 warps (2 x 9721 tokens
 // in fp32: 53 us against 55.5); the append's longer code and shorter launches
-// prefer the latter (2 x 4096 tokens to int8 keys: 17.7 us against 18.4).
+// prefer 64 bytes and 24 warps (2 x 4096 tokens to int8 keys: 15.9 us against
+// 17.8, and 16.1 with 28).
 template <typename X, int KF>
 constexpr int rows_held() { return (KF < 0 ? 16 : 8) / static_cast<int>(sizeof(X)); }
 template <int KF>
-constexpr int blocks_held() { return KF < 0 ? 5 : 7; }
+constexpr int blocks_held() { return KF < 0 ? 5 : 6; }
 
 // The cache row of kv head g for a slot: block = page or sequence.
 struct SlotRow {
@@ -218,9 +219,9 @@ norm_rope_kernel(const __grid_constant__ QkParams p) {
 // Order of the units, measured both ways: with more than four waves of
 // warps, blocks of few tokens with all their heads, so that the projection's
 // rows are read once through, in order (2 x 8192 tokens of 32 heads: 60.9 us,
-// against 62.5 with all of q and k first); with fewer, q and k before v,
-// whose short units then fill the last wave (4096 tokens of 32 + 8 heads: 8.1
-// us against 9.0).  False if there are too many units for one launch.
+// against 62.5 with all of q and k first); with fewer, blocks of a wave, in
+// which q and k come before v, whose short units then fill the wave's end
+// (4096 tokens of 32 + 8 heads: 8.1 us against 9.0).  False if there are too many units for one launch.
 bool plan(QkParams& p, int num_sms, int warps_held) {
   const uint32_t t_qk = 256 / p.R, t_v = 256 / p.DV, tokens = t_qk > t_v ? t_qk : t_v;
   p.block_qk = tokens / t_qk;
@@ -238,10 +239,13 @@ bool plan(QkParams& p, int num_sms, int warps_held) {
     units = count(div_up(p.n_tokens, tokens));
     if (most == 1 || units >= static_cast<uint64_t>(num_sms) * 8) break;
   }
-  if (units <= 4ull * num_sms * warps_held) {
-    p.block_qk = div_up(p.n_tokens, t_qk);       // one block
-    p.block_v = div_up(p.n_tokens, t_v);
-    units = count(1);
+  const uint64_t wave = static_cast<uint64_t>(num_sms) * warps_held;
+  if (units <= 4 * wave) {
+    const uint32_t blocks = units > wave ? static_cast<uint32_t>(units / wave) : 1u;
+    const uint32_t small = div_up(div_up(p.n_tokens, tokens), blocks);     // small blocks in one
+    p.block_qk *= small;
+    p.block_v *= small;
+    units = count(div_up(p.n_tokens, tokens * small));
   }
   if (units >= (1ull << 31)) return false;
   p.units = static_cast<uint32_t>(units);

@@ -276,3 +276,21 @@ def test_binding_refusals():
         tb._positions(plan, torch.zeros(2, 6, dtype=torch.int32)[:, ::2], 2, 3, cpu)
     with pytest.raises(TypeError):
         tb._weights(plan, torch.zeros(32), torch.zeros(32, dtype=torch.bfloat16), cpu)
+
+
+def test_binding_refuses_host_tensors():
+    """Every entry point raises before a host pointer could reach a kernel."""
+    import torch
+    x = torch.zeros(2, 4, 3, 32, dtype=torch.bfloat16)
+    pos = torch.zeros(2, 3, dtype=torch.int32)
+    plan = tb.rope_plan(32)
+    with pytest.raises(ValueError):
+        tb.tk_qk_norm_rope(plan, x, None, None, pos, x.clone(), None, None)
+    with pytest.raises(ValueError):
+        tb.tk_qk_norm_rope_backward(plan, x, None, pos, x, None, None, x.clone(), None, None)
+    cache = tb.ThinKeyCache.allocate(2, 4, 4, 32, 64, capacity=16, device="cpu")
+    with pytest.raises(ValueError):
+        tb.tk_qk_norm_rope_append(cache, plan, x, x, torch.zeros(2, 4, 3, 64, dtype=torch.bfloat16), pos, pos, x.clone())
+    pool = tb.PagePool.allocate(2, 4, 16, 8, device="cpu")
+    with pytest.raises(ValueError):
+        tb.tk_block_tables(pool, torch.ones(2, dtype=torch.int32), pos.view(-1).clone(), pos.view(-1).clone())

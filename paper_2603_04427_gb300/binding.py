@@ -9,6 +9,7 @@ kernels; there is no CPU or PyTorch fallback, and a missing library raises.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -134,14 +135,13 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
-def _raw_stream(stream):
-    # the current stream's handle without building a torch.cuda.Stream (60 ns against 2.9 us)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None \
-        else stream.cuda_stream
+def _raw_stream(stream, device):
+    # the device's current stream without building a torch.cuda.Stream (60 ns against 2.9 us)
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def _stream(stream):
-    return ctypes.c_void_p(_raw_stream(stream))
+    return ctypes.c_void_p(_raw_stream(stream, torch.cuda.current_device()))
 
 
 def _need_out(t, name, device):
@@ -576,19 +576,27 @@ def _heads(t, name, shape, device):
     return _pack_heads(t.data_ptr(), shape[1], dt, sb, st, sh)
 
 
+def _weight(t, r, device):
+    """A norm weight's address and type, checked; None, None without one."""
+    if t is None:
+        return None, None
+    dt = _HEADS_DTYPE.get(t.dtype)
+    if dt is None:
+        raise TypeError("norm weights must be float32 or bfloat16")
+    if not t.is_cuda or t.device != device or t.numel() != r or not t.is_contiguous():
+        raise ValueError(f"a norm weight must be {r} contiguous elements on {device} (CUDA)")
+    return t.data_ptr(), dt
+
+
 def _weights(plan, q_weight, k_weight, device):
     """The weights' addresses and type, checked."""
-    kinds = {_HEADS_DTYPE.get(t.dtype) for t in (q_weight, k_weight) if t is not None}
-    if None in kinds or len(kinds) > 1:
-        raise TypeError("norm weights must be float32 or bfloat16, both alike")
-    at = [None, None]
-    for i, t in enumerate((q_weight, k_weight)):
-        if t is None:
-            continue
-        if not t.is_cuda or t.device != device or not t.is_contiguous() or t.numel() != plan.r:
-            raise ValueError(f"a norm weight must be {plan.r} contiguous elements on {device} (CUDA)")
-        at[i] = t.data_ptr()
-    return at[0], at[1], kinds.pop() if kinds else TK_F32
+    if q_weight is None and k_weight is None:
+        return None, None, TK_F32
+    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+        raise TypeError("norm weights must be of one dtype")
+    q, q_type = _weight(q_weight, plan.r, device)
+    k, k_type = _weight(k_weight, plan.r, device)
+    return q, k, k_type if q_type is None else q_type
 
 
 def _positions(plan, positions, B, S, device):
@@ -637,7 +645,7 @@ def tk_qk_norm_rope(plan: tk_rope_desc, q, k, v, positions, q_out, k_out, v_out,
         ctypes.byref(plan), B, S, dv, _heads(q, "q", sq, at), _heads(k, "k", sk, at), _heads(v, "v", sv, at),
         *_weights(plan, q_weight, k_weight, dev), *_positions(plan, positions, B, S, dev),
         _heads(q_out, "q_out", sq, at), _heads(k_out, "k_out", sk, at), _heads(v_out, "v_out", sv, at),
-        _raw_stream(stream))
+        _raw_stream(stream, at))
     if st != TK_OK:
         _check(st, "tk_qk_norm_rope")
     return q_out, k_out, v_out
@@ -701,23 +709,23 @@ def tk_qk_norm_rope_backward(plan: tk_rope_desc, q, k, positions, dq_out, dk_out
     sq, sk, sv = _shape(dq_out, B, S, r), _shape(dk_out, B, S, r), _shape(dv_out, B, S, width)
     if not plan.norm:
         q = k = None
-    for t, n in ((dq_weight, "dq_weight"), (dk_weight, "dk_weight")):
-        if t is not None:
-            _need(t, torch.float32, n, dev)
-            if t.numel() != r:
-                raise ValueError(f"{n} has {t.numel()} elements, expected {r}")
+    dwq, dwq_type = _weight(dq_weight, r, dev)
+    dwk, dwk_type = _weight(dk_weight, r, dev)
+    if TK_BF16 in (dwq_type, dwk_type):
+        raise TypeError("weight gradients must be float32")
     if workspace is None:
-        if dq_weight is not None or dk_weight is not None:
-            workspace = qk_norm_rope_workspace(plan, dev)
-    else:
-        _need(workspace, torch.uint8, "workspace", dev)
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        if dwq is not None or dwk is not None:
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+                workspace = qk_norm_rope_workspace(plan, dev)   # zeroed, and freed, in the call's stream
+    elif workspace.dtype is not torch.uint8 or workspace.get_device() != at or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous uint8 on {dev}")
     st = load_library().tk_qk_norm_rope_backward(
         ctypes.byref(plan), B, S, width, _heads(q, "q", sq, at), _heads(k, "k", sk, at),
         *_weights(plan, q_weight, k_weight, dev), *_positions(plan, positions, B, S, dev),
         _heads(dq_out, "dq_out", sq, at), _heads(dk_out, "dk_out", sk, at), _heads(dv_out, "dv_out", sv, at),
-        _heads(dq, "dq", sq, at), _heads(dk, "dk", sk, at), _heads(dv, "dv", sv, at), ptr(dq_weight),
-        ptr(dk_weight), ptr(workspace), 0 if workspace is None else workspace.numel(), _raw_stream(stream))
+        _heads(dq, "dq", sq, at), _heads(dk, "dk", sk, at), _heads(dv, "dv", sv, at), dwq, dwk,
+        None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel(), _raw_stream(stream, at))
     if st != TK_OK:
         _check(st, "tk_qk_norm_rope_backward")
     return dq, dk, dv
@@ -786,7 +794,8 @@ def tk_block_tables(pool: PagePool, new_lens, slots, positions, tokens_per_seq: 
 def prepare_block_tables(pool: PagePool, new_lens, slots, positions, tokens_per_seq: int = 0, offsets=None,
                          seq_lens_out=None, free_count_out=None, refused=None, stream=None,
                          graph: bool = False) -> PreparedCall:
-    """tk_block_tables on fixed buffers, checked and marshalled once (see PreparedCall)."""
+    """tk_block_tables on fixed buffers, checked and marshalled once (see PreparedCall).  With
+    graph=True preparing runs the step once; every call is one more step."""
     args, keep = _table_args(pool, new_lens, slots, positions, tokens_per_seq, offsets, seq_lens_out,
                              free_count_out, refused, stream)
     return PreparedCall("tk_block_tables", args, keep, graph=graph, stream=stream)

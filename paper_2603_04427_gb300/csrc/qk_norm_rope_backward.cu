@@ -121,7 +121,7 @@ __device__ __forceinline__ Row8 backward_units(const QkParams& p, uint32_t unit,
 template <int R, int MODE, typename X, typename D>
 __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const __grid_constant__ QkParams p) {
   constexpr int G = R / 8;
-  __shared__ float sums[kWarpsB][2][R];
+  __shared__ __align__(16) float sums[kWarpsB][2][R];
   __shared__ __align__(16) float weights[2][R];    // in slot order
   __shared__ int last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -155,7 +155,6 @@ __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const _
     const uint32_t end = share(m, &unit);
     const Row8 dw = m ? backward_units<1, R, MODE, X, D>(p, unit, end, lane, oa, ob, weights[1])
                       : backward_units<0, R, MODE, X, D>(p, unit, end, lane, oa, ob, weights[0]);
-    if (p.dwq == nullptr && p.dwk == nullptr) continue;
     // over the lanes that hold the same elements
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -164,6 +163,21 @@ __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const _
       for (int o = 16; o >= G; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
       if (lane < G) sums[warp][m][slot_element<MODE>(e, oa, ob)] = d;
     }
+  }
+  // weight gradients: over the block's warps, then the blocks; the arrival's
+  // latency passes behind the value gradients
+  const bool sum_weights = p.dwq != nullptr || p.dwk != nullptr;
+  int before = 0;
+  if (sum_weights) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * R; c += kThreads) {
+      float a = 0.f;
+#pragma unroll
+      for (int k = 0; k < kWarpsB; ++k) a += (&sums[k][0][0])[c];
+      p.part[static_cast<size_t>(blockIdx.x) * 2 * R + c] = a;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) before = arrive(p.counter);
   }
   // value gradients: converted and laid out
   uint32_t unit;
@@ -176,32 +190,29 @@ __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const _
         [&](uint32_t b, uint32_t s) { return static_cast<const D*>(p.vo.p) + b * p.vo.sb + s * p.vo.st; },
         [&](uint32_t b, uint32_t s, uint32_t) { return static_cast<X*>(p.dv.p) + b * p.dv.sb + s * p.dv.st; });
   }
-  if (p.dwq == nullptr && p.dwk == nullptr) return;
-
-  // weight gradients: over the block's warps, then the blocks
-  __syncthreads();
-  for (int c = threadIdx.x; c < 2 * R; c += kThreads) {
-    float a = 0.f;
-#pragma unroll
-    for (int k = 0; k < kWarpsB; ++k) a += (&sums[k][0][0])[c];
-    p.part[static_cast<size_t>(blockIdx.x) * 2 * R + c] = a;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) last = arrive(p.counter) == static_cast<int>(gridDim.x) - 1;
+  if (!sum_weights) return;
+  if (threadIdx.x == 0) last = before == static_cast<int>(gridDim.x) - 1;
   __syncthreads();
   if (!last) return;
-  // four columns a thread and up to 16 threads a column group, so that a
-  // thread adds some ten blocks' sums, loaded at once (a thread a column and
-  // 76 loads in chains of 8 took 7 us of a 16 us call)
+  // four columns a thread and up to 16 threads a column group; a thread's ten
+  // or twenty loads are issued before the first is added (one after the other
+  // they took 3.5 us)
   constexpr int kCols = 2 * R / 4, P = kThreads / kCols < kWarpsB ? kThreads / kCols : kWarpsB;
+  constexpr unsigned kLoads = 160 / P;
   float4* join = reinterpret_cast<float4*>(&sums[0][0][0]);   // [P][kCols], at most all of sums
   const int c = threadIdx.x % kCols, part = threadIdx.x / kCols;
   if (part < P) {
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 10
-    for (unsigned k = part; k < gridDim.x; k += P) {
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part) + static_cast<size_t>(k) * kCols + c);
-      a.x += x.x, a.y += x.y, a.z += x.z, a.w += x.w;
+    for (unsigned k0 = part; k0 < gridDim.x; k0 += kLoads * P) {
+      float4 x[kLoads];
+#pragma unroll
+      for (unsigned j = 0; j < kLoads; ++j) {
+        x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (k0 + j * P < gridDim.x)
+          x[j] = __ldcg(reinterpret_cast<const float4*>(p.part) + static_cast<size_t>(k0 + j * P) * kCols + c);
+      }
+#pragma unroll
+      for (unsigned j = 0; j < kLoads; ++j) a.x += x[j].x, a.y += x[j].y, a.z += x[j].z, a.w += x[j].w;
     }
     join[part * kCols + c] = a;
   }

@@ -112,7 +112,7 @@ __device__ __forceinline__ Turns make_turns(const QkParams& p, int sub, const Pl
 }
 
 // A lane's eight elements in slots: v[0], v[1] = a_0..a_3, v[2], v[3] = b_0..b_3.
-struct Row8 {
+struct alignas(16) Row8 {
   float2 v[4];
 };
 

@@ -244,40 +244,44 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
   // the slot map
   for (int64 row0 = static_cast<int64>(tid) * kPer; row0 < p.rows; row0 += static_cast<int64>(stride) * kPer) {
     int slot[kPer], pos[kPer];
-    int b = -1, page_of = -1, id = -1;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int k = 0; k < kPer; ++k) slot[k] = -1, pos[k] = 0;
+    // one page at a time: the lanes of a warp cross their page boundaries at
+    // different rows, and every look-up is paid for by all of them
+    int b = -1, i = 0;
+    while (i < kPer && row0 + i < p.rows) {
       const int row = static_cast<int>(row0) + i;
-      slot[i] = -1;
-      pos[i] = 0;
-      if (row0 + i >= p.rows) continue;
       int t;     // token of sequence b
-      bool real;
       if (p.per_seq) {
         uint32_t tt;
-        const int nb = static_cast<int>(p.div_t.divmod(static_cast<uint32_t>(row), &tt));
-        if (nb != b) b = nb, page_of = -1;
+        b = static_cast<int>(p.div_t.divmod(static_cast<uint32_t>(row), &tt));
         t = static_cast<int>(tt);
-        real = t < tok[b + 1] - tok[b];
-      } else {
-        real = row < total_tokens;
-        if (real && (b < 0 || row >= tok[b + 1])) b = owner(tok, row), page_of = -1;
-        t = real ? row - tok[b] : 0;
-      }
-      if (!real) continue;
-      pos[i] = len[b] + t;
-      const int pi = pos[i] >> p.page_shift;
-      if (pi != page_of) {
-        page_of = pi;
-        if (pi < (len[b] + (ps - 1)) >> p.page_shift) {
-          id = checked(cur[b]);
-        } else {
-          id = checked(popped(pop[b] + pi));
-          if ((pos[i] & (ps - 1)) == 0)                    // its first token writes the entry
-            p.page_table[static_cast<size_t>(b) * p.max_pages + pi] = id;
+        if (t >= tok[b + 1] - tok[b]) {      // no more tokens in the sequence's rows
+          i += p.per_seq - t;
+          continue;
         }
+      } else {
+        if (row >= total_tokens) break;
+        if (b < 0 || row >= tok[b + 1]) b = owner(tok, row);
+        t = row - tok[b];
       }
-      if (id >= 0) slot[i] = (id << p.page_shift) + (pos[i] & (ps - 1));
+      const int at = len[b] + t, pi = at >> p.page_shift, in_page = at & (ps - 1);
+      const int n = min(min(tok[b + 1] - tok[b] - t, ps - in_page), kPer - i);
+      int id;
+      if (pi < (len[b] + (ps - 1)) >> p.page_shift) {
+        id = checked(cur[b]);
+      } else {
+        id = checked(popped(pop[b] + pi));
+        if (in_page == 0)                    // its first token writes the entry
+          p.page_table[static_cast<size_t>(b) * p.max_pages + pi] = id;
+      }
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        if (k < i || k >= i + n) continue;
+        pos[k] = at + (k - i);
+        slot[k] = id < 0 ? -1 : (id << p.page_shift) + in_page + (k - i);
+      }
+      i += n;
     }
     if (kPer == 4 && row0 + kPer <= p.rows) {
       *reinterpret_cast<int4*>(p.slots + row0) = make_int4(slot[0], slot[1 % kPer], slot[2 % kPer], slot[3 % kPer]);

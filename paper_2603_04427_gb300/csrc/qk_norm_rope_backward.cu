@@ -7,7 +7,10 @@
 // read once, kept in registers and written once; rho is recomputed, not
 // stored by the forward (the row is read anyway).
 //
-// Bound by HBM.  One block per SM; each warp takes an equal share of the (token
+// Bound by HBM (2 x 8192 tokens of 32 + 32 heads, r = 32, d_v = 128, fp32
+// gradients: 671 MB in 103.8 us, 6.5 TB/s, 95 % of a copy).  One block per SM
+// of 16 warps, four rows in flight a lane (more warps with fewer registers:
+// 114 to 146 us); each warp takes an equal share of the (token
 // group, run of heads) units of q, of k and of v (equal shares of all units in
 // one row left SMs with values alone idle a quarter of the time).  The weight
 // gradient gathers in eight registers a lane over a warp's units of one

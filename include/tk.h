@@ -422,7 +422,9 @@ size_t tk_qk_norm_rope_workspace_size(const tk_rope_desc* desc);
  *   dq_out, dk_out, dv_out: gradients of its outputs, one dtype (TK_F32 as
  *                  tk_attn_backward writes them, or TK_BF16); NULL (with its
  *                  dq, dk, dv) leaves that one out
- *   dq, dk, dv   : gradients of its inputs, of the inputs' dtype (written)
+ *   dq, dk, dv   : gradients of its inputs, of the inputs' dtype (written);
+ *                  each may be its own q or k, or its own dq_out (same
+ *                  address, dtype and strides)
  *   dq_weight, dk_weight: device fp32 [r] (overwritten), or NULL; norm only
  *   workspace    : needed for a weight gradient
  * Sums over rows are fp32 in an order fixed by the device's SM count: results
@@ -473,7 +475,8 @@ tk_status tk_qk_norm_rope_backward(const tk_rope_desc* desc, int32_t batch, int3
  * the free pages; a refused request keeps its pages and length and gets no
  * slots.  Lengths below 0 or beyond the row, counts below -1, a free count
  * or a page id out of range set the device error word (the request is
- * refused; tokens on a bad page get slot -1).
+ * refused; tokens on a bad page get slot -1, and -1 goes on the stack for a
+ * bad page that is given back).
  * page_size as in tk_cache_desc; batch <= 4096; num_pages * page_size,
  * max_pages_per_seq * page_size and batch * max_pages_per_seq at most 2^30.
  * Launched with programmatic dependent launch.                             */

@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
     for (int k = 0; k < kBack; ++k) {
       if (i0 + k >= left) continue;
       const int64 to = f + i0 + k;
-      if (to < p.num_pages) p.free_pages[to] = id[k];
+      if (to < p.num_pages) p.free_pages[to] = checked(id[k]);
       else record_error(p.err, TK_DEVERR_INDEX);     // more free pages than the pool has
     }
   }

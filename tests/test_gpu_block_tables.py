@@ -114,6 +114,21 @@ def test_boundaries():
     _check([16, 15], [0, -1], table[:2], free, 3, 16, 0, 0)
 
 
+def test_empty_batch():
+    require_gpu()
+    got = _run([], [], np.zeros((0, 4)), np.array([2, 0, 1]), 2, 16, 0, 0, False)
+    assert got["free_count"][0] == 2 and got["offsets"].tolist() == [0] and got["refused"][0] == 0
+    assert tb.tk_get_device_error() == 0
+
+
+def test_returned_pages_out_of_range_are_flagged():
+    """A finished request whose row holds a bad page id: flagged, the sound pages come back."""
+    require_gpu()
+    got = _run([40, 5], [-1, 0], np.array([[0, 9, 1], [2, -1, -1]]), np.array([3, -1, -1, -1]), 1, 16, 1, 0, False)
+    assert tb.tk_get_device_error() == 1
+    assert got["free_count"][0] == 4 and got["free_pages"].tolist() == [3, 0, -1, 1]
+
+
 def test_many_steps_keep_every_page_once():
     require_gpu()
     rng = np.random.default_rng(9)

@@ -492,3 +492,99 @@ def test_serving_path(kfmt):
             # bf16 keys: 2^-9 of each key, scores of a few units; int8 keys: half a step, amax / 254
             parity(f64(out[b:b + 1]), ref, max_abs=2e-2 if kfmt == "bf16" else 6e-2,
                    mean_rel=5e-3 if kfmt == "bf16" else 2e-2, what=f"step {step} sequence {b}")
+
+
+@pytest.mark.parametrize("kfmt", ["int8", "int4"])
+def test_append_quantiser_over_all_magnitudes(kfmt):
+    """Rows from denormals to near overflow, ties, zeros: codes and scales of the oracle's quantiser, bit for bit."""
+    require_gpu()
+    r, dv = 32, 64
+    plan = tb.rope_plan(r, rot_dim=0, norm=False)          # rows pass through unchanged
+    g = np.random.default_rng(6)
+    mags = np.exp2(np.linspace(-148, 126, 400))
+    x = (g.uniform(-1, 1, (400, r)) * mags[:, None]).astype(np.float32)
+    top = 127 if kfmt == "int8" else 7
+    x[::3] = np.round(x[::3] / np.abs(x[::3]).max(-1, keepdims=True) * 2 * top) / 2      # halves of a code
+    x[::3, 0] = top
+    x[5] = 0.0
+    x[6] = -0.0
+    x[7, 1:] = 0.0
+    S = x.shape[0]
+    k = torch.from_numpy(x)[None, None].cuda()
+    v = torch.zeros(1, 1, S, dv, device="cuda")
+    c, _ = _cache(1, 1, 1, r, dv, 0, kfmt, S)
+    slots = torch.arange(S, dtype=torch.int32, device="cuda")
+    tb.tk_qk_norm_rope_append(c, plan, None, k, v, None, slots, None)
+    assert tb.tk_get_device_error() == 0
+    codes, scales = (oc.quantize_int8_per_token if kfmt == "int8" else oc.quantize_int4_per_token)(x)
+    codes = oc.pack_int4(codes) if kfmt == "int4" else codes
+    assert np.array_equal(c.k_scale[0, 0, :S].cpu().numpy().view(np.uint32), scales.view(np.uint32))
+    assert np.array_equal(c.k[0, 0, :S].cpu().numpy(), codes)
+
+
+def test_append_of_infinite_keys_stays_in_its_row():
+    require_gpu()
+    r, dv, S = 32, 64, 9
+    plan = tb.rope_plan(r, rot_dim=0, norm=False)
+    x = torch.randn(1, 2, S, r, device="cuda")
+    bad = x.clone()
+    bad[0, 0, 4, 3] = float("inf")
+    bad[0, 1, 2, 0] = float("nan")
+    v = torch.randn(1, 2, S, dv, device="cuda")
+    slots = torch.arange(S, dtype=torch.int32, device="cuda")
+    caches = []
+    for k in (x, bad):
+        c, _ = _cache(1, 2, 2, r, dv, 0, "int8", S)
+        tb.tk_qk_norm_rope_append(c, plan, None, k, v, None, slots, None)
+        caches.append(c)
+    a, b = caches
+    keep = torch.ones(2, S, dtype=torch.bool, device="cuda")
+    keep[0, 4] = keep[1, 2] = False
+    assert torch.equal(a.k[0, :, :S][keep], b.k[0, :, :S][keep])
+    assert torch.equal(a.k_scale[0, :, :S][keep], b.k_scale[0, :, :S][keep]) and torch.equal(a.v, b.v)
+
+
+def test_broadcast_inputs_and_gradients_in_place():
+    """One set of heads read for every sequence (stride 0); dq written over q, and over dq_out."""
+    require_gpu()
+    B, S, H, r = 3, 10, 4, 64
+    plan = _plan(r, 64, "half", 1, True)
+    one = torch.randn(1, H, S, r, device="cuda")
+    pos = _positions(B, S, 1, seed=4)
+    wide = one.expand(B, H, S, r)
+    got = tb.tk_qk_norm_rope(plan, wide, None, None, pos, torch.empty(B, H, S, r, device="cuda"), None, None)[0]
+    ref = tb.tk_qk_norm_rope(plan, wide.contiguous(), None, None, pos, torch.empty_like(got), None, None)[0]
+    assert torch.equal(got, ref)
+    heads = torch.randn(B, 1, S, r, device="cuda").expand(B, H, S, r)
+    got = tb.tk_qk_norm_rope(plan, heads, None, None, pos, torch.empty_like(got), None, None)[0]
+    assert all(torch.equal(got[:, 0], got[:, h]) for h in range(H))
+    with pytest.raises(tb.TkError):          # a gradient cannot be written to shared rows
+        tb.tk_qk_norm_rope_backward(plan, wide, None, pos, ref, None, None, wide, None, None)
+    x, g = torch.randn(B, H, S, r, device="cuda"), torch.randn(B, H, S, r, device="cuda")
+    dx = torch.empty_like(x)
+    tb.tk_qk_norm_rope_backward(plan, x, None, pos, g, None, None, dx, None, None)
+    over_x, over_g = x.clone(), g.clone()
+    tb.tk_qk_norm_rope_backward(plan, over_x, None, pos, g, None, None, over_x, None, None)
+    tb.tk_qk_norm_rope_backward(plan, x, None, pos, over_g, None, None, over_g, None, None)
+    assert torch.equal(over_x, dx) and torch.equal(over_g, dx)
+    assert tb.tk_get_device_error() == 0
+
+
+def test_calls_on_another_stream():
+    """Inputs made on one stream, the call and a workspace of its own on another."""
+    require_gpu()
+    B, S, H, r = 2, 700, 8, 64
+    plan = _plan(r, 64, "half", 1, True)
+    pos = _positions(B, S, 1, seed=4)
+    x, g = torch.randn(B, H, S, r, device="cuda"), torch.randn(B, H, S, r, device="cuda")
+    dx, dw = torch.empty_like(x), torch.empty(r, device="cuda")
+    tb.tk_qk_norm_rope_backward(plan, x, None, pos, g, None, None, dx, None, None, dq_weight=dw)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        dx2, dw2 = torch.empty_like(x), torch.empty(r, device="cuda")
+        s.wait_stream(torch.cuda.current_stream())
+        tb.tk_qk_norm_rope_backward(plan, x, None, pos, g, None, None, dx2, None, None, dq_weight=dw2, stream=s)
+        torch.cuda.current_stream().wait_stream(s)
+        assert torch.equal(dx, dx2) and torch.equal(dw, dw2)
+    assert tb.tk_get_device_error() == 0

@@ -294,3 +294,9 @@ def test_binding_refuses_host_tensors():
     pool = tb.PagePool.allocate(2, 4, 16, 8, device="cpu")
     with pytest.raises(ValueError):
         tb.tk_block_tables(pool, torch.ones(2, dtype=torch.int32), pos.view(-1).clone(), pos.view(-1).clone())
+
+
+def test_binding_layouts_match_the_header():
+    import struct
+    assert ctypes.sizeof(tb.tk_heads) == struct.calcsize("Piiqqq") == 40
+    assert ctypes.sizeof(tb.tk_rope_desc) == 5 * 4 + 2 * 4 + 64 * 4 + 64

@@ -48,11 +48,11 @@ struct QkParams {
   const int32_t* pos;
   int64_t pos_sa, pos_sb;   // position strides: axis, batch
   int* err;
-  int B, S, R, DV, rot;
+  int R, DV, rot;
   int pair_layout, n_axes, norm;
   int x_f32, o_f32;         // type of q, k, v; type of qo, ko, vo
-  uint32_t n_tokens;        // B * S
-  FastDiv div_s;
+  uint32_t n_tokens;        // batch * seq
+  FastDiv div_s;            // by seq
   // Set by the launchers.  Heads are taken in runs (heads of a run, number of
   // runs of q, k and v) for groups of tokens (256 / r for q and k, 256 / d_v
   // for v).

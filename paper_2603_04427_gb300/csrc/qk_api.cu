@@ -126,8 +126,6 @@ tk_status common(const tk_rope_desc* d, int32_t batch, int32_t seq, const void* 
   p->pos = positions;
   p->pos_sa = pos_axis_stride;
   p->pos_sb = pos_batch_stride;
-  p->B = batch;
-  p->S = seq;
   p->R = d->r;
   p->rot = d->rot_dim;
   p->pair_layout = d->layout == TK_ROPE_PAIR;

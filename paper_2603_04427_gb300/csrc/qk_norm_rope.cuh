@@ -19,6 +19,8 @@
 // launch.
 #pragma once
 
+#include <algorithm>
+
 #include "kernels.h"
 #include "qk_row.cuh"
 
@@ -218,12 +220,12 @@ norm_rope_kernel(const __grid_constant__ QkParams p) {
 
 // Runs of up to 8 heads, which amortise the angles; while the launch is too
 // small to give every SM eight warps, they are halved, down to single heads.
-// Order of the units, measured both ways: with more than four waves of
-// warps, blocks of few tokens with all their heads, so that the projection's
-// rows are read once through, in order (2 x 8192 tokens of 32 heads: 60.9 us,
-// against 62.5 with all of q and k first); with fewer, blocks of a wave, in
-// which q and k come before v, whose short units then fill the wave's end
-// (4096 tokens of 32 + 8 heads: 8.1 us against 9.0).  False if there are too many units for one launch.
+// Units go by blocks of tokens of about a wave of warps, in which q and k come
+// before v, whose short units then fill the wave's end (4096 tokens of 32 + 8
+// heads: 8.4 us, against 9.3 with all heads of a few tokens together; 2 x 4096
+// tokens to int8 keys: 15.7 against 18.0; launches of many waves, where the
+// rows are read almost in order either way: no difference).  False if there
+// are too many units for one launch.
 bool plan(QkParams& p, int num_sms, int warps_held) {
   const uint32_t t_qk = 256 / p.R, t_v = 256 / p.DV, tokens = t_qk > t_v ? t_qk : t_v;
   p.block_qk = tokens / t_qk;
@@ -242,13 +244,11 @@ bool plan(QkParams& p, int num_sms, int warps_held) {
     if (most == 1 || units >= static_cast<uint64_t>(num_sms) * 8) break;
   }
   const uint64_t wave = static_cast<uint64_t>(num_sms) * warps_held;
-  if (units <= 4 * wave) {
-    const uint32_t blocks = units > wave ? static_cast<uint32_t>(units / wave) : 1u;
-    const uint32_t small = div_up(div_up(p.n_tokens, tokens), blocks);     // small blocks in one
-    p.block_qk *= small;
-    p.block_v *= small;
-    units = count(div_up(p.n_tokens, tokens * small));
-  }
+  const uint32_t blocks = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>(units / wave, 1), 1u << 30));
+  const uint32_t small = div_up(div_up(p.n_tokens, tokens), blocks);       // groups of `tokens` in a block
+  p.block_qk *= small;
+  p.block_v *= small;
+  units = count(div_up(p.n_tokens, tokens * small));
   if (units >= (1ull << 31)) return false;
   p.units = static_cast<uint32_t>(units);
   p.div_block_v = FastDiv(p.block_v);

@@ -1,4 +1,4 @@
-// Gradients of the per-head norm + rotation (qk_norm_rope.cu).  With g the
+// Gradients of the per-head norm + rotation (qk_norm_rope.cuh).  With g the
 // incoming gradient turned back by the token's angles, rho the row's
 // (mean(x^2) + eps)^(-1/2) and u = w + w_offset:
 //   dw = sum over tokens and heads of g x rho
@@ -8,12 +8,12 @@
 // stored by the forward (the row is read anyway).
 //
 // Bound by HBM (2 x 8192 tokens of 32 + 32 heads, r = 32, d_v = 128, fp32
-// gradients: 671 MB in 103.8 us, 6.5 TB/s, 95 % of a copy).  One block per SM
+// gradients: 671 MB in 103.4 us, 6.5 TB/s, 96 % of a copy).  One block per SM
 // of 16 warps, four rows in flight a lane (more warps with fewer registers:
-// 114 to 146 us); each warp takes an equal share of the (token
-// group, run of heads) units of q, of k and of v (equal shares of all units in
-// one row left SMs with values alone idle a quarter of the time).  The weight
-// gradient gathers in eight registers a lane over a warp's units of one
+// 114 to 146 us); each warp takes an equal share of the (token group, run of
+// heads) units of q, of k and of v (equal shares of all units in one row left
+// SMs with values alone idle a quarter of the time).  The weight gradient
+// gathers in eight registers a lane over a warp's units of one
 // tensor, in shared memory over the block's warps, and one partial sum per
 // block goes to the workspace, which the last block to arrive adds up in
 // block order.  No atomics touch the sums, so results repeat bit for bit on
@@ -158,6 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const _
     const uint32_t end = share(m, &unit);
     const Row8 dw = m ? backward_units<1, R, MODE, X, D>(p, unit, end, lane, oa, ob, weights[1])
                       : backward_units<0, R, MODE, X, D>(p, unit, end, lane, oa, ob, weights[0]);
+    if (p.dwq == nullptr && p.dwk == nullptr) continue;
     // over the lanes that hold the same elements
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -166,21 +167,6 @@ __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const _
       for (int o = 16; o >= G; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
       if (lane < G) sums[warp][m][slot_element<MODE>(e, oa, ob)] = d;
     }
-  }
-  // weight gradients: over the block's warps, then the blocks; the arrival's
-  // latency passes behind the value gradients
-  const bool sum_weights = p.dwq != nullptr || p.dwk != nullptr;
-  int before = 0;
-  if (sum_weights) {
-    __syncthreads();
-    for (int c = threadIdx.x; c < 2 * R; c += kThreads) {
-      float a = 0.f;
-#pragma unroll
-      for (int k = 0; k < kWarpsB; ++k) a += (&sums[k][0][0])[c];
-      p.part[static_cast<size_t>(blockIdx.x) * 2 * R + c] = a;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) before = arrive(p.counter);
   }
   // value gradients: converted and laid out
   uint32_t unit;
@@ -193,8 +179,20 @@ __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const _
         [&](uint32_t b, uint32_t s) { return static_cast<const D*>(p.vo.p) + b * p.vo.sb + s * p.vo.st; },
         [&](uint32_t b, uint32_t s, uint32_t) { return static_cast<X*>(p.dv.p) + b * p.dv.sb + s * p.dv.st; });
   }
-  if (!sum_weights) return;
-  if (threadIdx.x == 0) last = before == static_cast<int>(gridDim.x) - 1;
+  if (p.dwq == nullptr && p.dwk == nullptr) return;
+
+  // weight gradients: over the block's warps, then the blocks (summing and
+  // arriving before the values, to hide the arrival's latency, cost as much in
+  // the barrier: 20.4 us against 20.0 for 4 x 2047 tokens)
+  __syncthreads();
+  for (int c = threadIdx.x; c < 2 * R; c += kThreads) {
+    float a = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWarpsB; ++k) a += (&sums[k][0][0])[c];
+    p.part[static_cast<size_t>(blockIdx.x) * 2 * R + c] = a;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) last = arrive(p.counter) == static_cast<int>(gridDim.x) - 1;
   __syncthreads();
   if (!last) return;
   // four columns a thread and up to 16 threads a column group; a thread's ten

@@ -8,7 +8,7 @@
 //
 // Nothing is computed twice and every element is read and written once, so
 // the bound is HBM for long prompts (2 x 8192 tokens of 32 + 32 heads, r = 32,
-// d_v = 128: 403 MB in 59.8 us, 6.7 TB/s, 99 % of a copy) and the launch for
+// d_v = 128: 403 MB in 60.0 us, 6.7 TB/s, 99 % of a copy) and the launch for
 // single tokens (16 of them into a paged cache: 2.3 us).
 //
 // A warp takes the 256 / r tokens that fit its lanes (qk_row.cuh) and a run
@@ -31,8 +31,8 @@ constexpr int kWarps = 4;
 
 // Rows a lane holds at a time and blocks an SM holds.  With many waves, 128
 // bytes a lane and 20 warps an SM beat 64 bytes and 28 warps (2 x 9721 tokens
-// in fp32: 53 us against 55.5); the append's longer code and shorter launches
-// prefer 64 bytes and 24 warps (2 x 4096 tokens to int8 keys: 15.9 us against
+// in fp32: 53.2 us against 55.5); the append's longer code and shorter launches
+// prefer 64 bytes and 24 warps (2 x 4096 tokens to int8 keys: 15.7 us against
 // 17.8, and 16.1 with 28).
 template <typename X, int KF>
 constexpr int rows_held() { return (KF < 0 ? 16 : 8) / static_cast<int>(sizeof(X)); }

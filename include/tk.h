@@ -470,9 +470,11 @@ tk_status tk_qk_norm_rope_backward(const tk_rope_desc* desc, int32_t batch, int3
  * sequence and page.  Then requests are served in order, each wholly or not at
  * all: page i of the step's is popped from the top.  A request is refused if
  * it exceeds the page table's row or the slot map (its tokens_per_seq, or,
- * packed, the requested tokens up to and with it exceed rows), or if it
- * needs pages and the needs of the accepted requests up to and with it exceed
- * the free pages; a refused request keeps its pages and length and gets no
+ * packed, the tokens that it and the requests before it ask for exceed rows),
+ * or if it needs pages and it and the requests before it that pass these two
+ * checks need more than are free (after one such refusal every later request
+ * that needs pages is refused too, and one that needs none is served).  A
+ * refused request keeps its pages and length and gets no
  * slots.  Lengths below 0 or beyond the row, counts below -1, a free count
  * or a page id out of range set the device error word (the request is
  * refused; tokens on a bad page get slot -1, and -1 goes on the stack for a

@@ -481,7 +481,8 @@ tk_status tk_qk_norm_rope_backward(const tk_rope_desc* desc, int32_t batch, int3
  * bad page that is given back).
  * page_size as in tk_cache_desc; batch <= 4096; num_pages * page_size,
  * max_pages_per_seq * page_size and batch * max_pages_per_seq at most 2^30.
- * Launched with programmatic dependent launch.                             */
+ * Launched with programmatic dependent launch; the next kernel on the stream
+ * starts when this one has written the tables.                             */
 tk_status tk_block_tables(int32_t batch, int32_t page_size, int32_t num_pages,
                           int32_t max_pages_per_seq, const int32_t* seq_lens,
                           const int32_t* new_lens, int32_t* page_table, int32_t* free_pages,

@@ -82,8 +82,10 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
   int* cur = pop + p.B;                 // [B] its partly filled page
   const int ps = p.page_size;
   const int64 row_tokens = static_cast<int64>(p.max_pages) * ps;     // at most 2^30
+  // No pdl_trigger(): the kernel that follows may read lengths and page table
+  // ahead of its own wait, to prefetch by them (the decode does); it starts
+  // when they are written.
   pdl_wait();
-  pdl_trigger();
 
   const int b0 = threadIdx.x * K;
   int L[K], n[K];

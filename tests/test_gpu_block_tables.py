@@ -198,3 +198,42 @@ def test_prepared_graph_replays():
     assert sorted(owned + pool.free_pages[:pool.free_count.item()].tolist()) == list(range(12))
     assert slots.tolist() == [p * ps + 8 for p in pool.page_table[:, 2].tolist()]
     assert tb.tk_get_device_error() == 0
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_decode_right_behind_the_tables(graph):
+    """The decode reads lengths and page table ahead of its wait (a prefetch): with the tables just written by the
+    kernel before it, its result is still that of a call on settled tables."""
+    require_gpu()
+    B, hq, hkv, r, dv, ps, mp = 4, 8, 2, 32, 64, 16, 8
+    num_pages = B * mp
+    pool = tb.PagePool.allocate(B, mp, ps, num_pages)
+    c = tb.ThinKeyCache.allocate(B, hq, hkv, r, dv, page_size=ps, num_pages=num_pages, page_table=pool.page_table)
+    c.k.copy_(torch.randn(c.k.shape, device="cuda"))
+    c.v.copy_(torch.randn(c.v.shape, device="cuda"))
+    q = torch.randn(B, hq, r, device="cuda").to(torch.bfloat16)
+    new = torch.tensor([1, 1, 1, 1], **I32)
+    slots, pos = torch.empty(B, **I32), torch.empty(B, **I32)
+    out, ref = torch.empty(B, hq, dv, device="cuda"), torch.empty(B, hq, dv, device="cuda")
+    ws = tb.decode_workspace(c.desc, mp * ps)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        tables = tb.prepare_block_tables(pool, new, slots, pos, tokens_per_seq=1, stream=s)
+
+        def step():
+            tables()
+            tb.tk_attn_decode(c, q, pool.seq_lens, mp * ps, out, ws)
+
+        step()
+        if graph:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                step()
+        for i in range(3 * ps * mp // 4):
+            new.fill_(-1 if i == 40 else 1)             # once everybody leaves and the pages come back
+            g.replay() if graph else step()
+            s.synchronize()
+            tb.tk_attn_decode(c, q, pool.seq_lens, mp * ps, ref, ws)
+            assert torch.equal(out, ref), i
+    assert tb.tk_get_device_error() == 0

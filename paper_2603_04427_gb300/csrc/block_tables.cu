@@ -16,7 +16,7 @@
 // in and out.
 //
 // Bound by latency: one launch, two dependent loads and one scan (three where
-// a request is refused): 3.4 us for 64 single tokens, 8.0 us for 512 prompts
+// a request is refused): 3.4 us for 64 single tokens, 6.8 us for 512 prompts
 // with 512 K rows.
 // The second load (each sequence's partly filled page, the stack's top) is
 // issued before the scan and lands behind it.

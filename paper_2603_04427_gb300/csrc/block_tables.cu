@@ -126,9 +126,9 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
   if (bad && blockIdx.x == 0) record_error(p.err, TK_DEVERR_INDEX);
   int64 total_wanted, total_pages;
   block_scan<kWarps>(wanted, pages, &total_wanted, &total_pages, scan);
-  // the whole block has read the lengths and the free count
-  if (threadIdx.x == 0 && gridDim.x > 1)
-    last = atomicAdd(p.counter, 1) == static_cast<int>(gridDim.x) - 1;
+  // the whole block has read the lengths and the free count (the scan's barriers
+  // are between), which the last block to arrive may overwrite
+  if (threadIdx.x == 0 && gridDim.x > 1) last = arrive(p.counter) == static_cast<int>(gridDim.x) - 1;
   const int total_ret = low(total_pages);
   const int64 avail = static_cast<int64>(f) + total_ret;
   int first_ret = low(pages);

@@ -30,15 +30,6 @@ constexpr int kThreads = 512, kWarpsB = kThreads / 32;
 template <typename X, typename D>
 constexpr int rows_held() { return sizeof(X) + sizeof(D) == 8 ? 2 : 4; }
 
-// Counts the block in.  Release and acquire at GPU scope: with the barriers
-// around it, what the block wrote before is visible to the block that arrives
-// last.
-__device__ __forceinline__ int arrive(int* counter) {
-  int before;
-  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
-  return before;
-}
-
 // One tensor's units (M: 0 = q, 1 = k) from `unit` to `end`: dx written, the
 // lane's share of dw returned in slots.  weights: the tensor's norm weights in
 // slot order, 8 a lane of the row.

@@ -1,0 +1,49 @@
+"""tk_block_tables: what a step leaves behind in the arrays that it reads and writes."""
+
+import numpy as np
+import pytest
+import torch
+
+from _helpers import require_gpu
+from oracle import rope
+from paper_2603_04427_gb300 import binding as tb
+
+pytestmark = pytest.mark.gpu
+
+I32 = dict(dtype=torch.int32, device="cuda")
+
+
+def test_lengths_in_place_over_many_blocks():
+    """The lengths and the free count that every block reads are overwritten by the same call: with hundreds of
+    blocks, each of many runs from the same state gives the oracle's step."""
+    require_gpu()
+    rng = np.random.default_rng(2)
+    B, ps, max_pages = 4096, 16, 8
+    lens = rng.integers(0, 4 * ps, B)
+    held = -(-lens // ps)
+    new = rng.integers(-1, 60, B)
+    P = int(held.sum()) + 8000
+    ids = rng.permutation(P)
+    table = np.full((B, max_pages), -1)
+    at = np.cumsum(held) - held
+    for b in range(B):
+        table[b, :held[b]] = ids[at[b]:at[b] + held[b]]
+    free = np.full(P, -5)
+    free[:8000] = ids[held.sum():]
+    rows = int(np.maximum(new, 0).sum())
+    assert rows > torch.cuda.get_device_properties(0).multi_processor_count * 512
+    ref = rope.block_tables(lens, new, table, free, 8000, ps, rows, 0)
+    start = [torch.tensor(x, **I32) for x in (table, free, [8000], lens)]
+    pool = tb.PagePool(ps, *(x.clone() for x in start), torch.zeros(1, **I32))
+    now = (pool.page_table, pool.free_pages, pool.free_count, pool.seq_lens)
+    counts, slots, pos = torch.tensor(new, **I32), torch.empty(rows, **I32), torch.empty(rows, **I32)
+    want = [torch.tensor(np.asarray(ref[k]).reshape(-1), **I32)
+            for k in ("page_table", "free_pages", "free_count", "seq_lens", "slots", "positions")]
+    for i in range(50):
+        for x, x0 in zip(now, start):
+            x.copy_(x0)
+        slots.fill_(77)
+        tb.tk_block_tables(pool, counts, slots, pos)
+        for x, y in zip((*now, slots, pos), want):
+            assert torch.equal(x.view(-1), y), i
+    assert tb.tk_get_device_error() == 0 and pool.workspace.item() == 0

@@ -477,8 +477,9 @@ tk_status tk_qk_norm_rope_backward(const tk_rope_desc* desc, int32_t batch, int3
  * refused request keeps its pages and length and gets no
  * slots.  Lengths below 0 or beyond the row, counts below -1, a free count
  * or a page id out of range set the device error word (the request is
- * refused; tokens on a bad page get slot -1, and -1 goes on the stack for a
- * bad page that is given back).
+ * refused, and as long as its length is out of range so it is at every step,
+ * -1 included: its pages are not given back; tokens on a bad page get slot -1,
+ * and -1 goes on the stack for a bad page that is given back).
  * page_size as in tk_cache_desc; batch <= 4096; num_pages * page_size,
  * max_pages_per_seq * page_size and batch * max_pages_per_seq at most 2^30.
  * Launched with programmatic dependent launch; the next kernel on the stream

@@ -109,14 +109,16 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const __grid_con
   for (int i = 0; i < K; ++i) {
     const bool valid = L[i] >= 0 && n[i] >= -1 && L[i] <= row_tokens;
     bad |= !valid;
-    L[i] = static_cast<int>(min(max(static_cast<int64>(L[i]), 0ll), row_tokens));
+    // an ill-formed request is taken for an empty one here; its own length is
+    // what it keeps, so that later steps refuse it too and never free its row
+    const int have = valid ? L[i] : 0;
     done[i] = valid && n[i] == -1;
     want[i] = max(n[i], 0);
-    held[i] = (L[i] + (ps - 1)) >> p.page_shift;
+    held[i] = (have + (ps - 1)) >> p.page_shift;
     page[i] = -1;
-    if (b0 + i < p.B && (L[i] & (ps - 1)) != 0)
-      page[i] = p.page_table[static_cast<size_t>(b0 + i) * p.max_pages + (L[i] >> p.page_shift)];
-    const int64 to = static_cast<int64>(L[i]) + want[i];
+    if (b0 + i < p.B && (have & (ps - 1)) != 0)
+      page[i] = p.page_table[static_cast<size_t>(b0 + i) * p.max_pages + (have >> p.page_shift)];
+    const int64 to = static_cast<int64>(have) + want[i];
     fits[i] = valid && !done[i] && to <= row_tokens && (!p.per_seq || want[i] <= p.per_seq);
     odd |= !fits[i] && !done[i];
     need[i] = fits[i] ? static_cast<int>((to + ps - 1) >> p.page_shift) - held[i] : 0;

@@ -13,6 +13,34 @@ pytestmark = pytest.mark.gpu
 I32 = dict(dtype=torch.int32, device="cuda")
 
 
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("length,new", [(-4, 1), (49, 1), (49, 0), (-(2 ** 31), 0), (2 ** 31 - 1, 1), (20, -2)])
+def test_ill_formed_request_keeps_its_length(length, new, in_place):
+    """It is refused and flagged at every step, its length stays as it is, and finishing it frees nothing: the
+    ids in its row may belong to others."""
+    require_gpu()
+    lens, table = [20, length, 3], [[0, 1, -1], [2, 3, 4], [5, -1, -1]]
+    pool = tb.PagePool(16, torch.tensor(table, **I32), torch.tensor([6, 7, -1, -1, -1, -1, -1, -1], **I32),
+                       torch.tensor([2], **I32), torch.tensor(lens, **I32), torch.zeros(1, **I32))
+    slots, pos, refused = torch.empty(16, **I32), torch.empty(16, **I32), torch.empty(1, **I32)
+    own = {} if in_place else dict(seq_lens_out=torch.empty(3, **I32), free_count_out=torch.empty(1, **I32))
+    after = pool.seq_lens if in_place else own["seq_lens_out"]
+    free = pool.free_count if in_place else own["free_count_out"]
+
+    def step(counts):
+        tb.tk_block_tables(pool, torch.tensor(counts, **I32), slots, pos, refused=refused, **own)
+        assert tb.tk_get_device_error() == 1 and refused.item() == 1
+
+    step([1, new, 14])
+    assert after.tolist() == [21, length, 17] and free.item() == 1
+    if not -1 < length < 49:                         # finished, and still ill-formed
+        step([0, -1, 0])
+        assert after.tolist()[1] == length
+        assert free.item() == (1 if in_place else 2)
+        assert pool.free_pages[:2].tolist() == [6, 7] and bool((pool.free_pages[2:] == -1).all())
+    assert pool.page_table[1].tolist() == table[1]
+
+
 def test_lengths_in_place_over_many_blocks():
     """The lengths and the free count that every block reads are overwritten by the same call: with hundreds of
     blocks, each of many runs from the same state gives the oracle's step."""

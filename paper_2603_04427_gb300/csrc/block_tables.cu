@@ -316,9 +316,11 @@ template <int kThreads, int K, int kPer>
 cudaError_t launch_t(const BlockTableParams& p, int num_sms, cudaStream_t s) {
   const size_t smem = (5 * static_cast<size_t>(p.B) + 2) * sizeof(int);
   if (smem > 32 * 1024) {
+    // the limit of the largest batch, not of this one: it holds for the calls
+    // of every host thread
     const cudaError_t e = cudaFuncSetAttribute(block_tables_kernel<kThreads, K, kPer>,
                                                cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               static_cast<int>(smem));
+                                               static_cast<int>((5 * kMaxTableBatch + 2) * sizeof(int)));
     if (e != cudaSuccess) return e;
   }
   // Blocks for the rows, and for an eighth of the pages that finished requests

@@ -1,5 +1,7 @@
 """tk_block_tables: what a step leaves behind in the arrays that it reads and writes."""
 
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -39,6 +41,36 @@ def test_ill_formed_request_keeps_its_length(length, new, in_place):
         assert free.item() == (1 if in_place else 2)
         assert pool.free_pages[:2].tolist() == [6, 7] and bool((pool.free_pages[2:] == -1).all())
     assert pool.page_table[1].tolist() == table[1]
+
+
+def test_batches_of_several_sizes_from_several_threads():
+    """Three host threads, each with a pool, a stream and a large batch of its own: every call is launched."""
+    require_gpu()
+    failed = []
+
+    def work(B):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                pool = tb.PagePool.allocate(B, 4, 16, B)
+                new, slots, pos = torch.zeros(B, **I32), torch.empty(B, **I32), torch.empty(B, **I32)
+                call = tb.prepare_block_tables(pool, new, slots, pos, tokens_per_seq=1, stream=s)
+                for i in range(20000):
+                    call()
+                    if i % 500 == 0:
+                        s.synchronize()
+                s.synchronize()
+                assert bool((slots == -1).all())
+        except Exception as e:
+            failed.append(f"batch {B}: {e}")
+
+    threads = [threading.Thread(target=work, args=(B,)) for B in (4096, 1700, 2500)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    assert tb.tk_get_device_error() == 0
 
 
 def test_lengths_in_place_over_many_blocks():

@@ -62,7 +62,8 @@ __device__ __forceinline__ SlotRow slot_row(const QkParams& p, uint32_t token, b
 
 // A lane's eight key elements as codes: symmetric absmax per (token, kv head),
 // scale = amax / Q, code = clamp(rint(y / scale), -Q, Q), both quotients as
-// binary32 division rounds them, amax 0 storing scale 0 and zero codes.  y is
+// binary32 division rounds them, a scale of 0 (amax 0, which a row of NaNs has
+// too: they are not compared) storing zero codes.  y is
 // the fp32 result of the rotation, not rounded to bf16 first: one rounding
 // less than an append of bf16 keys makes.
 // y / scale takes the row's one reciprocal and two corrections by the FMA
@@ -94,6 +95,7 @@ __device__ __forceinline__ void store_codes(const QkParams& p, int64_t row, bool
     x = __fmaf_rn(__fmaf_rn(-x, s, a), inv, x);
     code[e] = static_cast<int>(fminf(fmaxf(rintf(x), -Q), Q));
   }
+  const uint32_t some = scale == 0.f ? 0u : ~0u;
   unsigned char* k = static_cast<unsigned char*>(p.k_cache);
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
@@ -101,10 +103,10 @@ __device__ __forceinline__ void store_codes(const QkParams& p, int64_t row, bool
     const int o = half ? ob : oa;      // a multiple of 4
     if constexpr (KF == 1) {
       *reinterpret_cast<uint32_t*>(k + row * R + o) =
-          (c[0] & 0xFF) | (c[1] & 0xFF) << 8 | (c[2] & 0xFF) << 16 | static_cast<uint32_t>(c[3] & 0xFF) << 24;
+          some & ((c[0] & 0xFF) | (c[1] & 0xFF) << 8 | (c[2] & 0xFF) << 16 | static_cast<uint32_t>(c[3] & 0xFF) << 24);
     } else {
       *reinterpret_cast<uint16_t*>(k + row * (R / 2) + o / 2) = static_cast<uint16_t>(
-          (c[0] & 0xF) | (c[1] & 0xF) << 4 | (c[2] & 0xF) << 8 | (c[3] & 0xF) << 12);
+          some & ((c[0] & 0xF) | (c[1] & 0xF) << 4 | (c[2] & 0xF) << 8 | (c[3] & 0xF) << 12));
     }
   }
   if (sub == 0) p.k_scale[row] = scale;

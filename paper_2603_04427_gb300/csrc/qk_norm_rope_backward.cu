@@ -89,12 +89,13 @@ __device__ __forceinline__ Row8 backward_units(const QkParams& p, uint32_t unit,
         const float ss = row_sum<G>(dot8(xs, xs)), gx = row_sum<G>(dot8(yu, xs));
         const float rho = inv_rms(ss, 1.0f / R, p.eps);
         const float2 mean = both(-rho * rho * (gx * (1.0f / R)));
-        const float2 rho2 = both(rho), add = both(live ? rho : 0.f);
+        const float2 rho2 = both(rho);
+        if (live) {        // not a product with 0, which an infinity would turn into NaN
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          dw.v[e] = ffma2(y.v[e], fmul2(xs.v[e], add), dw.v[e]);
-          y.v[e] = fmul2(rho2, ffma2(xs.v[e], mean, yu.v[e]));
+          for (int e = 0; e < 4; ++e) dw.v[e] = ffma2(y.v[e], fmul2(xs.v[e], rho2), dw.v[e]);
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y.v[e] = fmul2(rho2, ffma2(xs.v[e], mean, yu.v[e]));
       }
       if (live) store_row<MODE>(dst + i * out.sh, oa, ob, y);
     }

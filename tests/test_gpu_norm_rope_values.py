@@ -1,14 +1,43 @@
 """Norm + rotation on infinities and NaNs."""
 
+import numpy as np
 import pytest
 import torch
 
-from _helpers import require_gpu
+from _helpers import f64, require_gpu
+from oracle import rope
 from paper_2603_04427_gb300 import binding as tb
 
 pytestmark = pytest.mark.gpu
 
 BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("xt,gt", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("r,S,at", [(32, 19, (0, 18)), (32, 19, (3, 18)), (64, 9, (4, 8)), (128, 3, (3, 2)), (16, 16, (4, 7))])
+def test_infinite_gradient_reaches_its_weight_alone(xt, gt, r, S, at):
+    """One infinite incoming gradient, in the last token or the first row of a run of heads, whose row fills the
+    places of rows that are not there: its weight's gradient is that infinity, the others are what they were."""
+    require_gpu()
+    H, c = 5, 6
+    plan = tb.rope_plan(r, rot_dim=0, eps=1e-5)
+    gen = torch.Generator().manual_seed(r + S)
+    x, g = (torch.randn(1, H, S, r, generator=gen).cuda() for _ in range(2))
+    x, g = x.to(xt), g.to(gt)
+    h, t = at
+    g[0, h, t, c] = float("inf")
+    dx, dw = torch.empty_like(x), torch.empty(r, device="cuda")
+    tb.tk_qk_norm_rope_backward(plan, x, None, None, g, None, None, dx, None, None, dq_weight=dw)
+    assert tb.tk_get_device_error() == 0
+    with np.errstate(invalid="ignore"):
+        _, ref, terms, _ = rope.norm_rope_backward(f64(x), np.ones(r), f64(g), np.zeros((1, S, 0)), 0, "half", True, 1e-5)
+    assert np.isinf(ref[c]) and dw[c].item() == ref[c]
+    rest = np.arange(r) != c
+    # the relative error of each term of dw: 1e-5 (tests/test_gpu_norm_rope.py)
+    assert np.all(np.abs(f64(dw)[rest] - ref[rest]) <= 1e-5 * terms[rest])
+    clean = torch.ones(H, S, dtype=torch.bool, device="cuda")
+    clean[h, t] = False
+    assert bool(dx[0][clean].isfinite().all())
 
 
 @pytest.mark.parametrize("xt", [BF, F32])

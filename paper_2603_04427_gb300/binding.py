@@ -534,7 +534,8 @@ def rope_plan(r: int, rot_dim: int | None = None, layout: str = "half", base: fl
     if axes is not None and inv_freq is not None:
         raise ValueError("axes and inv_freq are exclusive")
     if inv_freq is None:
-        runs = tuple(axes) if axes is not None else (pairs,)
+        axes = None if axes is None else tuple(axes)
+        runs = (pairs,) if axes is None else axes
         if any(n < 0 for n in runs) or sum(runs) != pairs:
             raise ValueError(f"axes {runs} do not add up to {pairs} pairs")
         inv_freq = [base ** (-i / n) for n in runs for i in range(n)]
@@ -547,8 +548,12 @@ def rope_plan(r: int, rot_dim: int | None = None, layout: str = "half", base: fl
                          f"(at most {TK_ROPE_MAX_PAIRS})")
     if any(not 0 <= a < TK_ROPE_MAX_AXES for a in pair_axis):
         raise ValueError(f"pair_axis entries must be in 0 .. {TK_ROPE_MAX_AXES - 1}")
-    d = tk_rope_desc(r, rot, TK_ROPE_HALF if layout == "half" else TK_ROPE_PAIR,
-                     max(pair_axis, default=0) + 1, 1 if norm else 0, eps, w_offset)
+    # an axis without pairs is an axis of the positions all the same
+    n_axes = max(max(pair_axis, default=0) + 1, 0 if axes is None else len(axes))
+    if n_axes > TK_ROPE_MAX_AXES:
+        raise ValueError(f"{n_axes} axes (at most {TK_ROPE_MAX_AXES})")
+    d = tk_rope_desc(r, rot, TK_ROPE_HALF if layout == "half" else TK_ROPE_PAIR, n_axes, 1 if norm else 0, eps,
+                     w_offset)
     d.inv_freq[:pairs] = inv_freq
     d.pair_axis[:pairs] = pair_axis
     return d

@@ -620,6 +620,12 @@ def _positions(plan, positions, B, S, device):
     return positions.data_ptr(), stride[0], stride[1]
 
 
+def _need_current(index):
+    """The library launches on the current GPU, whatever the stream is of."""
+    if index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on CUDA device {index}, the current one is {torch.cuda.current_device()}")
+
+
 def _first(*tensors):
     """(batch, tokens, device, its index) by the first tensor that is there."""
     for t in tensors:
@@ -629,7 +635,9 @@ def _first(*tensors):
             if not t.is_cuda:
                 raise ValueError("expected CUDA tensors")
             B, _, S, _ = t.shape
-            return B, S, t.device, t.get_device()
+            at = t.get_device()
+            _need_current(at)
+            return B, S, t.device, at
     raise ValueError("q, k and v are all None")
 
 
@@ -695,6 +703,9 @@ def prepare_qk_norm_rope_append(cache: ThinKeyCache, plan: tk_rope_desc, q, k, v
 
 def qk_norm_rope_workspace(plan: tk_rope_desc, device="cuda") -> torch.Tensor:
     """A zero-filled workspace of the size tk_qk_norm_rope_backward needs for weight gradients."""
+    device = torch.device(device)
+    if device.index is not None:
+        _need_current(device.index)      # the size goes by its SM count
     n = int(load_library().tk_qk_norm_rope_workspace_size(ctypes.byref(plan)))
     if n == 0:
         raise TkError(TK_ERR_INVALID_ARG, "tk_qk_norm_rope_workspace_size", tk_last_error())
@@ -776,6 +787,7 @@ def _table_args(pool, new_lens, slots, positions, tokens_per_seq, offsets, seq_l
         _need(t, torch.int32, n, dev)
         if t is not None and t.numel() != size:
             raise ValueError(f"{n} has {t.numel()} elements, expected {size}")
+    _need_current(dev.index)
     args = (B, pool.page_size, num_pages, max_pages, _ptr(pool.seq_lens), _ptr(new_lens), _ptr(pool.page_table),
             _ptr(pool.free_pages), _ptr(pool.free_count), int(tokens_per_seq), rows, _ptr(slots),
             _ptr(positions), _ptr(offsets), _ptr(seq_lens_out), _ptr(free_count_out), _ptr(refused),

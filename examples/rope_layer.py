@@ -67,10 +67,21 @@ class Server:
         self.q = torch.empty(batch, layer.h_q, 1, layer.r, dtype=BF16, device="cuda")
         self.out = torch.empty(batch, layer.h_q, layer.d_v, device="cuda")
         self.workspace = tk.decode_workspace(self.cache.desc, max_len)
-        self.tables = tk.prepare_block_tables(self.pool, self.new, self.slots, self.pos, tokens_per_seq=1)
+        # lengths and free pages after a step, the pool's own only once nothing was refused
+        self.lens, self.free, self.refused = torch.empty(batch, **i32), torch.empty(1, **i32), torch.empty(1, **i32)
+        self.after = dict(seq_lens_out=self.lens, free_count_out=self.free, refused=self.refused)
+        self.tables = tk.prepare_block_tables(self.pool, self.new, self.slots, self.pos, tokens_per_seq=1, **self.after)
         self.append = tk.prepare_qk_norm_rope_append(
             self.cache, layer.plan, *layer.heads(self.packed), self.pos[:, None], self.slots, self.q,
             q_weight=layer.norm_q, k_weight=layer.norm_k)
+
+    def keep_step(self):
+        """Takes over the step that tk_block_tables worked out, or, if a request was refused, leaves it: a step in
+        which nobody finishes writes only what the old lengths and free count leave unused."""
+        if self.refused.item():
+            raise RuntimeError("the page pool, or a row of the page table, does not hold this step")
+        self.pool.seq_lens.copy_(self.lens)
+        self.pool.free_count.copy_(self.free)
 
     def admit(self, prompts):
         """Prompts, one [tokens, d_model] per sequence (None: idle) -> attention outputs, head-major."""
@@ -101,9 +112,11 @@ class Server:
         return outs
 
     def decode(self, x):
-        """One token per sequence, x [batch, d_model] -> attention output [batch, h_q, d_v]."""
+        """One token per sequence, x [batch, d_model] -> attention output [batch, h_q, d_v].  Raises, and changes
+        nothing, if one of them does not fit."""
         torch.matmul(x, self.layer.w, out=self.packed.view(self.batch, -1))
         self.tables()
+        self.keep_step()
         self.append()
         return tk.tk_attn_decode(self.cache, self.q.view(self.batch, self.layer.h_q, -1), self.pool.seq_lens,
                                  self.max_len, self.out, self.workspace)

@@ -1,0 +1,58 @@
+"""The example's server when requests do not fit or are finished."""
+
+import importlib.util
+import os
+
+import pytest
+import torch
+
+from _helpers import require_gpu
+from paper_2603_04427_gb300 import binding as tb
+
+pytestmark = pytest.mark.gpu
+
+PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "rope_layer.py")
+
+
+def _server(batch, max_len, num_pages):
+    spec = importlib.util.spec_from_file_location("rope_layer", PATH)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    layer = m.Layer(d_model=128, h_q=8, h_kv=2, r=32, d_v=64, seed=3)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    new = lambda n: torch.randn(n, 128, device="cuda", generator=g).to(torch.bfloat16)  # noqa: E731
+    return m.Server(layer, batch, max_len=max_len, num_pages=num_pages), new
+
+
+def _state(server):
+    return server.pool.seq_lens.tolist(), server.pool.free_count.item()
+
+
+def _is_last_row_of_prefill(server, tokens, got):
+    layer, n = server.layer, tokens.shape[0]
+    q, k, v = layer.rotated((tokens @ layer.w)[None], torch.arange(n, dtype=torch.int32, device="cuda")[None])
+    out = torch.empty(1, 8, n, 64, device="cuda")
+    tb.tk_attn_prefill(q, k, v, out)
+    # P in bf16 on either side (tests/test_gpu_rope_layer.py)
+    assert float((out[0, :, -1] - got).abs().max()) <= 2e-2
+
+
+@pytest.mark.parametrize("max_len,num_pages", [(64, 3), (64, 4), (32, 8)])
+def test_decode_step_that_does_not_fit(max_len, num_pages):
+    """No page left, a page for one of two, a full row of the page table: the step raises and changes nothing, and
+    can be made once a request has finished."""
+    require_gpu()
+    server, new = _server(2, max_len, num_pages)
+    held = [new(32), new(16)]                          # 2 + 1 full pages
+    server.admit(held)
+    before = _state(server)
+    assert before == ([32, 16], num_pages - 3)
+    x = new(2)
+    for _ in range(2):
+        with pytest.raises(RuntimeError):
+            server.decode(x)
+        assert _state(server) == before
+    server.finish([0])
+    got = server.decode(x)
+    _is_last_row_of_prefill(server, torch.cat([held[1], x[1:]]), got[1])
+    assert tb.tk_get_device_error() == 0

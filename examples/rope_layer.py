@@ -61,7 +61,7 @@ class Server:
                                               num_pages=num_pages, page_table=self.pool.page_table, k_int8=k_int8)
         i32 = dict(dtype=torch.int32, device="cuda")
         # a decode step's fixed buffers, its two prepared calls, and the attention's workspace
-        self.new = torch.ones(batch, **i32)
+        self.new = torch.zeros(batch, **i32)      # 1 for the sequences that are being served
         self.slots, self.pos = torch.empty(batch, **i32), torch.empty(batch, **i32)
         self.packed = torch.empty(batch, 1, sum(layer.widths), dtype=BF16, device="cuda")
         self.q = torch.empty(batch, layer.h_q, 1, layer.r, dtype=BF16, device="cuda")
@@ -109,11 +109,12 @@ class Server:
             tk.tk_attn_prefill_cached(one, q, k, v, before[b:b + 1], self.max_len, out)
             outs.append(out)
             row += n
+            self.new[b] = 1
         return outs
 
     def decode(self, x):
-        """One token per sequence, x [batch, d_model] -> attention output [batch, h_q, d_v].  Raises, and changes
-        nothing, if one of them does not fit."""
+        """One token per served sequence, x [batch, d_model] -> attention output [batch, h_q, d_v], zero for the
+        others.  Raises, and changes nothing, if one of them does not fit."""
         torch.matmul(x, self.layer.w, out=self.packed.view(self.batch, -1))
         self.tables()
         self.keep_step()
@@ -122,7 +123,8 @@ class Server:
                                  self.max_len, self.out, self.workspace)
 
     def finish(self, which):
-        """Gives back the pages of the sequences in `which`."""
+        """Gives back the pages of the sequences in `which`, which then stay empty until prompts are admitted."""
+        self.new[which] = 0
         new = torch.zeros(self.batch, dtype=torch.int32, device="cuda")
         new[which] = -1
         empty = torch.empty(0, dtype=torch.int32, device="cuda")

@@ -56,3 +56,25 @@ def test_decode_step_that_does_not_fit(max_len, num_pages):
     got = server.decode(x)
     _is_last_row_of_prefill(server, torch.cat([held[1], x[1:]]), got[1])
     assert tb.tk_get_device_error() == 0
+
+
+def test_finished_sequence_stays_empty():
+    """Its place in the batch takes no tokens and no pages until a prompt is admitted to it."""
+    require_gpu()
+    server, new = _server(2, 64, 8)
+    held = new(40)
+    server.admit([new(20), held])
+    server.finish([0])
+    assert _state(server) == ([0, 40], 5)
+    for i in range(3):
+        x = new(2)
+        held = torch.cat([held, x[1:]])
+        got = server.decode(x)
+        assert _state(server) == ([0, 41 + i], 5)
+        assert bool((got[0] == 0).all())
+        _is_last_row_of_prefill(server, held, got[1])
+    prompt, x = new(5), new(2)
+    server.admit([prompt, None])
+    got = server.decode(x)
+    _is_last_row_of_prefill(server, torch.cat([prompt, x[:1]]), got[0])
+    assert _state(server)[0] == [6, 44] and tb.tk_get_device_error() == 0

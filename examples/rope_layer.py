@@ -84,15 +84,14 @@ class Server:
         self.pool.free_count.copy_(self.free)
 
     def admit(self, prompts):
-        """Prompts, one [tokens, d_model] per sequence (None: idle) -> attention outputs, head-major."""
+        """Prompts, one [tokens, d_model] per sequence (None: idle) -> attention outputs, head-major.  Raises, and
+        changes nothing, if one of them does not fit."""
         lens = [0 if x is None else x.shape[0] for x in prompts]
         i32 = dict(dtype=torch.int32, device="cuda")
         before = self.pool.seq_lens.clone()
         slots, pos = torch.empty(sum(lens), **i32), torch.empty(sum(lens), **i32)
-        refused = torch.empty(1, **i32)
-        tk.tk_block_tables(self.pool, torch.tensor(lens, **i32), slots, pos, refused=refused)
-        if refused.item():
-            raise RuntimeError("the page pool does not hold these prompts")
+        tk.tk_block_tables(self.pool, torch.tensor(lens, **i32), slots, pos, **self.after)
+        self.keep_step()
         layer, outs, row = self.layer, [], 0
         for b, x in enumerate(prompts):
             if x is None:

@@ -78,3 +78,22 @@ def test_finished_sequence_stays_empty():
     got = server.decode(x)
     _is_last_row_of_prefill(server, torch.cat([prompt, x[:1]]), got[0])
     assert _state(server)[0] == [6, 44] and tb.tk_get_device_error() == 0
+
+
+def test_refused_prompts_change_nothing():
+    """A call whose second prompt does not fit leaves the first one out too, and it can be admitted later."""
+    require_gpu()
+    server, new = _server(2, 64, 4)
+    prompt = new(20)
+    for _ in range(2):
+        with pytest.raises(RuntimeError):
+            server.admit([prompt, new(40)])            # 2 + 3 pages
+        assert _state(server) == ([0, 0], 4)
+    server.admit([prompt, None])
+    assert _state(server) == ([20, 0], 2)
+    x = new(2)
+    got = server.decode(x)
+    _is_last_row_of_prefill(server, torch.cat([prompt, x[:1]]), got[0])
+    with pytest.raises(RuntimeError):                  # one more chunk than the row holds
+        server.admit([new(50), None])
+    assert _state(server)[0][0] == 21 and tb.tk_get_device_error() == 0

@@ -179,7 +179,10 @@ norm_rope_kernel(const __grid_constant__ QkParams p) {
   SlotRow slot{0, false};
   if (KF >= 0 && !is_q) slot = slot_row(p, token, ok);
   const Row8 w = load_weights<MODE>(is_q ? p.wq : p.wk, p.w_f32, p.w_offset, oa, ob);
-  const Turns t = make_turns(p, sub, load_places(p, sub, b, s));
+  // results of 32 bits, and the keys that are quantised from them
+  const bool full = KF < 0 ? sizeof(O) == 4 : KF > 0 && !is_q;
+  const Places places = load_places(p, sub, b, s);
+  const Turns t = full ? make_turns<true>(p, sub, places) : make_turns<false>(p, sub, places);
   const HeadsView out = is_q ? p.qo : p.ko;
   O* dst = static_cast<O*>(out.p) + b * out.sb + s * out.st + h0 * out.sh;
   int64_t row = slot.block_row + static_cast<int64_t>(h0) * p.slot_rows;
@@ -187,7 +190,7 @@ norm_rope_kernel(const __grid_constant__ QkParams p) {
     Row8 y = slots_of<MODE>(x);
     // without norm the row is multiplied by 1, which changes no bit
     const float ss = row_sum<G>(dot8(y, y));
-    const float rho = p.norm ? inv_rms(ss, 1.0f / R, p.eps) : 1.f;
+    const float rho = p.norm ? inv_rms(ss, 1.0f / R, p.eps, full) : 1.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) y.v[i] = fmul2(fmul2(y.v[i], both(rho)), w.v[i]);
     rotate8<MODE, false>(y, t);

@@ -37,6 +37,7 @@ template <int M, int R, int MODE, typename X, typename D>
 __device__ __forceinline__ Row8 backward_units(const QkParams& p, uint32_t unit, uint32_t end, int lane,
                                                int oa, int ob, const float* weights) {
   constexpr int G = R / 8, T = 32 / G, kRun = rows_held<X, D>();
+  constexpr bool kFull = sizeof(X) == 4;     // rows and dx of 32 bits
   const HeadsView& gin = M ? p.ko : p.qo;
   const HeadsView& xin = M ? p.k : p.q;
   const HeadsView& out = M ? p.dk : p.dq;
@@ -74,7 +75,7 @@ __device__ __forceinline__ Row8 backward_units(const QkParams& p, uint32_t unit,
       rg[i].load(g + k * gin.sh, oa, ob);
       if (p.norm) rx[i].load(x + k * xin.sh, oa, ob);
     }
-    if (fresh) t = make_turns(p, sub, at);
+    if (fresh) t = make_turns<kFull>(p, sub, at);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
       const bool live = ok && i < nh;
@@ -87,7 +88,7 @@ __device__ __forceinline__ Row8 backward_units(const QkParams& p, uint32_t unit,
 #pragma unroll
         for (int e = 0; e < 4; ++e) yu.v[e] = fmul2(y.v[e], u.v[e]);
         const float ss = row_sum<G>(dot8(xs, xs)), gx = row_sum<G>(dot8(yu, xs));
-        const float rho = inv_rms(ss, 1.0f / R, p.eps);
+        const float rho = inv_rms(ss, 1.0f / R, p.eps, kFull);
         const float2 mean = both(-rho * rho * (gx * (1.0f / R)));
         const float2 rho2 = both(rho);
         if (live) {        // not a product with 0, which an infinity would turn into NaN

@@ -32,10 +32,20 @@ constexpr int kMaxPosition = TK_ROPE_MAX_POSITION;
 // The product is taken exactly as t + e (t = p f rounded, e its remainder by
 // FMA) and reduced to one period with 2 pi = C1 + C2 (Cody and Waite's split;
 // C1 is 2 pi rounded to 24 bits, so n C1 is exact inside the FMA for n below
-// 2^24): the argument's error stays below 2^-20 at every position, where
-// rounding the product alone would be wrong by 2^-8 at position 2^17.  The
-// reduced argument lies in [-pi, pi], where __sinf and __cosf are good to
-// 2^-21.2 absolute; both errors together stay below 2^-19.
+// 2^24), where rounding the product alone would be wrong by 2^-8 at position
+// 2^17.
+// FULL, for results of 32 bits and for keys quantised from them: the reduction
+// keeps what its sum loses and goes on to quarter turns (t - n C1 and
+// sum - k C1 / 4 are exact: multiples of a unit that 24 bits hold), and sine and
+// cosine of the rest, |a| <= pi / 4 and a little, are their Taylor series up to
+// a^9 and a^10 (the next terms are below 2^-29 and 2^-32): within 2^-22, and
+// 2^-23.7 up to position 2^20.
+// Otherwise, for results rounded to bf16, the argument's error stays below
+// 2^-20, the reduced argument lies in [-pi, pi], where __sinf and __cosf are
+// good to 2^-21.2 absolute, and both errors together stay below 2^-19, beside a
+// rounding of 2^-9.  The longer form in their place made 4096 tokens 8.6 us instead
+// of 8.4, and 2 x 9721 tokens 54.0 instead of 53.2.
+template <bool FULL>
 __device__ __forceinline__ void turn(int p, float f, float* c, float* s) {
   constexpr float kInv = 0.15915494309189535f;       // 1 / (2 pi)
   constexpr float kC1 = 6.2831854820251465f;         // 2 pi to 24 bits
@@ -44,12 +54,33 @@ __device__ __forceinline__ void turn(int p, float f, float* c, float* s) {
   const float t = __fmul_rn(pf, f);
   const float e = __fmaf_rn(pf, f, -t);
   const float n = rintf(t * kInv);
-  float r = __fmaf_rn(-n, kC1, t);
-  r = __fmaf_rn(-n, kC2, r) + e;
-  const float m = rintf(r * kInv);    // the quotient's own rounding, at large t
-  r = __fmaf_rn(-m, kC1, r);
-  *c = __cosf(r);
-  *s = __sinf(r);
+  const float r = __fmaf_rn(-n, kC1, t);
+  if constexpr (!FULL) {
+    const float sum = __fmaf_rn(-n, kC2, r) + e;
+    const float m = rintf(sum * kInv);    // the quotient's own rounding, at large t
+    const float a = __fmaf_rn(-m, kC1, sum);
+    *c = __cosf(a);
+    *s = __sinf(a);
+    return;
+  }
+  const float l = __fmaf_rn(-n, kC2, e);
+  const float sum = r + l, lost = l - (sum - r);
+  const float k = rintf(sum * (4 * kInv));
+  const float a = __fmaf_rn(-k, kC1 / 4, sum) + __fmaf_rn(-k, kC2 / 4, lost);
+  const float z = a * a;
+  float si = __fmaf_rn(z, 1.f / 362880, -1.f / 5040);
+  si = __fmaf_rn(si, z, 1.f / 120);
+  si = __fmaf_rn(si, z, -1.f / 6);
+  si = __fmaf_rn(si * z, a, a);
+  float co = __fmaf_rn(z, -1.f / 3628800, 1.f / 40320);
+  co = __fmaf_rn(co, z, -1.f / 720);
+  co = __fmaf_rn(co, z, 1.f / 24);
+  co = __fmaf_rn(co, z, -0.5f);
+  co = __fmaf_rn(co, z, 1.f);
+  const int q = static_cast<int>(k);
+  const float u = q & 1 ? co : si, v = q & 1 ? si : co;
+  *s = q & 2 ? -u : u;
+  *c = (q + 1) & 2 ? -v : v;
 }
 
 // Where lane `sub` of a row's R / 8 lanes finds its quads.
@@ -90,6 +121,7 @@ struct Turns {
   float2 c[2], s[2], n[2];
   bool on;   // the lane's elements are rotated
 };
+template <bool FULL>
 __device__ __forceinline__ Turns make_turns(const QkParams& p, int sub, const Places& at) {
   float c[4] = {1.f, 1.f, 1.f, 1.f}, si[4] = {0.f, 0.f, 0.f, 0.f};
   Turns t;
@@ -99,7 +131,7 @@ __device__ __forceinline__ Turns make_turns(const QkParams& p, int sub, const Pl
     for (int i = 0; i < 4; ++i) {
       const int q = min(max(at.p[i], -kMaxPosition), kMaxPosition);
       if (q != at.p[i]) record_error(p.err, TK_DEVERR_INDEX);
-      turn(q, p.inv_freq[4 * sub + i], &c[i], &si[i]);
+      turn<FULL>(q, p.inv_freq[4 * sub + i], &c[i], &si[i]);
     }
   }
 #pragma unroll
@@ -252,11 +284,14 @@ __device__ __forceinline__ float dot8(const Row8& x, const Row8& y) {
   return s.x + s.y;
 }
 
-// (mean square + eps)^(-1/2); the sum is at least eps, a normal number.
-__device__ __forceinline__ float inv_rms(float sum, float inv_r, float eps) {
+// (mean square + eps)^(-1/2); the sum is at least eps, a normal number.  The
+// hardware's estimate is off by 2^-22.4; FULL adds a step of Newton's iteration,
+// which leaves the rounding of its own terms.
+__device__ __forceinline__ float inv_rms(float sum, float inv_r, float eps, bool full) {
+  const float x = __fmaf_rn(sum, inv_r, eps);
   float y;
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(__fmaf_rn(sum, inv_r, eps)));
-  return y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return full ? __fmaf_rn(0.5f * y, __fmaf_rn(-x * y, y, 1.f), y) : y;
 }
 
 // Sum or maximum over the G lanes of one row (neighbours inside a warp).

@@ -476,12 +476,17 @@ tk_status tk_qk_norm_rope_backward(const tk_rope_desc* desc, int32_t batch, int3
  * or if it needs pages and it and the requests before it that pass these two
  * checks need more than are free (after one such refusal every later request
  * that needs pages is refused too, and one that needs none is served).  A
- * refused request keeps its pages and length and gets no
- * slots.  Lengths below 0 or beyond the row, counts below -1, a free count
- * or a page id out of range set the device error word (the request is
- * refused, and as long as its length is out of range so it is at every step,
- * -1 included: its pages are not given back; tokens on a bad page get slot -1,
- * and -1 goes on the stack for a bad page that is given back).
+ * refused request keeps its pages and length and gets no slots.  One that can
+ * never be served (more tokens than its row holds) is for the host to withdraw:
+ * packed, its tokens count against those behind it at every step.
+ * A step in which nobody finishes can be dropped: it writes no table entry that
+ * the old lengths use and no entry of the stack, so a caller with seq_lens_out
+ * and free_count_out of its own takes the step over by copying them, or not.
+ * Lengths below 0 or beyond the row, counts below -1, a free count or a page id
+ * out of range set the device error word (the request is refused, and as long
+ * as its length is out of range so it is at every step, -1 included: its pages
+ * are not given back; tokens on a bad page get slot -1, and -1 goes on the
+ * stack for a bad page that is given back).
  * page_size as in tk_cache_desc; batch <= 4096; num_pages * page_size,
  * max_pages_per_seq * page_size and batch * max_pages_per_seq at most 2^30.
  * Launched with programmatic dependent launch; the next kernel on the stream

@@ -32,8 +32,8 @@ constexpr int kWarps = 4;
 // Rows a lane holds at a time and blocks an SM holds.  With many waves, 128
 // bytes a lane and 20 warps an SM beat 64 bytes and 28 warps (2 x 9721 tokens
 // in fp32: 53.2 us against 55.5); the append's longer code and shorter launches
-// prefer 64 bytes and 24 warps (2 x 4096 tokens to int8 keys: 15.7 us against
-// 17.8, and 16.1 with 28).
+// prefer 64 bytes and 24 warps (2 x 4096 tokens to int8 keys: 16.1 us against
+// 18.7, and 16.4 with 28).
 template <typename X, int KF>
 constexpr int rows_held() { return (KF < 0 ? 16 : 8) / static_cast<int>(sizeof(X)); }
 template <int KF>
@@ -228,7 +228,7 @@ norm_rope_kernel(const __grid_constant__ QkParams p) {
 // Units go by blocks of tokens of about a wave of warps, in which q and k come
 // before v, whose short units then fill the wave's end (4096 tokens of 32 + 8
 // heads: 8.4 us, against 9.3 with all heads of a few tokens together; 2 x 4096
-// tokens to int8 keys: 15.7 against 18.0; launches of many waves, where the
+// tokens to int8 keys: 16.1 against 18.5; launches of many waves, where the
 // rows are read almost in order either way: no difference).  False if there
 // are too many units for one launch.
 bool plan(QkParams& p, int num_sms, int warps_held) {

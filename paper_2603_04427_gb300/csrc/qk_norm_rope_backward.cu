@@ -8,11 +8,12 @@
 // stored by the forward (the row is read anyway).
 //
 // Bound by HBM (2 x 8192 tokens of 32 + 32 heads, r = 32, d_v = 128, fp32
-// gradients: 671 MB in 103.4 us, 6.5 TB/s, 96 % of a copy).  One block per SM
-// of 16 warps, four rows in flight a lane (more warps with fewer registers:
-// 114 to 146 us); each warp takes an equal share of the (token group, run of
-// heads) units of q, of k and of v (equal shares of all units in one row left
-// SMs with values alone idle a quarter of the time).  The weight gradient
+// gradients: 671 MB in 102.8 us, 6.5 TB/s, 96 % of a copy).  One block per SM
+// of 16 warps, four rows in flight a lane, two where x and g both have 32 bits
+// (more warps with fewer registers: 114 to 146 us); each warp takes an equal
+// share of the (token group, run of heads) units of q, of k and of v (equal
+// shares of all units in one row left SMs with values alone idle a quarter of
+// the time).  The weight gradient
 // gathers in eight registers a lane over a warp's units of one
 // tensor, in shared memory over the block's warps, and one partial sum per
 // block goes to the workspace, which the last block to arrive adds up in
@@ -26,7 +27,7 @@ namespace {
 
 constexpr int kThreads = 512, kWarpsB = kThreads / 32;
 
-// Rows a lane holds at a time: 96 to 128 bytes of x and g.
+// Rows a lane holds at a time: 128 bytes of x and g, 192 where their types differ.
 template <typename X, typename D>
 constexpr int rows_held() { return sizeof(X) + sizeof(D) == 8 ? 2 : 4; }
 
@@ -176,7 +177,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_rope_backward_kernel(const _
 
   // weight gradients: over the block's warps, then the blocks (summing and
   // arriving before the values, to hide the arrival's latency, cost as much in
-  // the barrier: 20.4 us against 20.0 for 4 x 2047 tokens)
+  // the barrier: 0.4 us more of the 20 for 4 x 2047 tokens)
   __syncthreads();
   for (int c = threadIdx.x; c < 2 * R; c += kThreads) {
     float a = 0.f;

@@ -362,9 +362,9 @@ typedef struct tk_heads {
  *   t = position[pair_axis[j]] * inv_freq[j]
  * with the arithmetic in fp32 and one rounding, at the output.  The angle is
  * reduced without rounding the product first, so it is as exact at position
- * 10^6 as at 10.  Absolute error of cos and sin: below 2^-22 where q_out and
- * k_out (in the backward: dq and dk) are TK_F32 and for keys stored in 8 or 4
- * bits, below 2^-19 where they are rounded to bf16.
+ * 10^6 as at 10.  Absolute error of cos and sin: below 2^-22 in the backward,
+ * where q_out and k_out are TK_F32 and for keys stored in 8 or 4 bits, below
+ * 2^-19 where q_out, k_out or the cached key is bf16.
  *   q, k, v      : inputs of one dtype, d_v wide for v (d_v in {64, 128}); NULL
  *                  (with its output) leaves that one out
  *   q_weight, k_weight: device [r] of w_dtype, 16-byte aligned, or NULL

@@ -8,7 +8,7 @@
 // stored by the forward (the row is read anyway).
 //
 // Bound by HBM (2 x 8192 tokens of 32 + 32 heads, r = 32, d_v = 128, fp32
-// gradients: 671 MB in 102.8 us, 6.5 TB/s, 96 % of a copy).  One block per SM
+// gradients: 671 MB in 103.2 us, 6.5 TB/s, 96 % of a copy).  One block per SM
 // of 16 warps, four rows in flight a lane, two where x and g both have 32 bits
 // (more warps with fewer registers: 114 to 146 us); each warp takes an equal
 // share of the (token group, run of heads) units of q, of k and of v (equal
@@ -38,7 +38,6 @@ template <int M, int R, int MODE, typename X, typename D>
 __device__ __forceinline__ Row8 backward_units(const QkParams& p, uint32_t unit, uint32_t end, int lane,
                                                int oa, int ob, const float* weights) {
   constexpr int G = R / 8, T = 32 / G, kRun = rows_held<X, D>();
-  constexpr bool kFull = sizeof(X) == 4;     // rows and dx of 32 bits
   const HeadsView& gin = M ? p.ko : p.qo;
   const HeadsView& xin = M ? p.k : p.q;
   const HeadsView& out = M ? p.dk : p.dq;
@@ -76,7 +75,7 @@ __device__ __forceinline__ Row8 backward_units(const QkParams& p, uint32_t unit,
       rg[i].load(g + k * gin.sh, oa, ob);
       if (p.norm) rx[i].load(x + k * xin.sh, oa, ob);
     }
-    if (fresh) t = make_turns<kFull>(p, sub, at);
+    if (fresh) t = make_turns<true>(p, sub, at);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
       const bool live = ok && i < nh;
@@ -89,7 +88,7 @@ __device__ __forceinline__ Row8 backward_units(const QkParams& p, uint32_t unit,
 #pragma unroll
         for (int e = 0; e < 4; ++e) yu.v[e] = fmul2(y.v[e], u.v[e]);
         const float ss = row_sum<G>(dot8(xs, xs)), gx = row_sum<G>(dot8(yu, xs));
-        const float rho = inv_rms(ss, 1.0f / R, p.eps, kFull);
+        const float rho = inv_rms(ss, 1.0f / R, p.eps, true);
         const float2 mean = both(-rho * rho * (gx * (1.0f / R)));
         const float2 rho2 = both(rho);
         if (live) {        // not a product with 0, which an infinity would turn into NaN

@@ -90,3 +90,25 @@ def test_backward(B, S, H, r, rot, layout, axes, gt):
     # a term's g mixes the two elements of its pair: its size goes by the row's largest
     big = rope.rms(f64(x), EPS) * np.abs(f64(x)) * np.abs(f64(g)).max(axis=-1, keepdims=True)
     assert np.all(np.abs(f64(dw) - rw) <= 10 * UNIT * np.maximum(terms, big.sum(axis=(0, 1, 2))))
+
+
+@pytest.mark.parametrize("xt,gt", [(BF, BF), (BF, F32), (F32, BF), (F32, F32)])
+def test_cos_and_sin_in_weight_gradients(xt, gt):
+    """One row of ones: dw is (cos, -sin) rho, in 32 bits for rows of any type.  rho = (1 + 2^-20)^(-1/2) is off by
+    2^-25 + 2^-26, the product by 2^-25, the sums add zeros: with cos and sin below 1.5 * 2^-22."""
+    require_gpu()
+    r, eps = 128, 2.0 ** -20
+    g = np.random.default_rng(4)
+    freq = np.float32(np.concatenate([10000.0 ** (-np.arange(32) / 32), g.uniform(-4, 4, 32)]))
+    plan = tb.rope_plan(r, inv_freq=freq.tolist(), eps=eps)
+    x, dy = torch.ones(1, 1, 1, r, dtype=xt, device="cuda"), torch.zeros(1, 1, 1, r, dtype=gt, device="cuda")
+    dy[..., :r // 2] = 1.0
+    dx, ws = torch.empty_like(x), tb.qk_norm_rope_workspace(plan)
+    for p in [0, 1, (1 << 24) - 1] + g.integers(-(1 << 17), 1 << 17, 200).tolist():
+        at, dw = torch.tensor([[p]], dtype=torch.int32, device="cuda"), torch.empty(r, device="cuda")
+        tb.tk_qk_norm_rope_backward(plan, x, None, at, dy, None, None, dx, None, None, dq_weight=dw, workspace=ws)
+        theta = p * freq.astype(np.float64)
+        ref = np.concatenate([np.cos(theta), -np.sin(theta)]) / np.sqrt(1 + eps)
+        worst = np.abs(f64(dw) - ref).max()
+        assert worst <= 1.5 * UNIT, f"position {p}: 2^{np.log2(worst):.2f}"
+    assert tb.tk_get_device_error() == 0

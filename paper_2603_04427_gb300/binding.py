@@ -620,10 +620,13 @@ def _positions(plan, positions, B, S, device):
     return positions.data_ptr(), stride[0], stride[1]
 
 
+_current_device = torch._C._cuda_getDevice     # torch.cuda.current_device without its set-up check (0.25 us)
+
+
 def _need_current(index):
     """The library launches on the current GPU, whatever the stream is of."""
-    if index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on CUDA device {index}, the current one is {torch.cuda.current_device()}")
+    if index != _current_device():
+        raise ValueError(f"the tensors are on CUDA device {index}, the current one is {_current_device()}")
 
 
 def _first(*tensors):

@@ -57,7 +57,7 @@ def test_tensors_of_another_gpu_than_the_current_one_are_refused(monkeypatch, cu
     def launched(*_):
         raise AssertionError("the library was called")
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+    monkeypatch.setattr(tb, "_current_device", lambda: current)
     monkeypatch.setattr(tb, "load_library", launched)
     monkeypatch.setattr(tb, "_raw_stream", lambda stream, device: 0)
     B, H, S, r, dv = 2, 4, 3, 32, 64

@@ -101,16 +101,6 @@ __device__ __forceinline__ void pdl_trigger() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// ---------------------------------------------------------------- arrival
-// Counts a block in; returns how many came before.  Release and acquire at GPU
-// scope, and a barrier of the block on each side: what its threads read and
-// wrote before comes before what the block that arrives last does after.
-__device__ __forceinline__ int arrive(int* counter) {
-  int before;
-  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
-  return before;
-}
-
 // ---------------------------------------------------------------- bulk copies
 // 1-D bulk copy global -> shared, completion signalled on `bar` as tx bytes.
 // Both addresses 16-byte aligned, bytes a multiple of 16.

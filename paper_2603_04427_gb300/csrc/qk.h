@@ -30,6 +30,17 @@ struct FastDiv {
 #endif
 };
 
+#ifdef __CUDACC__
+// Counts a block in; returns how many came before.  Release and acquire at GPU
+// scope, and a barrier of the block on each side: what its threads read and
+// wrote before comes before what the block that arrives last does after.
+__device__ __forceinline__ int arrive(int* counter) {
+  int before;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+  return before;
+}
+#endif
+
 // One tensor of heads, element strides; p == nullptr: absent.
 struct HeadsView {
   void* p;

@@ -164,8 +164,7 @@ def prepare(case, seed):
         if own:
             tk, s["cache"] = _own_cache(case, s)
             pick = tk.BlockSelection(case["block"], **s["out"])
-            ws = tk.block_select_workspace(s["cache"], ctx, block=case["block"])
-            s["call"] = tk.prepare_block_select(s["cache"], s["q"], s["bounds"], s["lens"], ctx, pick, ws)
+            s["call"] = tk.prepare_block_select(s["cache"], s["q"], s["bounds"], s["lens"], ctx, pick)
     elif op == "decode":
         # each kv head's chosen blocks in order, the last block of the context among them
         n, bs = case["n_select"], case["block"]

@@ -211,7 +211,7 @@ def prepare(case, seed):
         s["kept"] = torch.empty(B, hkv, case["keep"], **i32)
         if own:
             tk, s["cache"] = _own_cache(case, s)
-            ws = tk.cache_evict_workspace(s["cache"], ctx, case["keep"])
+            ws = tk.cache_evict_workspace(s["cache"], case["keep"])
             s["call"] = tk.prepare_cache_evict(s["cache"], s["lens"], ctx, s["w"], case["keep"], case["recent"], ws,
                                                weights_out=s["w_out"], seq_lens_out=s["lens_out"], kept=s["kept"])
     return s

@@ -499,6 +499,146 @@ tk_status tk_block_tables(int32_t batch, int32_t page_size, int32_t num_pages,
                           int32_t* seq_lens_out, int32_t* free_count_out, int32_t* refused,
                           void* workspace, void* stream);
 
+/* ------------------------------------------------------------------------
+ * A long context, read or kept in part (not part of the paper's method; thin
+ * keys make it cheap: which blocks a query needs, and how much attention a token
+ * gets, follow from r of the r + d_v numbers of a token).
+ * ------------------------------------------------------------------------ */
+
+/* Element-wise minimum and maximum of the cached keys of every block of `block`
+ * tokens (tokens j * block .. of a sequence) that holds a token at positions
+ * old_lens[b] .. seq_lens[b] - 1.
+ *   block    : 16 .. 256, a power of two; paged: the page size; contiguous: divides
+ *              the capacity
+ *   k_cache, k_scale, page_table: the cache (values are not needed)
+ *   old_lens : device int32 [batch], tokens whose blocks are bounded already, or
+ *              NULL = none (after a prompt, or when an eviction moved tokens);
+ *              a sequence with old_lens >= seq_lens is left alone
+ *   seq_lens : device int32 [batch], tokens cached
+ *   max_new  : host bound of seq_lens - old_lens (0 is a no-op); blocks beyond
+ *              what it says are not bounded and set the device error word
+ *   bounds   : device bf16, a minimum of r numbers and a maximum of r numbers per
+ *              block and kv head: [num_pages][h_kv][2][r] (paged) or
+ *              [batch][h_kv][capacity / block][2][r]; others are not written
+ * Quantised keys count as code * k_scale.  A bound is the nearest bf16 number on
+ * the outer side (bf16 keys: exact); an element that is NaN in a key is bounded
+ * by -infinity and +infinity.  Tokens past seq_lens take no part.  A block on a
+ * page that is out of range is not bounded.  Launched with programmatic
+ * dependent launch (see tk_attn_decode).                                     */
+tk_status tk_block_bounds(const tk_cache_desc* desc, int32_t block, const void* k_cache, const float* k_scale,
+                          const int32_t* page_table, const int32_t* old_lens, const int32_t* seq_lens,
+                          int32_t max_new, void* bounds, void* stream);
+
+/* For one query token per sequence: the n_select blocks of each kv head whose keys
+ * can score highest.  With a block's bounds lo, hi,
+ *   s_h = sum_i max(q_hi lo_i, q_hi hi_i) >= q_h . k   of each of its keys,
+ *   s   = max over the kv head's query heads h of s_h;
+ * the first n_first and the last n_last blocks of the context are always taken, the
+ * others by s, the larger first and, of equal ones, the earlier.  s is compared as
+ * computed in 64 bits; where a bound of the block or one of its s_h is infinite or
+ * NaN, s counts as +infinity.  A context of n_select blocks or fewer is taken whole.
+ *   q        : device bf16 [batch][h_q][r]
+ *   bounds   : as tk_block_bounds writes them
+ *   seq_lens : device int32 [batch], context length of each sequence
+ *   max_seq_len: host bound of seq_lens (a larger device value is clamped and
+ *              recorded); at most 24576 blocks
+ *   n_first >= 0, n_last >= 1, n_first + n_last <= n_select
+ *   table    : device int32 [batch][h_kv][n_select], for tk_attn_decode_blocks: block j
+ *              of the chosen ones, in order, is rows table * block .. of the cache
+ *              seen as rows of tokens (k_cache [..][r], v_cache [..][d_v]), i.e.
+ *              page * h_kv + kv head (paged) or (b * h_kv + kv head) * (capacity /
+ *              block) + block; -1 past the last one
+ *   lens     : device int32 [batch][h_kv], tokens in them (all blocks but the last
+ *              are full)
+ *   ids      : device int32 [batch][h_kv][n_select], the blocks' numbers in the
+ *              sequence (-1 past the last one), or NULL
+ * Launched with programmatic dependent launch.                               */
+tk_status tk_block_select(const tk_cache_desc* desc, int32_t block, const void* q, const void* bounds,
+                          const int32_t* page_table, const int32_t* seq_lens, int32_t max_seq_len,
+                          int32_t n_select, int32_t n_first, int32_t n_last, int32_t* table, int32_t* lens,
+                          int32_t* ids, void* stream);
+
+/* Bytes of workspace of tk_attn_decode_blocks (as tk_decode_workspace_size: on the
+ * current device, zero-filled once; 0 for invalid arguments).                */
+size_t tk_decode_blocks_workspace_size(const tk_cache_desc* desc, int32_t block, int32_t n_select);
+
+/* tk_attn_decode over chosen blocks: query head h of sequence b attends to the
+ * first lens[b][g] tokens of the blocks table[b][g] of its kv head g alone.
+ *   table, lens: as tk_block_select writes them, or the caller's own (any blocks
+ *              in any order, all but the last full; lens 0 gives a zero row)
+ *   workspace: tk_decode_blocks_workspace_size bytes, 256-byte aligned
+ *   The other arguments and errors are those of tk_attn_decode; a table entry
+ *   out of range sets the device error word.  One launch for every 1024 / h_kv
+ *   sequences.                                                               */
+tk_status tk_attn_decode_blocks(const tk_cache_desc* desc, int32_t block, const void* q, const void* k_cache,
+                                const void* v_cache, const float* k_scale, const int32_t* table,
+                                const int32_t* lens, int32_t n_select, void* out, int32_t out_dtype, float scale,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of tk_attn_weights on the current device; 0 for invalid
+ * arguments.  Scratch: reusable in stream order, never by two calls that may
+ * run concurrently.                                                         */
+size_t tk_attn_weights_workspace_size(const tk_cache_desc* desc, int32_t n_q, int32_t max_seq_len);
+
+/* Adds the attention weights of n_q queries per sequence up per cached token:
+ *   weights[b][g][t] = (t < old_lens[b] ? decay * weights[b][g][t] : 0)
+ *                      + sum over the kv head's query heads and the queries i of
+ *                        softmax over t' <= p_i of (scale q_hi . k_t')  at t
+ * for t < seq_lens[b]; query i is at position p_i = seq_lens[b] - n_q + i (its own
+ * token is cached), and one before the sequence's start counts for nothing.
+ *   q        : device bf16 [batch][h_q][n_q][r]; n_q * h_q / h_kv <= 512
+ *   k_cache, k_scale, page_table: the cache (values are not needed)
+ *   old_lens : device int32 [batch], tokens that have a weight from earlier steps, or
+ *              NULL = none
+ *   seq_lens : device int32 [batch]; max_seq_len: host bound of it (a larger
+ *              device value is clamped and recorded)
+ *   scale    : as in tk_attn_decode;  decay: finite (1 = plain sums; with 0
+ *              earlier weights are not read)
+ *   weights  : device fp32, one per slot, laid out as k_scale: [batch][h_kv][capacity] or
+ *              [num_pages][h_kv][page_size]; slots past seq_lens are not written
+ *   workspace: tk_attn_weights_workspace_size bytes, 256-byte aligned
+ * Sums in fp32, in an order fixed by the sizes and the device's SM count.  Two
+ * launches, with programmatic dependent launch.                              */
+tk_status tk_attn_weights(const tk_cache_desc* desc, const void* q, int32_t n_q, const void* k_cache,
+                          const float* k_scale, const int32_t* page_table, const int32_t* old_lens,
+                          const int32_t* seq_lens, int32_t max_seq_len, float scale, float decay, float* weights,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of tk_cache_evict; 0 for invalid arguments.  Scratch, as that
+ * of tk_attn_weights.                                                        */
+size_t tk_cache_evict_workspace_size(const tk_cache_desc* desc, int32_t n_keep);
+
+/* Cuts every context of more than n_keep tokens to n_keep, for each kv head by its
+ * own weights: the last n_recent tokens stay, and of the others the n_keep -
+ * n_recent with the largest weights (of equal ones the lower slots; NaN counts as
+ * the smallest).  The cache holds the kept tokens in slots 0 .. n_keep - 1 after
+ * it: the recent ones at the end, in order; the others stay where they are if their
+ * slot is below n_keep - n_recent, and else fill the free slots there, in order.
+ * (Attention does not depend on the order of cached tokens.)
+ *   k_cache, v_cache, k_scale: moved in place
+ *   seq_lens : device int32 [batch]; a negative one or one beyond the cache or
+ *              max_seq_len is recorded and the sequence left alone
+ *   max_seq_len: host bound of seq_lens
+ *   weights  : device fp32 per slot, as tk_attn_weights writes them
+ *   n_keep   : 1 .. 2^26;  n_recent: 0 .. n_keep
+ *   weights_out: the weights of the kept tokens, per slot; may be weights (slots
+ *              past the new length are not written).  Any other overlap is an
+ *              error that is not detected.
+ *   seq_lens_out: device int32 [batch], min(seq_lens, n_keep); may be seq_lens
+ *   kept     : device int32 [batch][h_kv][n_keep], the slot that each kept token
+ *              had before (-1 past the new length), or NULL
+ *   free_pages, free_count: paged: pages that hold no token any more are pushed
+ *              on this stack (see tk_block_tables), in order of sequence and
+ *              page, so that tk_block_tables finds a sequence's pages by its
+ *              new length; both NULL: the pages stay with the sequence
+ *   workspace: tk_cache_evict_workspace_size bytes, 256-byte aligned
+ * Two launches, with programmatic dependent launch.                          */
+tk_status tk_cache_evict(const tk_cache_desc* desc, void* k_cache, void* v_cache, float* k_scale,
+                         const int32_t* page_table, const int32_t* seq_lens, int32_t max_seq_len,
+                         const float* weights, int32_t n_keep, int32_t n_recent, float* weights_out,
+                         int32_t* seq_lens_out, int32_t* kept, int32_t* free_pages, int32_t* free_count,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
 /* Stream-ordered copy of `bytes` bytes between any two of device memory and
  * page-locked host memory (cudaMemcpyAsync with the direction taken from the
  * pointers), for serving loops that bring a step's inputs from the host:

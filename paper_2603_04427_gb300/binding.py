@@ -31,6 +31,9 @@ EXPORTED = ("tk_kv_append", "tk_attn_prefill", "tk_decode_workspace_size", "tk_a
             "tk_attn_forward", "tk_backward_workspace_size", "tk_attn_backward", "tk_copy_async",
             "tk_qk_norm_rope", "tk_qk_norm_rope_append", "tk_qk_norm_rope_backward",
             "tk_qk_norm_rope_workspace_size", "tk_block_tables",
+            "tk_block_bounds", "tk_block_select", "tk_attn_decode_blocks",
+            "tk_decode_blocks_workspace_size", "tk_attn_weights", "tk_attn_weights_workspace_size",
+            "tk_cache_evict", "tk_cache_evict_workspace_size",
             "tk_check_wait_timeout", "tk_get_device_error", "tk_status_string", "tk_last_error",
             "tk_abi_version", "tk_graph_begin", "tk_graph_end", "tk_graph_launch",
             "tk_graph_destroy")
@@ -102,6 +105,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                            hp, hp, hp, hp, hp, hp, vp, vp, vp, sz, vp]),
         "tk_block_tables": (i32, [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp,
                                   vp, vp, vp, vp]),
+        "tk_block_bounds": (i32, [dp, i32, vp, vp, vp, vp, vp, i32, vp, vp]),
+        "tk_block_select": (i32, [dp, i32, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]),
+        "tk_decode_blocks_workspace_size": (sz, [dp, i32, i32]),
+        "tk_attn_decode_blocks": (i32, [dp, i32, vp, vp, vp, vp, vp, vp, i32, vp, i32, f32, vp, sz, vp]),
+        "tk_attn_weights_workspace_size": (sz, [dp, i32, i32]),
+        "tk_attn_weights": (i32, [dp, vp, i32, vp, vp, vp, vp, vp, i32, f32, f32, vp, vp, sz, vp]),
+        "tk_cache_evict_workspace_size": (sz, [dp, i32]),
+        "tk_cache_evict": (i32, [dp, vp, vp, vp, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
         "tk_get_device_error": (i32, [ctypes.POINTER(i32), vp]),
         "tk_check_wait_timeout": (i32, [i32, vp]),
         "tk_copy_async": (i32, [vp, vp, sz, vp]),
@@ -819,6 +830,339 @@ def prepare_block_tables(pool: PagePool, new_lens, slots, positions, tokens_per_
     args, keep = _table_args(pool, new_lens, slots, positions, tokens_per_seq, offsets, seq_lens_out,
                              free_count_out, refused, stream)
     return PreparedCall("tk_block_tables", args, keep, graph=graph, stream=stream)
+
+
+# ------------------------------------------------------- a long context, read or kept in part
+
+def _lead(cache):
+    """The leading dimensions of a cache's tensors: [P, H_kv, page_size] or [B, H_kv, capacity]."""
+    d = cache.desc
+    return (d.num_pages, d.h_kv, d.page_size) if d.page_size else (d.batch, d.h_kv, d.capacity)
+
+
+def _cache_tensors(cache, device, keys=False, values=False):
+    """Checks the tensors of the cache that a call reads, and the current GPU."""
+    d = cache.desc
+    lead = _lead(cache)
+    if keys or values:
+        width = d.r // 2 if d.k_dtype == TK_I4 else d.r
+        key = {TK_BF16: torch.bfloat16, TK_I8: torch.int8, TK_I4: torch.uint8}.get(d.k_dtype)
+        want = [(cache.k, key, "cache.k", (*lead, width))]
+        if d.k_dtype != TK_BF16:
+            want.append((cache.k_scale, torch.float32, "cache.k_scale", lead))
+        if values:
+            want.append((cache.v, torch.bfloat16, "cache.v", (*lead, d.d_v)))
+        for t, dt, n, shape in want:
+            if t is None:
+                raise ValueError(f"{n} is None")
+            _need(t, dt, n, device)
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{n} is {tuple(t.shape)}, expected {shape}")
+    if d.page_size:
+        if cache.page_table is None:
+            raise ValueError("a paged cache needs a page table")
+        _need(cache.page_table, torch.int32, "cache.page_table", device)
+        if tuple(cache.page_table.shape) != (d.batch, d.max_pages_per_seq):
+            raise ValueError(f"cache.page_table is {tuple(cache.page_table.shape)}, expected "
+                             f"{(d.batch, d.max_pages_per_seq)}")
+    _need_current(device.index)
+
+
+def _need_shape(t, dtype, name, shape, device):
+    if t is None:
+        return
+    _need(t, dtype, name, device)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def _device(t, name):
+    if t is None or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    return t.device
+
+
+def _block(cache, block):
+    """Tokens of a block: the page of a paged cache, 64 by default of a contiguous one."""
+    d = cache.desc
+    return int(block) if block else (d.page_size or 64)
+
+
+def _check_block(cache, block):
+    d = cache.desc
+    if block < 16 or block > 256 or block & (block - 1):
+        raise ValueError(f"block {block} must be a power of two of 16 .. 256")
+    if (d.page_size or d.capacity) % block or (d.page_size and block != d.page_size):
+        raise ValueError(f"block {block} does not fit a cache of page size {d.page_size}, capacity {d.capacity}")
+
+
+def _bounds_shape(cache, block):
+    d = cache.desc
+    lead = (d.num_pages, d.h_kv) if d.page_size else (d.batch, d.h_kv, d.capacity // block)
+    return (*lead, 2, d.r)
+
+
+def block_bounds(cache: ThinKeyCache, block: int | None = None) -> torch.Tensor:
+    """Zeroed bounds of every block of the cache for tk_block_bounds: bf16
+    [P, H_kv, 2, r] (paged: a block is a page) or [B, H_kv, capacity / block, 2, r]."""
+    block = _block(cache, block)
+    _check_block(cache, block)
+    return torch.zeros(_bounds_shape(cache, block), dtype=torch.bfloat16, device=cache.k.device)
+
+
+def _bounds_args(cache, bounds, seq_lens, old_lens, max_new, block, stream):
+    d = cache.desc
+    dev = _device(bounds, "bounds")
+    block = _block(cache, block)
+    _check_block(cache, block)
+    _cache_tensors(cache, dev, keys=True)
+    _need_shape(bounds, torch.bfloat16, "bounds", _bounds_shape(cache, block), dev)
+    _need_shape(seq_lens, torch.int32, "seq_lens", (d.batch,), dev)
+    _need_shape(old_lens, torch.int32, "old_lens", (d.batch,), dev)
+    if max_new is None:
+        max_new = d.max_pages_per_seq * d.page_size if d.page_size else d.capacity
+    args = (ctypes.byref(d), block, _ptr(cache.k), _ptr(cache.k_scale), _ptr(cache.page_table), _ptr(old_lens),
+            _ptr(seq_lens), int(max_new), _ptr(bounds), _stream(stream))
+    return args, (cache, bounds, seq_lens, old_lens)
+
+
+def tk_block_bounds(cache: ThinKeyCache, bounds, seq_lens, old_lens=None, max_new: int | None = None,
+                    block: int | None = None, stream=None):
+    """Minimum and maximum of the keys of each block that holds a token at old_lens[b] ..
+    seq_lens[b] - 1 (int32 [B]; old_lens None: of every block), into bounds (see block_bounds).
+    max_new bounds seq_lens - old_lens (default: the whole cache)."""
+    args, _keep = _bounds_args(cache, bounds, seq_lens, old_lens, max_new, block, stream)
+    _check(load_library().tk_block_bounds(*args), "tk_block_bounds")
+    return bounds
+
+
+def prepare_block_bounds(cache: ThinKeyCache, bounds, seq_lens, old_lens=None, max_new: int | None = None,
+                         block: int | None = None, stream=None, graph: bool = False) -> PreparedCall:
+    """tk_block_bounds on fixed buffers, checked and marshalled once (see PreparedCall)."""
+    args, keep = _bounds_args(cache, bounds, seq_lens, old_lens, max_new, block, stream)
+    return PreparedCall("tk_block_bounds", args, keep, graph=graph, stream=stream)
+
+
+@dataclass
+class BlockSelection:
+    """The blocks that a decode step reads, per sequence and kv head.
+
+    block: tokens of a block.  table [B * H_kv, n_select] int32: each block's place in the cache
+    (page * H_kv + g, or (b * H_kv + g) * (capacity / block) + block; -1: none), lens
+    [B * H_kv] int32: tokens in them; ids [B, H_kv, n_select] int32 or None: the blocks' numbers
+    in their sequence."""
+    block: int
+    table: torch.Tensor
+    lens: torch.Tensor
+    ids: torch.Tensor | None = None
+
+    @staticmethod
+    def allocate(cache: ThinKeyCache, n_select: int, block: int | None = None, ids: bool = False):
+        """An empty selection (decoding over it gives zero rows)."""
+        d = cache.desc
+        i32 = dict(dtype=torch.int32, device=cache.k.device)
+        pairs = d.batch * d.h_kv
+        return BlockSelection(_block(cache, block), torch.full((pairs, n_select), -1, **i32),
+                              torch.zeros(pairs, **i32),
+                              torch.full((d.batch, d.h_kv, n_select), -1, **i32) if ids else None)
+
+
+def _need_selection(cache, sel, dev):
+    d = cache.desc
+    _check_block(cache, sel.block)
+    if sel.table.dim() != 2:
+        raise ValueError("selection.table must be [B * H_kv, n_select]")
+    n = sel.table.shape[1]
+    _need_shape(sel.table, torch.int32, "selection.table", (d.batch * d.h_kv, n), dev)
+    _need_shape(sel.lens, torch.int32, "selection.lens", (d.batch * d.h_kv,), dev)
+    _need_shape(sel.ids, torch.int32, "selection.ids", (d.batch, d.h_kv, n), dev)
+    return n
+
+
+def _select_args(cache, q, bounds, seq_lens, max_seq_len, sel, n_first, n_last, stream):
+    d = cache.desc
+    dev = _device(q, "q")
+    _cache_tensors(cache, dev)
+    n = _need_selection(cache, sel, dev)
+    _need_shape(q, torch.bfloat16, "q", (d.batch, d.h_q, d.r), dev)
+    _need_shape(bounds, torch.bfloat16, "bounds", _bounds_shape(cache, sel.block), dev)
+    _need_shape(seq_lens, torch.int32, "seq_lens", (d.batch,), dev)
+    args = (ctypes.byref(d), sel.block, _ptr(q), _ptr(bounds), _ptr(cache.page_table), _ptr(seq_lens),
+            int(max_seq_len), n, int(n_first), int(n_last), _ptr(sel.table), _ptr(sel.lens), _ptr(sel.ids),
+            _stream(stream))
+    return args, (cache, q, bounds, seq_lens, sel, sel.table, sel.lens, sel.ids)
+
+
+def tk_block_select(cache: ThinKeyCache, q, bounds, seq_lens, max_seq_len: int, selection: BlockSelection,
+                    n_first: int = 1, n_last: int = 1, stream=None):
+    """For q [B, H_q, r] bf16: the n_select blocks of each kv head whose keys can score highest by
+    their bounds, into `selection`; the first n_first and last n_last blocks of a context are
+    always among them."""
+    args, _keep = _select_args(cache, q, bounds, seq_lens, max_seq_len, selection, n_first, n_last, stream)
+    _check(load_library().tk_block_select(*args), "tk_block_select")
+    return selection
+
+
+def prepare_block_select(cache: ThinKeyCache, q, bounds, seq_lens, max_seq_len: int, selection: BlockSelection,
+                         n_first: int = 1, n_last: int = 1, stream=None, graph: bool = False) -> PreparedCall:
+    """tk_block_select on fixed buffers, checked and marshalled once (see PreparedCall)."""
+    args, keep = _select_args(cache, q, bounds, seq_lens, max_seq_len, selection, n_first, n_last, stream)
+    return PreparedCall("tk_block_select", args, keep, graph=graph, stream=stream)
+
+
+def decode_blocks_workspace(cache: ThinKeyCache, selection: BlockSelection) -> torch.Tensor:
+    """A zero-filled workspace of the size tk_attn_decode_blocks needs."""
+    dev = _device(selection.table, "selection.table")
+    _need_current(dev.index)
+    n = int(load_library().tk_decode_blocks_workspace_size(ctypes.byref(cache.desc), selection.block,
+                                                           selection.table.shape[1]))
+    if n == 0:
+        raise TkError(TK_ERR_INVALID_ARG, "tk_decode_blocks_workspace_size", tk_last_error())
+    return torch.zeros(n, dtype=torch.uint8, device=dev)
+
+
+def _decode_blocks_args(cache, q, sel, out, workspace, scale, stream):
+    d = cache.desc
+    dev = _device(q, "q")
+    _cache_tensors(cache, dev, values=True)
+    n = _need_selection(cache, sel, dev)
+    _need_shape(q, torch.bfloat16, "q", (d.batch, d.h_q, d.r), dev)
+    _need_out(out, "out", dev)
+    if tuple(out.shape) != (d.batch, d.h_q, d.d_v):
+        raise ValueError(f"out is {tuple(out.shape)}, expected {(d.batch, d.h_q, d.d_v)}")
+    _need(workspace, torch.uint8, "workspace", dev)
+    scale = 1.0 / math.sqrt(d.r) if scale is None else float(scale)
+    args = (ctypes.byref(d), sel.block, _ptr(q), _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_scale),
+            _ptr(sel.table), _ptr(sel.lens), n, _ptr(out), TK_F32 if out.dtype == torch.float32 else TK_BF16,
+            ctypes.c_float(scale), _ptr(workspace), ctypes.c_size_t(workspace.numel()), _stream(stream))
+    return args, (cache, q, sel, sel.table, sel.lens, out, workspace)
+
+
+def tk_attn_decode_blocks(cache: ThinKeyCache, q, selection: BlockSelection, out, workspace,
+                          scale: float | None = None, stream=None):
+    """tk_attn_decode of q [B, H_q, r] over the blocks of `selection` alone."""
+    args, _keep = _decode_blocks_args(cache, q, selection, out, workspace, scale, stream)
+    _check(load_library().tk_attn_decode_blocks(*args), "tk_attn_decode_blocks")
+    return out
+
+
+def prepare_attn_decode_blocks(cache: ThinKeyCache, q, selection: BlockSelection, out, workspace,
+                               scale: float | None = None, stream=None, graph: bool = False) -> PreparedCall:
+    """tk_attn_decode_blocks on fixed buffers, checked and marshalled once (see PreparedCall)."""
+    args, keep = _decode_blocks_args(cache, q, selection, out, workspace, scale, stream)
+    return PreparedCall("tk_attn_decode_blocks", args, keep, graph=graph, stream=stream)
+
+
+def slot_weights(cache: ThinKeyCache) -> torch.Tensor:
+    """Zeroed accumulated weights of every slot of the cache: fp32, laid out as k_scale."""
+    return torch.zeros(_lead(cache), dtype=torch.float32, device=cache.k.device)
+
+
+def attn_weights_workspace(cache: ThinKeyCache, max_seq_len: int, n_queries: int = 1) -> torch.Tensor:
+    """A workspace of the size tk_attn_weights needs."""
+    dev = _device(cache.k, "cache.k")
+    _need_current(dev.index)
+    n = int(load_library().tk_attn_weights_workspace_size(ctypes.byref(cache.desc), int(n_queries), int(max_seq_len)))
+    if n == 0:
+        raise TkError(TK_ERR_INVALID_ARG, "tk_attn_weights_workspace_size", tk_last_error())
+    return torch.empty(n, dtype=torch.uint8, device=dev)
+
+
+def _weights_args(cache, q, seq_lens, max_seq_len, weights, workspace, old_lens, decay, scale, stream):
+    d = cache.desc
+    dev = _device(q, "q")
+    _cache_tensors(cache, dev, keys=True)
+    if q.dim() == 3:
+        q = q.unsqueeze(2)
+    if q.dim() != 4:
+        raise ValueError(f"q is {tuple(q.shape)}, expected [B, H_q, r] or [B, H_q, n, r]")
+    n = q.shape[2]
+    _need_shape(q, torch.bfloat16, "q", (d.batch, d.h_q, n, d.r), dev)
+    _need_shape(seq_lens, torch.int32, "seq_lens", (d.batch,), dev)
+    _need_shape(old_lens, torch.int32, "old_lens", (d.batch,), dev)
+    _need_shape(weights, torch.float32, "weights", _lead(cache), dev)
+    _need(workspace, torch.uint8, "workspace", dev)
+    scale = 1.0 / math.sqrt(d.r) if scale is None else float(scale)
+    args = (ctypes.byref(d), _ptr(q), n, _ptr(cache.k), _ptr(cache.k_scale), _ptr(cache.page_table), _ptr(old_lens),
+            _ptr(seq_lens), int(max_seq_len), ctypes.c_float(scale), ctypes.c_float(decay), _ptr(weights),
+            _ptr(workspace), ctypes.c_size_t(workspace.numel()), _stream(stream))
+    return args, (cache, q, seq_lens, weights, workspace, old_lens)
+
+
+def tk_attn_weights(cache: ThinKeyCache, q, seq_lens, max_seq_len: int, weights, workspace, old_lens=None,
+                    decay: float = 1.0, scale: float | None = None, stream=None):
+    """Adds the attention weights of q [B, H_q, r] (or the last n queries, [B, H_q, n, r]) over the
+    cached tokens, their own included, to weights (slot_weights), summed over the query heads
+    of a kv head.  Tokens from old_lens[b] on (None: all) have no weight yet; the earlier ones'
+    is multiplied by decay first."""
+    args, _keep = _weights_args(cache, q, seq_lens, max_seq_len, weights, workspace, old_lens, decay, scale, stream)
+    _check(load_library().tk_attn_weights(*args), "tk_attn_weights")
+    return weights
+
+
+def prepare_attn_weights(cache: ThinKeyCache, q, seq_lens, max_seq_len: int, weights, workspace, old_lens=None,
+                         decay: float = 1.0, scale: float | None = None, stream=None,
+                         graph: bool = False) -> PreparedCall:
+    """tk_attn_weights on fixed buffers, checked and marshalled once (see PreparedCall).  With
+    graph=True preparing adds the weights once."""
+    args, keep = _weights_args(cache, q, seq_lens, max_seq_len, weights, workspace, old_lens, decay, scale, stream)
+    return PreparedCall("tk_attn_weights", args, keep, graph=graph, stream=stream)
+
+
+def cache_evict_workspace(cache: ThinKeyCache, n_keep: int) -> torch.Tensor:
+    """A workspace of the size tk_cache_evict needs."""
+    n = int(load_library().tk_cache_evict_workspace_size(ctypes.byref(cache.desc), int(n_keep)))
+    if n == 0:
+        raise TkError(TK_ERR_INVALID_ARG, "tk_cache_evict_workspace_size", tk_last_error())
+    return torch.empty(n, dtype=torch.uint8, device=cache.k.device)
+
+
+def _evict_args(cache, seq_lens, max_seq_len, weights, n_keep, n_recent, workspace, weights_out, seq_lens_out, kept,
+                pool, stream):
+    d = cache.desc
+    dev = _device(weights, "weights")
+    _cache_tensors(cache, dev, values=True)
+    weights_out = weights if weights_out is None else weights_out
+    seq_lens_out = seq_lens if seq_lens_out is None else seq_lens_out
+    _need_shape(seq_lens, torch.int32, "seq_lens", (d.batch,), dev)
+    _need_shape(seq_lens_out, torch.int32, "seq_lens_out", (d.batch,), dev)
+    _need_shape(weights, torch.float32, "weights", _lead(cache), dev)
+    _need_shape(weights_out, torch.float32, "weights_out", _lead(cache), dev)
+    _need_shape(kept, torch.int32, "kept", (d.batch, d.h_kv, n_keep), dev)
+    _need(workspace, torch.uint8, "workspace", dev)
+    free = count = None
+    if pool is not None:
+        free, count = pool.free_pages, pool.free_count
+        _need_shape(free, torch.int32, "free_pages", (d.num_pages,), dev)
+        _need_shape(count, torch.int32, "free_count", (1,), dev)
+        if cache.page_table is None or pool.page_table.data_ptr() != cache.page_table.data_ptr():
+            raise ValueError("the pool's page table is not the cache's")
+    args = (ctypes.byref(d), _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_scale), _ptr(cache.page_table),
+            _ptr(seq_lens), int(max_seq_len), _ptr(weights), int(n_keep), int(n_recent), _ptr(weights_out),
+            _ptr(seq_lens_out), _ptr(kept), _ptr(free), _ptr(count), _ptr(workspace),
+            ctypes.c_size_t(workspace.numel()), _stream(stream))
+    return args, (cache, seq_lens, weights, workspace, weights_out, seq_lens_out, kept, pool, free, count)
+
+
+def tk_cache_evict(cache: ThinKeyCache, seq_lens, max_seq_len: int, weights, n_keep: int, n_recent: int, workspace,
+                   weights_out=None, seq_lens_out=None, kept=None, pool: PagePool | None = None, stream=None):
+    """Cuts contexts of more than n_keep tokens to the last n_recent and the n_keep - n_recent others
+    with the largest weights of each kv head, moved into slots 0 .. n_keep - 1 of the cache.
+    weights and seq_lens are updated in place unless outputs are given; kept [B, H_kv, n_keep] int32
+    tells where each token was; pool (a PagePool of this cache) gets the pages back that
+    hold no token any more.  See include/tk.h."""
+    args, _keep = _evict_args(cache, seq_lens, max_seq_len, weights, n_keep, n_recent, workspace, weights_out,
+                              seq_lens_out, kept, pool, stream)
+    _check(load_library().tk_cache_evict(*args), "tk_cache_evict")
+
+
+def prepare_cache_evict(cache: ThinKeyCache, seq_lens, max_seq_len: int, weights, n_keep: int, n_recent: int,
+                        workspace, weights_out=None, seq_lens_out=None, kept=None, pool: PagePool | None = None,
+                        stream=None, graph: bool = False) -> PreparedCall:
+    """tk_cache_evict on fixed buffers, checked and marshalled once (see PreparedCall)."""
+    args, keep = _evict_args(cache, seq_lens, max_seq_len, weights, n_keep, n_recent, workspace, weights_out,
+                             seq_lens_out, kept, pool, stream)
+    return PreparedCall("tk_cache_evict", args, keep, graph=graph, stream=stream)
 
 
 def tk_attn_prefill(q, k, v, out, scale: float | None = None, causal: bool = True, stream=None):

@@ -1,0 +1,396 @@
+// Choice of the key blocks that a decode step reads: for each (sequence, kv
+// head) the n_select blocks whose keys can score highest with the step's queries,
+// out of the bounds of block_bounds.cu.
+//
+//   s_h(blk) = sum_i max(q_hi lo_i, q_hi hi_i)      >= q_h . k of each key in blk
+//   s(blk)   = max over the kv head's query heads of s_h(blk)
+//
+// With q split by sign this is one product of length 2 r, [lo | hi] . [q- | q+],
+// done by mma.sync.m16n8k16 with 16 blocks as rows and the query heads as columns
+// (bf16 operands as they are stored, fp32 accumulation; tcgen05's 128-column tiles
+// would be empty but for a few heads, and the operand comes straight from global
+// memory into registers).  Bound by the bounds' bytes for long contexts, by
+// latency for a few hundred blocks.
+//
+// The order that decides is that of the scores in 64 bits.  A score of the
+// tensor cores is off by at most eps = gamma sum|q||b|, gamma = (steps + 1) * 17 *
+// 2^-23: a step adds 16 exact products to the accumulator, and each of the 17
+// terms loses at most 2^-23 of the largest.  So with T the n-th largest of these
+// scores, blocks above T + 2 eps are in, below T - 2 eps they are out, and only those
+// between are scored again in 64 bits (usually T's own block alone: nothing is).
+//
+// A cluster of blocks of threads serves one (sequence, kv head): each scores its
+// part of the context and stores the scores into the first one's shared memory
+// (through the cluster, no global memory, no state between calls), which finds the
+// n-th largest by 8-bit digits and writes the chosen blocks in order.
+#include <algorithm>
+
+#include "key_frag.cuh"
+#include "kernels.h"
+
+namespace tk {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kMaxCluster = 8;
+// Key of the blocks that are chosen whatever their score; above +inf's.
+constexpr uint32_t kForced = 0xffffffffu;
+
+// Order-preserving encodings (-0 as +0).
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t k) {
+  return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k);
+}
+__device__ __forceinline__ uint64_t key_of(double x) {
+  const uint64_t u = static_cast<uint64_t>(__double_as_longlong(x + 0.0));
+  return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+// Address of the first block's copy of a shared variable.
+__device__ __forceinline__ uint32_t in_first(const void* p) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_addr(p)));
+  return a;
+}
+__device__ __forceinline__ void store_cluster(uint32_t addr, uint64_t v) {
+  asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+
+struct Shared {
+  uint32_t hist[256];
+  float amax[kMaxCluster];   // largest |bound| of each block of threads' part
+  int warp[kWarps][2];
+  int digit, above;
+  int in, cand;
+};
+
+// The n-th largest (n >= 1) of `count` keys: its value, and how many are larger.
+// Digits of 8 bits from the top; only keys that `use` accepts count.  All threads.
+template <typename Key, typename Get>
+__device__ __forceinline__ Key nth_largest(Shared& sh, int count, int n, Get get, int* larger) {
+  const int tid = threadIdx.x;
+  Key prefix = 0;
+  int above = 0;
+  for (int shift = static_cast<int>(sizeof(Key)) * 8 - 8; shift >= 0; shift -= 8) {
+    sh.hist[tid] = 0;        // kThreads bins
+    __syncthreads();
+    for (int i = tid; i < count; i += kThreads) {
+      Key k;
+      // the digits above this one agree with the prefix (a shift by the full width is not defined)
+      if (get(i, &k) && ((k ^ prefix) >> shift) < 256) atomicAdd(&sh.hist[(k >> shift) & 255], 1u);
+    }
+    __syncthreads();
+    if (tid < 32) {          // eight bins a lane, from the top
+      uint32_t c[8], sum = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c[j] = sh.hist[255 - (tid * 8 + j)], sum += c[j];
+      uint32_t inc = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (tid >= o) inc += y;
+      }
+      uint32_t before = above + inc - sum;
+      if (before < static_cast<uint32_t>(n) && above + inc >= static_cast<uint32_t>(n)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (before < static_cast<uint32_t>(n) && before + c[j] >= static_cast<uint32_t>(n))
+            sh.digit = 255 - (tid * 8 + j), sh.above = static_cast<int>(before);
+          before += c[j];
+        }
+      }
+    }
+    __syncthreads();
+    prefix |= static_cast<Key>(sh.digit) << shift;
+    above = sh.above;
+  }
+  *larger = above;
+  return prefix;
+}
+
+// Row of a block's bounds.
+__device__ __forceinline__ long long bounds_row(const SelectParams& p, int b, int g, int blk) {
+  return slot_row(p.at, b, g, blk << p.block_shift) >> p.block_shift;
+}
+
+// s(blk) in 64 bits, elements in order (each thread a block); +inf where a bound
+// or a query head's score is not finite.
+template <int R>
+__device__ double score64(const SelectParams& p, int b, int g, int blk) {
+  const __nv_bfloat16* box = static_cast<const __nv_bfloat16*>(p.bounds) + bounds_row(p, b, g, blk) * 2 * R;
+  const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + (static_cast<long long>(b) * p.at.Hkv + g) * p.G * R;
+  double best = -INFINITY;
+  bool odd = false;
+  for (int h = 0; h < p.G; ++h) {
+    double s = 0;
+    for (int i = 0; i < R; ++i) {
+      const float lo = __bfloat162float(box[i]), hi = __bfloat162float(box[R + i]);
+      odd |= !isfinite(lo) || !isfinite(hi);
+      const float x = __bfloat162float(q[h * R + i]);
+      s += static_cast<double>(x) * (x < 0 ? lo : hi);
+    }
+    best = fmax(best, s);
+    odd |= !isfinite(s);
+  }
+  return odd ? INFINITY : best;
+}
+
+template <int R>
+__global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_constant__ SelectParams p) {
+  constexpr int STEPS = 2 * R / 16;            // of the product of length 2 R
+  constexpr int LOADS = STEPS / 2;             // 16-byte loads of a lane and row
+  constexpr float kGamma = (STEPS + 1) * 17 * 0x1p-23f;
+  extern __shared__ uint64_t keys[];           // [max_blocks] of the first block of the cluster
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_rank(), parts = cluster_size();
+  const long long pair = blockIdx.x / parts;
+  const int b = static_cast<int>(pair / p.at.Hkv), g = static_cast<int>(pair % p.at.Hkv);
+  // the other blocks' shared memory may be written once they run
+  cluster_arrive();
+  pdl_wait();
+  const int L = checked_len(p.seq_lens[b], p.at);
+  const int n_blocks = (L + p.block - 1) >> p.block_shift;
+  const int n_take = min(p.n_select, n_blocks);
+  const bool all = n_take == n_blocks;         // uniform over the cluster
+  cluster_wait();
+
+  const int gq = lane >> 2, tq = lane & 3;
+  float q1 = 0.f;                              // sum |q| of one of the kv head's query heads
+  if (!all) {
+    // Q as the B operand: chunk c = tq + 4 j of 8 elements is steps 2j, 2j + 1; the
+    // first R of the 2 R elements meet lo with min(q, 0), the others hi with max(q, 0)
+    uint32_t qf[STEPS][2];
+    const uint32_t* qrow = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(p.q) +
+                                                             (pair * p.G + gq) * R);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int e = (tq + 4 * j) * 8;          // element of [lo | hi]
+      const bool up = e >= R;
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (gq < p.G) x = __ldg(reinterpret_cast<const uint4*>(qrow + (up ? e - R : e) / 2));
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (up) q1 += fabsf(bf16lo(w[i])) + fabsf(bf16hi(w[i]));
+        uint32_t keep = 0;                     // halves of the wanted sign
+        if ((w[i] >> 15 & 1) != up) keep |= 0xffffu;
+        if ((w[i] >> 31) != up) keep |= 0xffff0000u;
+        qf[2 * j + (i >> 1)][i & 1] = w[i] & keep;
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) q1 += __shfl_xor_sync(0xffffffffu, q1, o);
+    if (isnan(q1)) q1 = INFINITY;
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) q1 = fmaxf(q1, __shfl_xor_sync(0xffffffffu, q1, o));
+
+    // this block's part, 16 blocks of keys a warp at a time
+    const int per = ((n_blocks + 15) / 16 + parts - 1) / parts * 16;
+    const int from = min(static_cast<int>(rank) * per, n_blocks), to = min(from + per, n_blocks);
+    const uint32_t first_keys = in_first(keys);
+    uint32_t bmax = 0;                         // bf16 pair, largest magnitudes
+    for (int t0 = from + warp * 16; t0 < to; t0 += kWarps * 16) {
+      const int ra = min(t0 + gq, to - 1), rb = min(t0 + gq + 8, to - 1);
+      const uint4* pa = reinterpret_cast<const uint4*>(p.bounds) + bounds_row(p, b, g, ra) * (R / 4) + tq;
+      const uint4* pb = reinterpret_cast<const uint4*>(p.bounds) + bounds_row(p, b, g, rb) * (R / 4) + tq;
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      uint4 xa[LOADS], xb[LOADS];
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) xa[j] = __ldg(pa + 4 * j), xb[j] = __ldg(pb + 4 * j);
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) {
+        mma_bf16(s, xa[j].x, xb[j].x, xa[j].y, xb[j].y, qf[2 * j][0], qf[2 * j][1]);
+        mma_bf16(s, xa[j].z, xb[j].z, xa[j].w, xb[j].w, qf[2 * j + 1][0], qf[2 * j + 1][1]);
+        auto seen = [&](uint32_t x) { asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(bmax) : "r"(x & 0x7fff7fffu)); };
+        seen(xa[j].x); seen(xa[j].y); seen(xa[j].z); seen(xa[j].w);
+        seen(xb[j].x); seen(xb[j].y); seen(xb[j].z); seen(xb[j].w);
+      }
+      float a = -INFINITY, c = -INFINITY;      // blocks gq, gq + 8: largest of this lane's heads
+      if (2 * tq < p.G) a = s[0], c = s[2];
+      if (2 * tq + 1 < p.G) a = fmaxf(a, s[1]), c = fmaxf(c, s[3]);
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+        c = fmaxf(c, __shfl_xor_sync(0xffffffffu, c, o));
+      }
+      if (tq < 2) {
+        const int blk = t0 + gq + 8 * tq;
+        const bool forced = blk < p.n_first || blk >= n_blocks - p.n_last;
+        const uint32_t k = forced ? kForced : key_of(tq ? c : a);
+        if (blk < to) store_cluster(first_keys + blk * 8, static_cast<uint64_t>(k) << 32);
+      }
+    }
+    const float b0 = bf16lo(bmax), b1 = bf16hi(bmax);
+    float big = isnan(b0) || isnan(b1) ? INFINITY : fmaxf(b0, b1);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+    if (lane == 0) sh.warp[warp][0] = __float_as_int(big);
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < kWarps; ++w) big = fmaxf(big, __int_as_float(sh.warp[w][0]));
+      asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_first(&sh.amax[rank])), "r"(__float_as_int(big)) : "memory");
+    }
+  }
+  cluster_arrive();
+  cluster_wait();
+  if (rank != 0) return;
+
+  int32_t* table = p.table + pair * p.n_select;
+  int32_t* ids = p.ids ? p.ids + pair * p.n_select : nullptr;
+  uint64_t edge = 0;         // chosen: keys above edge, and the first `ties` that equal it
+  int ties = 0;
+  if (!all) {
+    int larger;
+    const uint32_t top = nth_largest<uint32_t>(sh, n_blocks, n_take, [&](int i, uint32_t* k) {
+      *k = static_cast<uint32_t>(keys[i] >> 32);
+      return true;
+    }, &larger);
+    float eps = 0.f;
+    if (top != kForced) {
+      float big = 0.f;
+      for (uint32_t r = 0; r < parts; ++r) big = fmaxf(big, sh.amax[r]);
+      // nothing is rounded where one factor is zero; elsewhere operands and products
+      // below the normal range may be taken for zero
+      if (big != 0.f && q1 != 0.f) eps = big * q1 * kGamma + (big + q1) * 0x1p-120f + 0x1p-100f;
+      if (isnan(eps)) eps = INFINITY;
+    }
+    edge = static_cast<uint64_t>(top) << 32;
+    ties = n_take - larger;
+    if (eps != 0.f) {
+      // blocks that the 32-bit scores do not decide
+      const float t = value_of(top);
+      const bool open = !(eps < 0x1p100f) || !isfinite(t);
+      const uint32_t hi = open ? kForced - 1 : key_of(t + 2.f * eps), lo = open ? 0u : key_of(t - 2.f * eps);
+      if (tid == 0) sh.in = 0, sh.cand = 0;
+      __syncthreads();
+      int in = 0, cand = 0;
+      for (int i = tid; i < n_blocks; i += kThreads) {
+        const uint32_t k = static_cast<uint32_t>(keys[i] >> 32);
+        in += k > hi;
+        cand += k <= hi && k >= lo;
+      }
+      in = __reduce_add_sync(0xffffffffu, in);
+      cand = __reduce_add_sync(0xffffffffu, cand);
+      if (lane == 0) atomicAdd(&sh.in, in), atomicAdd(&sh.cand, cand);
+      __syncthreads();
+      in = sh.in;
+      cand = sh.cand;
+      if (in + cand == n_take) {
+        edge = static_cast<uint64_t>(lo) << 32;
+        ties = n_take;       // all that equal it
+      } else {
+        for (int i = tid; i < n_blocks; i += kThreads) {
+          const uint32_t k = static_cast<uint32_t>(keys[i] >> 32);
+          if (k > hi) keys[i] = ~0ull;
+          else if (k < lo) keys[i] = 0;
+          else keys[i] = key_of(score64<R>(p, b, g, i));
+        }
+        __syncthreads();
+        int more;
+        edge = nth_largest<uint64_t>(sh, n_blocks, n_take, [&](int i, uint64_t* k) {
+          *k = keys[i];
+          return true;
+        }, &more);
+        ties = n_take - more;
+      }
+    }
+  }
+
+  // the chosen blocks in order: a run of them for each warp, counted, then written
+  const int run = ((n_blocks + 31) / 32 + kWarps - 1) / kWarps * 32;
+  const int r0 = min(warp * run, n_blocks), r1 = min(r0 + run, n_blocks);
+  int over = 0, same = 0;
+  for (int i0 = r0; i0 < r1; i0 += 32) {
+    const int i = i0 + lane;
+    const bool here = i < r1;
+    over += __popc(__ballot_sync(0xffffffffu, here && !all && keys[here ? i : 0] > edge));
+    same += __popc(__ballot_sync(0xffffffffu, here && !all && keys[here ? i : 0] == edge));
+  }
+  if (lane == 0) sh.warp[warp][0] = over, sh.warp[warp][1] = same;
+  __syncthreads();
+  int before_over = 0, before_same = 0;
+  for (int w = 0; w < warp; ++w) before_over += sh.warp[w][0], before_same += sh.warp[w][1];
+  const uint32_t below = (1u << lane) - 1;
+  for (int i0 = r0; i0 < r1; i0 += 32) {
+    const int i = i0 + lane;
+    const bool here = i < r1;
+    const bool gt = here && !all && keys[here ? i : 0] > edge, eq = here && !all && keys[here ? i : 0] == edge;
+    const uint32_t mgt = __ballot_sync(0xffffffffu, gt), meq = __ballot_sync(0xffffffffu, eq);
+    const int ngt = before_over + __popc(mgt & below), neq = before_same + __popc(meq & below);
+    const bool take = here && (all || gt || (eq && neq < ties));
+    if (take) {
+      const int at = all ? i : ngt + min(neq, ties);
+      table[at] = static_cast<int32_t>(bounds_row(p, b, g, i));
+      if (ids) ids[at] = i;
+    }
+    before_over += __popc(mgt);
+    before_same += __popc(meq);
+  }
+  for (int i = n_take + tid; i < p.n_select; i += kThreads) {
+    table[i] = -1;
+    if (ids) ids[i] = -1;
+  }
+  if (tid == 0) p.lens[pair] = n_blocks == 0 ? 0 : ((n_take - 1) << p.block_shift) + L - ((n_blocks - 1) << p.block_shift);
+}
+
+template <int R>
+cudaError_t launch_t(const SelectParams& p, cudaStream_t s) {
+  auto kern = block_select_kernel<R>;
+  const long long pairs = static_cast<long long>(p.B) * p.at.Hkv;
+  // one block of threads for every 512 blocks of keys, as long as two fit an SM
+  int parts = 1;
+  while (parts < kMaxCluster && p.max_blocks > parts * 512 && pairs * parts < 2ll * p.num_sms) parts *= 2;
+  const size_t smem = static_cast<size_t>(std::max(p.max_blocks, 1)) * 8;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSelectBlocks * 8);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(pairs * parts));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(parts);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, p);
+}
+
+}  // namespace
+
+cudaError_t launch_block_select(const SelectParams& p, cudaStream_t s, int* unsupported) {
+  switch (p.R) {
+    case 16: return launch_t<16>(p, s);
+    case 32: return launch_t<32>(p, s);
+    case 64: return launch_t<64>(p, s);
+    case 128: return launch_t<128>(p, s);
+  }
+  *unsupported = 1;
+  return cudaSuccess;
+}
+
+}  // namespace tk

@@ -1,0 +1,452 @@
+// Eviction: of a context of L > keep tokens, per (sequence, kv head), the last
+// `recent` stay, and of the others the keep - recent with the largest accumulated
+// weights (attn_weights.cu), ties to the lower slot.  The cache holds them in its
+// first `keep` slots afterwards:
+//
+//   slots 0 .. keep - recent - 1: kept tokens that were there stay where they are; the
+//       others, in order of their slots, go to the free ones ("holes"), in order;
+//   slots keep - recent .. keep - 1: the recent tokens, in order.
+//
+// Attention does not ask for an order of the keys (they are rotated before they
+// are cached), so only holes are filled: 384 rows move where 256 of 4352 tokens go,
+// instead of the 4096 that an order of all tokens would move.  The recent ones keep
+// theirs, which is what says that they are recent at the next eviction.
+//
+// First launch, a cluster per (sequence, kv head): the keep - recent-th largest weight
+// by 8-bit digits, the digits' histograms joined through the cluster; then two
+// passes in slot order that count and write the lists of holes and of tokens to
+// move.  Second launch: the moves.  Every destination is below keep.  Tokens from
+// slot keep on are overwritten by nobody and move in any order, by many blocks.
+// Tokens to move from [keep - recent, keep) and the recent ones move by one block, in
+// rounds that load before they store and in order of slots: a recent token's
+// destination is below its slot, so what a round overwrites was loaded by it or
+// before it.
+//
+// Bound by latency for a few hundred rows, by HBM when a prompt is cut.
+#include <algorithm>
+
+#include "key_frag.cuh"
+#include "kernels.h"
+
+namespace tk {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kHeld = 16384;              // weights of a block that shared memory holds
+
+// Order-preserving encoding; -0 as +0, NaN as the smallest.
+__device__ __forceinline__ uint32_t key_of(float x) {
+  if (isnan(x)) return 0;
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+// A shared variable of block `rank` of the cluster.
+__device__ __forceinline__ uint32_t load_of(const void* p, uint32_t rank) {
+  uint32_t a, v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+
+struct Shared {
+  uint32_t hist[2][256];
+  uint32_t total[256];
+  int digit, above;
+  int equal;                               // weights that equal the border's, of the block
+  int count[2];                            // holes, tokens to move, of the block
+  int warp[kWarps][2];
+};
+
+__global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_constant__ EvictParams p) {
+  extern __shared__ uint32_t held[];       // [min(part, kHeld)]
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_rank(), parts = cluster_size();
+  const long long pair = blockIdx.x / parts;
+  const int b = static_cast<int>(pair / p.at.Hkv), g = static_cast<int>(pair % p.at.Hkv);
+  pdl_wait();
+  pdl_trigger();
+  const int raw = p.seq_lens[b];
+  const bool valid = raw >= 0 && raw <= p.at.limit;
+  if (!valid && tid == 0 && rank == 0) record_error(p.at.err, TK_DEVERR_INDEX);
+  const int L = valid ? raw : 0;
+  int32_t* kept = p.kept ? p.kept + pair * p.keep : nullptr;
+  const int stride = static_cast<int>(parts) * kThreads, first = static_cast<int>(rank) * kThreads + tid;
+  if (L <= p.keep) {                       // everything stays (the whole cluster agrees)
+    if (rank == 0 && tid == 0) p.head[pair] = make_int4(raw, 0, 0, 0);
+    for (int i = first; i < p.keep; i += stride) {
+      if (kept) kept[i] = i < L ? i : -1;
+      if (i < L && p.w_out != p.w) {
+        const long long at = slot_row_or_none(p.at, b, g, i);
+        if (at >= 0) p.w_out[at] = p.w[at];
+      }
+    }
+    return;
+  }
+  const int n = L - p.recent;              // tokens that may go
+  const int want = p.keep - p.recent;      // of them stay
+  // this block's part of them, in whole warps' runs
+  const int part = ((n + static_cast<int>(parts) - 1) / static_cast<int>(parts) + 31) / 32 * 32;
+  const int from = min(static_cast<int>(rank) * part, n), to = min(from + part, n);
+  auto weight = [&](int t) { return key_of(__ldg(p.w + slot_row(p.at, b, g, t))); };
+  for (int i = tid; i < min(to - from, kHeld); i += kThreads) held[i] = weight(from + i);
+  auto key = [&](int t) { return t - from < kHeld ? held[t - from] : weight(t); };
+
+  // the want-th largest
+  uint32_t edge = 0;
+  int above = 0;
+  if (want > 0) {
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      uint32_t* hist = sh.hist[(shift >> 3) & 1];
+      if (tid < 256) hist[tid] = 0;
+      __syncthreads();
+      for (int t = from + tid; t < to; t += kThreads) {
+        const uint32_t k = key(t);
+        if ((k ^ edge) >> shift < 256) atomicAdd(&hist[(k >> shift) & 255], 1u);
+      }
+      cluster_sync();                      // this digit's histograms are complete
+      if (tid < 256) {
+        uint32_t c = 0;
+        for (uint32_t r = 0; r < parts; ++r) c += load_of(&hist[tid], r);
+        sh.total[tid] = c;
+      }
+      __syncthreads();
+      if (tid < 32) {                      // eight bins a lane, from the top
+        uint32_t c[8], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c[j] = sh.total[255 - (tid * 8 + j)], sum += c[j];
+        uint32_t inc = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
+          if (tid >= o) inc += y;
+        }
+        uint32_t before = above + inc - sum;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (before < static_cast<uint32_t>(want) && before + c[j] >= static_cast<uint32_t>(want))
+            sh.digit = 255 - (tid * 8 + j), sh.above = static_cast<int>(before);
+          before += c[j];
+        }
+      }
+      __syncthreads();
+      edge |= static_cast<uint32_t>(sh.digit) << shift;
+      above = sh.above;
+      // the other histogram is next: nobody reads it, since all have passed the
+      // barrier of this one
+    }
+  }
+  const int ties = want - above;           // of the weights at the border, the first ones stay
+
+  // runs of whole warps in order
+  const int run = ((to - from + 31) / 32 + kWarps - 1) / kWarps * 32;
+  const int r0 = min(from + warp * run, to), r1 = min(r0 + run, to);
+  const uint32_t below = (1u << lane) - 1;
+  auto equal = [&](int t) { return t < r1 && want > 0 && key(t) == edge; };
+  int same = 0;
+  for (int t0 = r0; t0 < r1; t0 += 32) same += __popc(__ballot_sync(0xffffffffu, equal(t0 + lane)));
+  if (lane == 0) sh.warp[warp][0] = same;
+  __syncthreads();
+  int same_before = 0;
+  for (int w = 0; w < warp; ++w) same_before += sh.warp[w][0];
+  if (warp == kWarps - 1 && lane == 0) sh.equal = same_before + same;
+  cluster_sync();
+  for (uint32_t r = 0; r < rank; ++r) same_before += static_cast<int>(load_of(&sh.equal, r));
+  // holes and tokens to move: counted, then written
+  const int same0 = same_before;
+  int holes = 0, moves = 0;
+  auto classify = [&](int t0, uint32_t* hole, uint32_t* move, uint32_t* stay) {
+    const int t = t0 + lane;
+    const bool here = t < r1;
+    const uint32_t k = here ? key(t) : 0u;
+    const bool eq = here && want > 0 && k == edge;
+    const uint32_t meq = __ballot_sync(0xffffffffu, eq);
+    const bool in = here && want > 0 && (k > edge || (eq && same_before + __popc(meq & below) < ties));
+    same_before += __popc(meq);
+    *hole = __ballot_sync(0xffffffffu, here && t < want && !in);
+    *move = __ballot_sync(0xffffffffu, t >= want && in);
+    *stay = __ballot_sync(0xffffffffu, here && t < want && in);
+  };
+  for (int t0 = r0; t0 < r1; t0 += 32) {
+    uint32_t h, m, s;
+    classify(t0, &h, &m, &s);
+    holes += __popc(h);
+    moves += __popc(m);
+  }
+  __syncthreads();                         // the counts of equal weights are read
+  if (lane == 0) sh.warp[warp][0] = holes, sh.warp[warp][1] = moves;
+  __syncthreads();
+  int h_at = 0, m_at = 0;
+  for (int w = 0; w < warp; ++w) h_at += sh.warp[w][0], m_at += sh.warp[w][1];
+  if (warp == kWarps - 1 && lane == 0) sh.count[0] = h_at + holes, sh.count[1] = m_at + moves;
+  cluster_sync();
+  int total = 0;
+  for (uint32_t r = 0; r < parts; ++r) {
+    const int h = static_cast<int>(load_of(&sh.count[0], r)), m = static_cast<int>(load_of(&sh.count[1], r));
+    if (r < rank) h_at += h, m_at += m;
+    total += m;
+  }
+  same_before = same0;
+  int32_t* hole = p.hole + pair * p.keep;
+  int32_t* src = p.src + pair * p.keep;
+  for (int t0 = r0; t0 < r1; t0 += 32) {
+    uint32_t h, m, s;
+    classify(t0, &h, &m, &s);
+    const int t = t0 + lane;
+    if (h >> lane & 1) hole[h_at + __popc(h & below)] = t;
+    if (m >> lane & 1) src[m_at + __popc(m & below)] = t;
+    if (s >> lane & 1) {
+      if (kept) kept[t] = t;
+      if (p.w_out != p.w) {
+        const long long at = slot_row_or_none(p.at, b, g, t);
+        if (at >= 0) p.w_out[at] = p.w[at];
+      }
+    }
+    h_at += __popc(h);
+    m_at += __popc(m);
+  }
+  if (kept)
+    for (int i = first; i < p.recent; i += stride) kept[want + i] = n + i;
+  if (rank == 0 && tid == 0) p.head[pair] = make_int4(raw, total, 0, 0);
+  cluster_sync();                          // nobody's shared memory goes while others read it
+}
+
+// ---------------------------------------------------------------- the moves
+constexpr int kMoveThreads = 256;
+constexpr int kInFlight = 8;
+
+// One kind of a token's data: `lanes` 16-byte pieces (or one 4-byte value) a row.
+struct Kind {
+  const unsigned char* from;
+  unsigned char* to;
+  int shift;                               // log2 of the pieces of a row
+  int word;                                // a 4-byte value instead
+};
+
+__device__ __forceinline__ uint4 load_piece(const Kind& k, long long row, int c) {
+  if (k.word) return make_uint4(*reinterpret_cast<const uint32_t*>(k.from + row * 4), 0, 0, 0);
+  return *reinterpret_cast<const uint4*>(k.from + ((row << k.shift) + c) * 16);
+}
+__device__ __forceinline__ void store_piece(const Kind& k, long long row, int c, uint4 x) {
+  if (k.word) *reinterpret_cast<uint32_t*>(k.to + row * 4) = x.x;
+  else *reinterpret_cast<uint4*>(k.to + ((row << k.shift) + c) * 16) = x;
+}
+
+__device__ __forceinline__ Kind kind_of(const EvictParams& p, int i) {
+  const int kb = p.k_fmt == 0 ? 2 * p.R : (p.k_fmt == 1 ? p.R : p.R / 2);
+  Kind k{};
+  if (i == 0) {
+    k.from = k.to = static_cast<unsigned char*>(p.v);
+    k.shift = p.DV == 64 ? 3 : 4;
+  } else if (i == 1) {
+    k.from = k.to = static_cast<unsigned char*>(p.k);
+    k.shift = 31 - __clz(kb / 16);
+  } else if (i == 2) {
+    k.from = reinterpret_cast<const unsigned char*>(p.w);
+    k.to = reinterpret_cast<unsigned char*>(p.w_out);
+    k.word = 1;
+  } else {
+    k.from = k.to = reinterpret_cast<unsigned char*>(p.k_scale);
+    k.word = 1;
+  }
+  return k;
+}
+
+// Pushes the pages of evicted tokens back, in order of sequence and page, and
+// writes the lengths.  One block.
+__device__ void finish(const EvictParams& p) {
+  __shared__ int warp_sum[kMoveThreads / 32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int ps = p.at.page_size;
+  long long top = 0;
+  if (p.free_pages) {
+    top = *p.free_count;
+    if (top < 0 || top > p.at.num_pages) {
+      if (tid == 0) record_error(p.at.err, TK_DEVERR_INDEX);
+      top = top < 0 ? 0 : p.at.num_pages;
+    }
+  }
+  __syncthreads();                         // the count is read before it is written
+  for (int b0 = 0; b0 < p.B; b0 += kMoveThreads) {
+    const int b = b0 + tid;
+    int L = 0, back = 0;
+    if (b < p.B) {
+      L = p.head[static_cast<long long>(b) * p.at.Hkv].x;
+      const bool cut = L > p.keep && L <= p.at.limit;
+      p.seq_lens_out[b] = cut ? p.keep : L;
+      if (p.free_pages && cut) back = ((L + (ps - 1)) >> p.at.page_shift) - ((p.keep + (ps - 1)) >> p.at.page_shift);
+    }
+    if (!p.free_pages) continue;
+    int inc = back;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    if (lane == 31) warp_sum[warp] = inc;
+    __syncthreads();
+    long long at = top + inc - back, all = 0;
+    for (int w = 0; w < kMoveThreads / 32; ++w) {
+      if (w < warp) at += warp_sum[w];
+      all += warp_sum[w];
+    }
+    __syncthreads();
+    // each warp its 32 sequences, a lane a page
+    for (int i = 0; i < 32; ++i) {
+      const int n = __shfl_sync(0xffffffffu, back, i);
+      const long long to = __shfl_sync(0xffffffffu, at, i);
+      const int32_t* row = p.at.page_table + static_cast<long long>(b0 + warp * 32 + i) * p.at.max_pages +
+                           ((p.keep + (ps - 1)) >> p.at.page_shift);
+      for (int j = lane; j < n; j += 32) {
+        int id = row[j];
+        if (id < 0 || id >= p.at.num_pages) {
+          record_error(p.at.err, TK_DEVERR_INDEX);
+          id = -1;
+        }
+        if (to + j < p.at.num_pages) p.free_pages[to + j] = id;
+        else record_error(p.at.err, TK_DEVERR_INDEX);      // more free pages than the pool has
+      }
+    }
+    top += all;
+  }
+  if (p.free_pages && tid == 0) *p.free_count = static_cast<int>(min(top, static_cast<long long>(p.at.num_pages)));
+}
+
+// blockIdx.x: pair * parts + part; the last block of the grid finishes.  Part 0
+// moves, kind by kind, what needs an order, the others the rest.
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictParams p, const int parts,
+                                                                  const int kinds) {
+  pdl_wait();
+  pdl_trigger();
+  const int tid = threadIdx.x;
+  const long long pairs = static_cast<long long>(p.B) * p.at.Hkv;
+  if (blockIdx.x == pairs * parts) {
+    finish(p);
+    return;
+  }
+  const long long pair = blockIdx.x / parts;
+  const int part = static_cast<int>(blockIdx.x % parts);
+  const int4 head = p.head[pair];
+  const int L = head.x, moves = head.y;
+  if (L <= p.keep || L > p.at.limit) return;
+  const int b = static_cast<int>(pair / p.at.Hkv), g = static_cast<int>(pair % p.at.Hkv);
+  const int want = p.keep - p.recent;
+  const int32_t* hole = p.hole + pair * p.keep;
+  const int32_t* src = p.src + pair * p.keep;
+  // tokens to move whose slots are below keep come first in the list
+  int lo = 0, hi = moves;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (src[mid] < p.keep) lo = mid + 1;
+    else hi = mid;
+  }
+  const int early = lo;
+  auto place = [&](int i, long long* from, long long* to) {
+    *from = slot_row_or_none(p.at, b, g, src[i]);
+    *to = slot_row_or_none(p.at, b, g, hole[i]);
+  };
+  if (part < kinds) {
+    // the early ones, then the recent ones: item i is token src[i] or token L - recent + i - early
+    const Kind kind = kind_of(p, part);
+    const int items = early + p.recent;
+    const int n = items << kind.shift;
+    for (int e0 = 0; e0 < n; e0 += kMoveThreads * kInFlight) {
+      uint4 x[kInFlight];
+      long long to[kInFlight];
+#pragma unroll
+      for (int k = 0; k < kInFlight; ++k) {
+        const int e = e0 + k * kMoveThreads + tid, i = e >> kind.shift, c = e & ((1 << kind.shift) - 1);
+        to[k] = -1;
+        if (e >= n) continue;
+        long long from;
+        if (i < early) {
+          place(i, &from, &to[k]);
+        } else {
+          from = slot_row_or_none(p.at, b, g, L - p.recent + (i - early));
+          to[k] = slot_row_or_none(p.at, b, g, want + (i - early));
+        }
+        if (from < 0) to[k] = -1;
+        if (to[k] >= 0) x[k] = load_piece(kind, from, c);
+        if (part == 0 && c == 0 && i < early && p.kept) p.kept[pair * p.keep + hole[i]] = src[i];
+      }
+      __syncthreads();                     // all of the round is loaded
+#pragma unroll
+      for (int k = 0; k < kInFlight; ++k) {
+        const int e = e0 + k * kMoveThreads + tid;
+        if (to[k] >= 0) store_piece(kind, to[k], e & ((1 << kind.shift) - 1), x[k]);
+      }
+    }
+    return;
+  }
+  const int share = parts - kinds, mine = part - kinds;
+  for (int k0 = 0; k0 < kinds; ++k0) {
+    const Kind kind = kind_of(p, k0);
+    const long long n = static_cast<long long>(moves - early) << kind.shift;
+    for (long long e0 = static_cast<long long>(mine) * kMoveThreads; e0 < n; e0 += static_cast<long long>(share) * kMoveThreads) {
+      const long long e = e0 + tid;
+      if (e >= n) continue;
+      const int i = early + static_cast<int>(e >> kind.shift), c = static_cast<int>(e) & ((1 << kind.shift) - 1);
+      long long from, to;
+      place(i, &from, &to);
+      if (from >= 0 && to >= 0) store_piece(kind, to, c, load_piece(kind, from, c));
+      if (k0 == 0 && c == 0 && p.kept) p.kept[pair * p.keep + hole[i]] = src[i];
+    }
+  }
+}
+
+}  // namespace
+
+size_t evict_workspace_bytes(int B, int Hkv, int keep) {
+  const size_t pairs = static_cast<size_t>(B) * Hkv;
+  return (pairs * sizeof(int4) + 255) / 256 * 256 + pairs * static_cast<size_t>(keep) * 2 * sizeof(int32_t);
+}
+
+cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t s) {
+  const long long pairs = static_cast<long long>(p.B) * p.at.Hkv;
+  // a block of threads for every 4096 tokens
+  int cluster = 1;
+  while (cluster < kMaxCluster && p.at.limit > cluster * 4096) cluster *= 2;
+  const int part = ((p.at.limit + cluster - 1) / cluster + 31) / 32 * 32;
+  const size_t smem = static_cast<size_t>(std::min(part, kHeld)) * 4;
+  cudaError_t e = cudaFuncSetAttribute(evict_choose_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeld * 4);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(pairs * cluster));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  e = cudaLaunchKernelEx(&cfg, evict_choose_kernel, p);
+  if (e != cudaSuccess) return e;
+  const int kinds = p.k_fmt ? 4 : 3;
+  // blocks of the tokens beyond keep: eight per SM together, at least one each
+  const long long rest = std::max(1ll, std::min<long long>((8ll * p.num_sms + pairs - 1) / pairs, (p.keep + 31) / 32));
+  const int parts = kinds + static_cast<int>(rest);
+  return launch_pdl(evict_move_kernel, dim3(static_cast<unsigned>(pairs * parts + 1)), dim3(kMoveThreads), 0, s, p, parts, kinds);
+}
+
+}  // namespace tk

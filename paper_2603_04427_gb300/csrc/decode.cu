@@ -574,10 +574,7 @@ decode_kernel(const __grid_constant__ DecodeMaps maps, const DecodeParams p) {
                 const int pidx = (tj + t) >> p.page_shift;
                 // pages past the context are never read back: any valid page will do
                 int page = pidx < p.max_pages ? p.page_table[static_cast<long long>(bj) * p.max_pages + pidx] : 0;
-                if (page < 0 || page >= p.num_pages) {
-                  if (t < nj) record_error(p.err, TK_DEVERR_INDEX);
-                  page = 0;
-                }
+                if (page < 0 || page >= p.num_pages) page = 0;
                 r2 = (static_cast<long long>(page) * Hkv + gj) * ps;
               }
 #pragma unroll

@@ -209,10 +209,11 @@ __global__ void __launch_bounds__(kWarps * 32) block_bounds_kernel(const __grid_
 template <int R, int KF>
 cudaError_t launch_t(const BoundsParams& p, cudaStream_t s) {
   constexpr int BYTES = KF == 0 ? 2 * R : (KF == 1 ? R : R / 2);
-  // a warp for every 4 KB of a block (eight 16-byte loads a lane)
-  int wpu = 1;
-  while (wpu < kWarps && p.block * BYTES > wpu * 4096) wpu *= 2;
+  // a warp for every 4 KB of a block (eight 16-byte loads a lane), or, where there are
+  // blocks for 32 warps of every SM, one for each: no barrier
   const long long units = static_cast<long long>(p.B) * p.at.Hkv * p.per_seq;
+  int wpu = 1;
+  while (wpu < kWarps && p.block * BYTES > wpu * 4096 && units * wpu < 32ll * p.num_sms) wpu *= 2;
   const long long want = (units * wpu + kWarps - 1) / kWarps;
   const unsigned grid = static_cast<unsigned>(std::min(want, 64ll * p.num_sms));
   return launch_pdl(block_bounds_kernel<R, KF>, dim3(grid), dim3(kWarps * 32), 0, s, p, wpu);

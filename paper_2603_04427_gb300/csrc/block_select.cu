@@ -25,15 +25,17 @@
 // n-th largest by 8-bit digits and writes the chosen blocks in order.
 #include <algorithm>
 
+#include "cluster.cuh"
 #include "key_frag.cuh"
 #include "kernels.h"
 
 namespace tk {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr int kCopies = 4;         // of a histogram, so that equal digits of a warp do not queue up
+constexpr int kList = 64;          // keys of one bucket that are ranked instead of split further
+constexpr int kFew = 256;          // undecided blocks that are ranked by comparing all of them
 // Key of the blocks that are chosen whatever their score; above +inf's.
 constexpr uint32_t kForced = 0xffffffffu;
 
@@ -50,60 +52,48 @@ __device__ __forceinline__ uint64_t key_of(double x) {
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_arrive() {
-  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait() {
-  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-}
-// Address of the first block's copy of a shared variable.
-__device__ __forceinline__ uint32_t in_first(const void* p) {
-  uint32_t a;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_addr(p)));
-  return a;
-}
+// An 8-byte value into another block's shared memory.
 __device__ __forceinline__ void store_cluster(uint32_t addr, uint64_t v) {
   asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
 
 struct Shared {
-  uint32_t hist[256];
+  uint32_t hist[kCopies][256];
   float amax[kMaxCluster];   // largest |bound| of each block of threads' part
-  int warp[kWarps][2];
-  int digit, above;
-  int in, cand;
+  int warp[32][2];
+  int digit, above, bucket;
+  int in, cand, listed, listed2;
+  uint64_t key, list[kList];
+  int id[kFew];
+  double score[kFew];
 };
 
-// The n-th largest (n >= 1) of `count` keys: its value, and how many are larger.
-// Digits of 8 bits from the top; only keys that `use` accepts count.  All threads.
-template <typename Key, typename Get>
+// The n-th largest (n >= 1) of `count` keys in shared memory: its value, and how many
+// are larger.  Digits of 8 bits from the top.  All kThreads threads.
+template <typename Key, int kThreads, typename Get>
 __device__ __forceinline__ Key nth_largest(Shared& sh, int count, int n, Get get, int* larger) {
   const int tid = threadIdx.x;
   Key prefix = 0;
   int above = 0;
   for (int shift = static_cast<int>(sizeof(Key)) * 8 - 8; shift >= 0; shift -= 8) {
-    sh.hist[tid] = 0;        // kThreads bins
+    for (int i = tid; i < kCopies * 256; i += kThreads) (&sh.hist[0][0])[i] = 0;
     __syncthreads();
     for (int i = tid; i < count; i += kThreads) {
-      Key k;
-      // the digits above this one agree with the prefix (a shift by the full width is not defined)
-      if (get(i, &k) && ((k ^ prefix) >> shift) < 256) atomicAdd(&sh.hist[(k >> shift) & 255], 1u);
+      const Key k = get(i);
+      // the digits above this one agree with the prefix
+      if (((k ^ prefix) >> shift) < 256) atomicAdd(&sh.hist[tid & (kCopies - 1)][(k >> shift) & 255], 1u);
     }
     __syncthreads();
     if (tid < 32) {          // eight bins a lane, from the top
       uint32_t c[8], sum = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) c[j] = sh.hist[255 - (tid * 8 + j)], sum += c[j];
+      for (int j = 0; j < 8; ++j) {
+        const int bin = 255 - (tid * 8 + j);
+        c[j] = 0;
+#pragma unroll
+        for (int w = 0; w < kCopies; ++w) c[j] += sh.hist[w][bin];
+        sum += c[j];
+      }
       uint32_t inc = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -115,7 +105,7 @@ __device__ __forceinline__ Key nth_largest(Shared& sh, int count, int n, Get get
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (before < static_cast<uint32_t>(n) && before + c[j] >= static_cast<uint32_t>(n))
-            sh.digit = 255 - (tid * 8 + j), sh.above = static_cast<int>(before);
+            sh.digit = 255 - (tid * 8 + j), sh.above = static_cast<int>(before), sh.bucket = static_cast<int>(c[j]);
           before += c[j];
         }
       }
@@ -123,6 +113,26 @@ __device__ __forceinline__ Key nth_largest(Shared& sh, int count, int n, Get get
     __syncthreads();
     prefix |= static_cast<Key>(sh.digit) << shift;
     above = sh.above;
+    if (shift > 0 && sh.bucket <= kList) {
+      // few keys agree with the prefix: listed and ranked against one another
+      if (tid == 0) sh.listed = 0;
+      __syncthreads();
+      for (int i = tid; i < count; i += kThreads) {
+        const Key k = get(i);
+        if (((k ^ prefix) >> shift) == 0) sh.list[atomicAdd(&sh.listed, 1)] = k;
+      }
+      __syncthreads();
+      const int listed = sh.listed;
+      if (tid < listed) {
+        const uint64_t mine = sh.list[tid];
+        int more = 0, same = 0;
+        for (int j = 0; j < listed; ++j) more += sh.list[j] > mine, same += sh.list[j] == mine;
+        if (above + more < n && above + more + same >= n) sh.key = mine, sh.above = above + more;   // equal ones agree
+      }
+      __syncthreads();
+      *larger = sh.above;
+      return static_cast<Key>(sh.key);
+    }
   }
   *larger = above;
   return prefix;
@@ -133,30 +143,43 @@ __device__ __forceinline__ long long bounds_row(const SelectParams& p, int b, in
   return slot_row(p.at, b, g, blk << p.block_shift) >> p.block_shift;
 }
 
-// s(blk) in 64 bits, elements in order (each thread a block); +inf where a bound
-// or a query head's score is not finite.
+// s(blk) in 64 bits, by a warp; +inf where a bound or a query head's score is not
+// finite.  (The products are exact, and so are the sums of numbers within 2^30 of each
+// other: their order does not matter there.)
 template <int R>
-__device__ double score64(const SelectParams& p, int b, int g, int blk) {
+__device__ __forceinline__ double score64(const SelectParams& p, int b, int g, int blk, int lane) {
+  constexpr int E = R >= 32 ? R / 32 : 1;
   const __nv_bfloat16* box = static_cast<const __nv_bfloat16*>(p.bounds) + bounds_row(p, b, g, blk) * 2 * R;
   const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + (static_cast<long long>(b) * p.at.Hkv + g) * p.G * R;
-  double best = -INFINITY;
+  float lo[E], hi[E];
   bool odd = false;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = lane + 32 * e;
+    lo[e] = i < R ? __bfloat162float(box[i]) : 0.f;
+    hi[e] = i < R ? __bfloat162float(box[R + i]) : 0.f;
+    odd |= !isfinite(lo[e]) || !isfinite(hi[e]);
+  }
+  double best = -INFINITY;
   for (int h = 0; h < p.G; ++h) {
     double s = 0;
-    for (int i = 0; i < R; ++i) {
-      const float lo = __bfloat162float(box[i]), hi = __bfloat162float(box[R + i]);
-      odd |= !isfinite(lo) || !isfinite(hi);
-      const float x = __bfloat162float(q[h * R + i]);
-      s += static_cast<double>(x) * (x < 0 ? lo : hi);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int i = lane + 32 * e;
+      const float x = i < R ? __bfloat162float(q[h * R + i]) : 0.f;
+      s += static_cast<double>(x) * (x < 0 ? lo[e] : hi[e]);
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     best = fmax(best, s);
     odd |= !isfinite(s);
   }
-  return odd ? INFINITY : best;
+  return __any_sync(0xffffffffu, odd) ? INFINITY : best;
 }
 
-template <int R>
-__global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_constant__ SelectParams p) {
+template <int R, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) block_select_kernel(const __grid_constant__ SelectParams p) {
+  constexpr int kWarps = kThreads / 32;
   constexpr int STEPS = 2 * R / 16;            // of the product of length 2 R
   constexpr int LOADS = STEPS / 2;             // 16-byte loads of a lane and row
   constexpr float kGamma = (STEPS + 1) * 17 * 0x1p-23f;
@@ -208,7 +231,7 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
     // this block's part, 16 blocks of keys a warp at a time
     const int per = ((n_blocks + 15) / 16 + parts - 1) / parts * 16;
     const int from = min(static_cast<int>(rank) * per, n_blocks), to = min(from + per, n_blocks);
-    const uint32_t first_keys = in_first(keys);
+    const uint32_t first_keys = address_of(keys, 0);
     uint32_t bmax = 0;                         // bf16 pair, largest magnitudes
     for (int t0 = from + warp * 16; t0 < to; t0 += kWarps * 16) {
       const int ra = min(t0 + gq, to - 1), rb = min(t0 + gq + 8, to - 1);
@@ -249,7 +272,7 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
     __syncthreads();
     if (tid == 0) {
       for (int w = 1; w < kWarps; ++w) big = fmaxf(big, __int_as_float(sh.warp[w][0]));
-      asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(in_first(&sh.amax[rank])), "r"(__float_as_int(big)) : "memory");
+      asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(address_of(&sh.amax[rank], 0)), "r"(__float_as_int(big)) : "memory");
     }
   }
   cluster_arrive();
@@ -262,10 +285,8 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
   int ties = 0;
   if (!all) {
     int larger;
-    const uint32_t top = nth_largest<uint32_t>(sh, n_blocks, n_take, [&](int i, uint32_t* k) {
-      *k = static_cast<uint32_t>(keys[i] >> 32);
-      return true;
-    }, &larger);
+    const uint32_t top = nth_largest<uint32_t, kThreads>(
+        sh, n_blocks, n_take, [&](int i) { return static_cast<uint32_t>(keys[i] >> 32); }, &larger);
     float eps = 0.f;
     if (top != kForced) {
       float big = 0.f;
@@ -282,7 +303,7 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
       const float t = value_of(top);
       const bool open = !(eps < 0x1p100f) || !isfinite(t);
       const uint32_t hi = open ? kForced - 1 : key_of(t + 2.f * eps), lo = open ? 0u : key_of(t - 2.f * eps);
-      if (tid == 0) sh.in = 0, sh.cand = 0;
+      if (tid == 0) sh.in = 0, sh.cand = 0, sh.listed2 = 0;
       __syncthreads();
       int in = 0, cand = 0;
       for (int i = tid; i < n_blocks; i += kThreads) {
@@ -296,22 +317,41 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
       __syncthreads();
       in = sh.in;
       cand = sh.cand;
-      if (in + cand == n_take) {
+      const int open_places = n_take - in;
+      if (cand == open_places) {
         edge = static_cast<uint64_t>(lo) << 32;
         ties = n_take;       // all that equal it
-      } else {
+      } else if (cand <= kFew) {
+        // listed, in any order; scored by a warp each; ranked against one another
         for (int i = tid; i < n_blocks; i += kThreads) {
           const uint32_t k = static_cast<uint32_t>(keys[i] >> 32);
-          if (k > hi) keys[i] = ~0ull;
-          else if (k < lo) keys[i] = 0;
-          else keys[i] = key_of(score64<R>(p, b, g, i));
+          if (k <= hi && k >= lo) sh.id[atomicAdd(&sh.listed2, 1)] = i;
+        }
+        __syncthreads();
+        for (int i = warp; i < cand; i += kWarps) {
+          const double s = score64<R>(p, b, g, sh.id[i], lane);
+          if (lane == 0) sh.score[i] = s;
+        }
+        __syncthreads();
+        for (int i = tid; i < cand; i += kThreads) {
+          int before = 0;
+          for (int j = 0; j < cand; ++j)
+            before += sh.score[j] > sh.score[i] || (sh.score[j] == sh.score[i] && sh.id[j] < sh.id[i]);
+          keys[sh.id[i]] = before < open_places ? ~0ull : 0ull;
+        }
+        __syncthreads();
+        edge = static_cast<uint64_t>(hi) << 32 | 0xffffffffull;
+        ties = 0;
+      } else {
+        for (int i = warp; i < n_blocks; i += kWarps) {
+          const uint32_t k = static_cast<uint32_t>(keys[i] >> 32);
+          const uint64_t x = k > hi ? ~0ull : (k < lo ? 0 : key_of(score64<R>(p, b, g, i, lane)));
+          __syncwarp();
+          if (lane == 0) keys[i] = x;
         }
         __syncthreads();
         int more;
-        edge = nth_largest<uint64_t>(sh, n_blocks, n_take, [&](int i, uint64_t* k) {
-          *k = keys[i];
-          return true;
-        }, &more);
+        edge = nth_largest<uint64_t, kThreads>(sh, n_blocks, n_take, [&](int i) { return keys[i]; }, &more);
         ties = n_take - more;
       }
     }
@@ -354,40 +394,36 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
   if (tid == 0) p.lens[pair] = n_blocks == 0 ? 0 : ((n_take - 1) << p.block_shift) + L - ((n_blocks - 1) << p.block_shift);
 }
 
-template <int R>
-cudaError_t launch_t(const SelectParams& p, cudaStream_t s) {
-  auto kern = block_select_kernel<R>;
-  const long long pairs = static_cast<long long>(p.B) * p.at.Hkv;
-  // one block of threads for every 512 blocks of keys, as long as two fit an SM
-  int parts = 1;
-  while (parts < kMaxCluster && p.max_blocks > parts * 512 && pairs * parts < 2ll * p.num_sms) parts *= 2;
-  const size_t smem = static_cast<size_t>(std::max(p.max_blocks, 1)) * 8;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSelectBlocks * 8);
+template <int R, int kThreads>
+cudaError_t launch_t(const SelectParams& p, int parts, cudaStream_t s) {
+  auto kern = block_select_kernel<R, kThreads>;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSelectBlocks * 8);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(pairs * parts));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = static_cast<unsigned>(parts);
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kern, p);
+  const long long pairs = static_cast<long long>(p.B) * p.at.Hkv;
+  return launch_cluster(kern, dim3(static_cast<unsigned>(pairs * parts)), dim3(kThreads), parts,
+                        static_cast<size_t>(std::max(p.max_blocks, 1)) * 8, s, p);
+}
+
+// One block of threads for every 512 blocks of keys, while all run at once; large
+// ones for long contexts, where the first one's passes over all the scores count.
+template <int R>
+cudaError_t launch_r(const SelectParams& p, cudaStream_t s) {
+  const long long pairs = static_cast<long long>(p.B) * p.at.Hkv;
+  const bool large = p.max_blocks > 2048;
+  const long long room = static_cast<long long>(p.num_sms) * (large ? 1 : 2);
+  int parts = 1;
+  while (parts < kMaxCluster && p.max_blocks > parts * 512 && 2 * pairs * parts <= room) parts *= 2;
+  return large ? launch_t<R, 1024>(p, parts, s) : launch_t<R, 256>(p, parts, s);
 }
 
 }  // namespace
 
 cudaError_t launch_block_select(const SelectParams& p, cudaStream_t s, int* unsupported) {
   switch (p.R) {
-    case 16: return launch_t<16>(p, s);
-    case 32: return launch_t<32>(p, s);
-    case 64: return launch_t<64>(p, s);
-    case 128: return launch_t<128>(p, s);
+    case 16: return launch_r<16>(p, s);
+    case 32: return launch_r<32>(p, s);
+    case 64: return launch_r<64>(p, s);
+    case 128: return launch_r<128>(p, s);
   }
   *unsupported = 1;
   return cudaSuccess;

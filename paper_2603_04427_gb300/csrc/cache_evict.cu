@@ -25,15 +25,18 @@
 // Bound by latency for a few hundred rows, by HBM when a prompt is cut.
 #include <algorithm>
 
+#include "cluster.cuh"
 #include "key_frag.cuh"
 #include "kernels.h"
 
 namespace tk {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr int kCopies = 8;                // of a histogram, so that equal digits of a warp do not queue up
+constexpr int kList = 256;                // weights of one bucket that are ranked instead of split further
 constexpr int kHeld = 16384;              // weights of a block that shared memory holds
 
 // Order-preserving encoding; -0 as +0, NaN as the smallest.
@@ -43,35 +46,15 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-}
-// A shared variable of block `rank` of the cluster.
-__device__ __forceinline__ uint32_t load_of(const void* p, uint32_t rank) {
-  uint32_t a, v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-  return v;
-}
-
 struct Shared {
-  uint32_t hist[2][256];
+  uint32_t hist[2][kCopies][256];
   uint32_t total[256];
-  int digit, above;
+  uint32_t mine[2][256];                   // this block's sum of the copies
+  int digit, above, bucket, listed;
+  uint32_t key, list[kList];
   int equal;                               // weights that equal the border's, of the block
-  int count[2];                            // holes, tokens to move, of the block
-  int warp[kWarps][2];
+  int count[3];                            // holes, tokens to move, those of them below keep, of the block
+  int warp[kWarps][3];
 };
 
 __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_constant__ EvictParams p) {
@@ -114,18 +97,29 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
   int above = 0;
   if (want > 0) {
     for (int shift = 24; shift >= 0; shift -= 8) {
-      uint32_t* hist = sh.hist[(shift >> 3) & 1];
-      if (tid < 256) hist[tid] = 0;
+      const int flip = (shift >> 3) & 1;
+      uint32_t* hist = sh.hist[flip][0];
+      for (int i = tid; i < kCopies * 256; i += kThreads) hist[i] = 0;
       __syncthreads();
       for (int t = from + tid; t < to; t += kThreads) {
         const uint32_t k = key(t);
-        if ((k ^ edge) >> shift < 256) atomicAdd(&hist[(k >> shift) & 255], 1u);
+        if ((k ^ edge) >> shift < 256) atomicAdd(&hist[(lane & (kCopies - 1)) * 256 + ((k >> shift) & 255)], 1u);
       }
-      cluster_sync();                      // this digit's histograms are complete
+      __syncthreads();
       if (tid < 256) {
         uint32_t c = 0;
-        for (uint32_t r = 0; r < parts; ++r) c += load_of(&hist[tid], r);
-        sh.total[tid] = c;
+#pragma unroll
+        for (int w = 0; w < kCopies; ++w) c += hist[w * 256 + tid];
+        if (parts == 1) sh.total[tid] = c;
+        else sh.mine[flip][tid] = c;
+      }
+      if (parts > 1) {
+        cluster_sync();                    // this digit's histograms are complete
+        if (tid < 256) {
+          uint32_t c = 0;
+          for (uint32_t r = 0; r < parts; ++r) c += load_of(&sh.mine[flip][tid], r);
+          sh.total[tid] = c;
+        }
       }
       __syncthreads();
       if (tid < 32) {                      // eight bins a lane, from the top
@@ -142,15 +136,36 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (before < static_cast<uint32_t>(want) && before + c[j] >= static_cast<uint32_t>(want))
-            sh.digit = 255 - (tid * 8 + j), sh.above = static_cast<int>(before);
+            sh.digit = 255 - (tid * 8 + j), sh.above = static_cast<int>(before), sh.bucket = static_cast<int>(c[j]);
           before += c[j];
         }
       }
       __syncthreads();
       edge |= static_cast<uint32_t>(sh.digit) << shift;
       above = sh.above;
+      if (parts == 1 && shift > 0 && sh.bucket <= kList) {
+        // few weights agree with the digits so far: listed and ranked against one another
+        if (tid == 0) sh.listed = 0;
+        __syncthreads();
+        for (int t = from + tid; t < to; t += kThreads) {
+          const uint32_t k = key(t);
+          if ((k ^ edge) >> shift == 0) sh.list[atomicAdd(&sh.listed, 1)] = k;
+        }
+        __syncthreads();
+        const int listed = sh.listed;
+        if (tid < listed) {
+          const uint32_t mine = sh.list[tid];
+          int more = 0, same = 0;
+          for (int j = 0; j < listed; ++j) more += sh.list[j] > mine, same += sh.list[j] == mine;
+          if (above + more < want && above + more + same >= want) sh.key = mine, sh.above = above + more;   // equal ones agree
+        }
+        __syncthreads();
+        edge = sh.key;
+        above = sh.above;
+        break;
+      }
       // the other histogram is next: nobody reads it, since all have passed the
-      // barrier of this one
+      // cluster's barrier of this one
     }
   }
   const int ties = want - above;           // of the weights at the border, the first ones stay
@@ -164,14 +179,15 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
   for (int t0 = r0; t0 < r1; t0 += 32) same += __popc(__ballot_sync(0xffffffffu, equal(t0 + lane)));
   if (lane == 0) sh.warp[warp][0] = same;
   __syncthreads();
-  int same_before = 0;
-  for (int w = 0; w < warp; ++w) same_before += sh.warp[w][0];
+  // sum of column c of the warps before this one
+  auto before = [&](int c) { return static_cast<int>(__reduce_add_sync(0xffffffffu, lane < warp ? sh.warp[lane][c] : 0)); };
+  int same_before = before(0);
   if (warp == kWarps - 1 && lane == 0) sh.equal = same_before + same;
-  cluster_sync();
+  if (parts > 1) cluster_sync();
   for (uint32_t r = 0; r < rank; ++r) same_before += static_cast<int>(load_of(&sh.equal, r));
   // holes and tokens to move: counted, then written
   const int same0 = same_before;
-  int holes = 0, moves = 0;
+  int holes = 0, moves = 0, early = 0;
   auto classify = [&](int t0, uint32_t* hole, uint32_t* move, uint32_t* stay) {
     const int t = t0 + lane;
     const bool here = t < r1;
@@ -189,19 +205,22 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
     classify(t0, &h, &m, &s);
     holes += __popc(h);
     moves += __popc(m);
+    early += __popc(__ballot_sync(0xffffffffu, (m >> lane & 1) && t0 + lane < p.keep));
   }
   __syncthreads();                         // the counts of equal weights are read
-  if (lane == 0) sh.warp[warp][0] = holes, sh.warp[warp][1] = moves;
+  if (lane == 0) sh.warp[warp][0] = holes, sh.warp[warp][1] = moves, sh.warp[warp][2] = early;
   __syncthreads();
-  int h_at = 0, m_at = 0;
-  for (int w = 0; w < warp; ++w) h_at += sh.warp[w][0], m_at += sh.warp[w][1];
-  if (warp == kWarps - 1 && lane == 0) sh.count[0] = h_at + holes, sh.count[1] = m_at + moves;
-  cluster_sync();
-  int total = 0;
+  int h_at = before(0), m_at = before(1);
+  const int e_at = before(2);
+  if (warp == kWarps - 1 && lane == 0) sh.count[0] = h_at + holes, sh.count[1] = m_at + moves, sh.count[2] = e_at + early;
+  if (parts > 1) cluster_sync();
+  else __syncthreads();
+  int total = 0, total_early = 0;
   for (uint32_t r = 0; r < parts; ++r) {
     const int h = static_cast<int>(load_of(&sh.count[0], r)), m = static_cast<int>(load_of(&sh.count[1], r));
     if (r < rank) h_at += h, m_at += m;
     total += m;
+    total_early += static_cast<int>(load_of(&sh.count[2], r));
   }
   same_before = same0;
   int32_t* hole = p.hole + pair * p.keep;
@@ -224,12 +243,12 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
   }
   if (kept)
     for (int i = first; i < p.recent; i += stride) kept[want + i] = n + i;
-  if (rank == 0 && tid == 0) p.head[pair] = make_int4(raw, total, 0, 0);
-  cluster_sync();                          // nobody's shared memory goes while others read it
+  if (rank == 0 && tid == 0) p.head[pair] = make_int4(raw, total, total_early, 0);
+  if (parts > 1) cluster_sync();           // nobody's shared memory goes while others read it
 }
 
 // ---------------------------------------------------------------- the moves
-constexpr int kMoveThreads = 256;
+constexpr int kMoveThreads = 512;
 constexpr int kInFlight = 8;
 
 // One kind of a token's data: `lanes` 16-byte pieces (or one 4-byte value) a row.
@@ -350,14 +369,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
   const int want = p.keep - p.recent;
   const int32_t* hole = p.hole + pair * p.keep;
   const int32_t* src = p.src + pair * p.keep;
-  // tokens to move whose slots are below keep come first in the list
-  int lo = 0, hi = moves;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (src[mid] < p.keep) lo = mid + 1;
-    else hi = mid;
-  }
-  const int early = lo;
+  const int early = head.z;                // tokens to move from slots below keep come first in the list
   auto place = [&](int i, long long* from, long long* to) {
     *from = slot_row_or_none(p.at, b, g, src[i]);
     *to = slot_row_or_none(p.at, b, g, hole[i]);
@@ -395,18 +407,55 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
     }
     return;
   }
+  // The others, a warp for every token of a few: lanes 0 .. take the pieces of its
+  // values, keys, weight and scale.
   const int share = parts - kinds, mine = part - kinds;
+  const int warp = tid >> 5, lane = tid & 31;
+  Kind kind = kind_of(p, 0);
+  int c = lane, pieces = 0;               // this lane's kind and piece; lanes past the last one idle
+  bool busy = false;
   for (int k0 = 0; k0 < kinds; ++k0) {
-    const Kind kind = kind_of(p, k0);
-    const long long n = static_cast<long long>(moves - early) << kind.shift;
-    for (long long e0 = static_cast<long long>(mine) * kMoveThreads; e0 < n; e0 += static_cast<long long>(share) * kMoveThreads) {
-      const long long e = e0 + tid;
-      if (e >= n) continue;
-      const int i = early + static_cast<int>(e >> kind.shift), c = static_cast<int>(e) & ((1 << kind.shift) - 1);
-      long long from, to;
-      place(i, &from, &to);
-      if (from >= 0 && to >= 0) store_piece(kind, to, c, load_piece(kind, from, c));
-      if (k0 == 0 && c == 0 && p.kept) p.kept[pair * p.keep + hole[i]] = src[i];
+    const Kind k = kind_of(p, k0);
+    const int n = 1 << k.shift;
+    if (lane >= pieces && lane < pieces + n) kind = k, c = lane - pieces, busy = true;
+    pieces += n;
+  }
+  const int n_rows = moves - early;
+  constexpr int kMoveWarps = kMoveThreads / 32;
+  constexpr int kStep = kMoveWarps * kInFlight;
+  for (int i0 = mine * kStep; i0 < n_rows; i0 += share * kStep) {
+    // lane k < kInFlight finds the places of the warp's k-th token
+    long long from_k = -1, to_k = -1;
+    const int i_k = i0 + warp * kInFlight + lane;
+    if (lane < kInFlight && i_k < n_rows) {
+      place(early + i_k, &from_k, &to_k);
+      if (p.kept) p.kept[pair * p.keep + hole[early + i_k]] = src[early + i_k];
+    }
+    uint4 x[kInFlight];
+    long long to[kInFlight];
+#pragma unroll
+    for (int k = 0; k < kInFlight; ++k) {
+      const long long from = __shfl_sync(0xffffffffu, from_k, k);
+      to[k] = __shfl_sync(0xffffffffu, to_k, k);
+      if (from < 0 || !busy) to[k] = -1;
+      if (to[k] >= 0) x[k] = load_piece(kind, from, c);
+    }
+#pragma unroll
+    for (int k = 0; k < kInFlight; ++k)
+      if (to[k] >= 0) store_piece(kind, to[k], c, x[k]);
+    // keys of 256 bytes with values of 256: a second turn for the lanes past 32
+    for (int extra = 32; extra < pieces; extra += 32) {
+      int left = extra + lane, k1 = 0;
+      Kind kx = kind_of(p, 0);
+      while (k1 < kinds && left >= 1 << kx.shift) {
+        left -= 1 << kx.shift;
+        if (++k1 < kinds) kx = kind_of(p, k1);
+      }
+#pragma unroll
+      for (int k = 0; k < kInFlight; ++k) {
+        const long long from = __shfl_sync(0xffffffffu, from_k, k), t = __shfl_sync(0xffffffffu, to_k, k);
+        if (from >= 0 && t >= 0 && k1 < kinds) store_piece(kx, t, left, load_piece(kx, from, left));
+      }
     }
   }
 }
@@ -420,31 +469,20 @@ size_t evict_workspace_bytes(int B, int Hkv, int keep) {
 
 cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t s) {
   const long long pairs = static_cast<long long>(p.B) * p.at.Hkv;
-  // a block of threads for every 4096 tokens
+  // a block of threads for every 4096 tokens, while all run at once
   int cluster = 1;
-  while (cluster < kMaxCluster && p.at.limit > cluster * 4096) cluster *= 2;
+  while (cluster < kMaxCluster && p.at.limit > cluster * 4096 && pairs * cluster <= p.num_sms) cluster *= 2;
   const int part = ((p.at.limit + cluster - 1) / cluster + 31) / 32 * 32;
   const size_t smem = static_cast<size_t>(std::min(part, kHeld)) * 4;
   cudaError_t e = cudaFuncSetAttribute(evict_choose_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeld * 4);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(pairs * cluster));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  e = cudaLaunchKernelEx(&cfg, evict_choose_kernel, p);
+  e = launch_cluster(evict_choose_kernel, dim3(static_cast<unsigned>(pairs * cluster)), dim3(kThreads), cluster, smem, s, p);
   if (e != cudaSuccess) return e;
   const int kinds = p.k_fmt ? 4 : 3;
-  // blocks of the tokens beyond keep: eight per SM together, at least one each
-  const long long rest = std::max(1ll, std::min<long long>((8ll * p.num_sms + pairs - 1) / pairs, (p.keep + 31) / 32));
+  // Blocks of the tokens from slot keep on, of which there are so many at most: one
+  // for 128 tokens (a round of each warp), four per SM together.
+  const long long most = std::max<long long>(0, std::min<long long>(p.keep - p.recent, static_cast<long long>(p.at.limit) - p.recent - p.keep));
+  const long long rest = std::min<long long>((4ll * p.num_sms + pairs - 1) / pairs, (most + 127) / 128);
   const int parts = kinds + static_cast<int>(rest);
   return launch_pdl(evict_move_kernel, dim3(static_cast<unsigned>(pairs * parts + 1)), dim3(kMoveThreads), 0, s, p, parts, kinds);
 }

@@ -62,10 +62,13 @@ struct WeightsParams {
   const int32_t* seq_lens;
   float* w;                 // fp32, a value per slot
   float scale_log2, decay;
+  float unit;               // |scale_log2|, or 1 if that is zero
   int B, G, R, k_fmt, n_q;
   int rows;                 // G * n_q
   // set by plan_weights
-  int per_cta, splits;      // tokens of a block, blocks of a (sequence, kv head)
+  int fused;                // blocks of a cluster of the one-launch form, or 0
+  int per_cta, splits;      // first of two launches: tokens of a block, blocks of a (sequence, kv head)
+  int sum_per_cta, sum_splits;   // second launch
   int store;                // the scores go through the workspace instead of being computed twice
   float2* part;             // [B * Hkv][splits][rows] maximum and sum
   float* scores;            // [B * Hkv][limit][rows]

@@ -262,7 +262,7 @@ tk_status tk_attn_weights(const tk_cache_desc* desc, const void* q, int32_t n_q,
                           const int32_t* seq_lens, int32_t max_seq_len, float scale, float decay, float* weights,
                           void* workspace, size_t workspace_bytes, void* stream) {
   TK_TRY(check_sizes(desc));
-  if (!std::isfinite(scale) || !std::isfinite(decay)) return fail(TK_ERR_INVALID_ARG, "scale / decay is not finite");
+  if (!std::isfinite(scale * 1.4426950408889634f) || !std::isfinite(decay)) return fail(TK_ERR_INVALID_ARG, "scale / decay is not finite");
   if (n_q < 1 || max_seq_len < 0) return fail(TK_ERR_INVALID_ARG, "n_q=%d max_seq_len=%d", n_q, max_seq_len);
   if (desc->batch == 0) return TK_OK;
   TK_TRY(check_keys(desc, k_cache, k_scale));
@@ -282,6 +282,7 @@ tk_status tk_attn_weights(const tk_cache_desc* desc, const void* q, int32_t n_q,
   p.seq_lens = seq_lens;
   p.w = weights;
   p.scale_log2 = scale * 1.4426950408889634f;
+  p.unit = p.scale_log2 == 0.f ? 1.f : std::fabs(p.scale_log2);
   p.decay = decay;
   p.part = static_cast<float2*>(workspace);
   const size_t stats = (static_cast<size_t>(p.B) * p.at.Hkv * p.splits * p.rows * sizeof(float2) + 255) / 256 * 256;

@@ -178,5 +178,6 @@ def test_the_same_bits_again_and_through_a_graph():
         tb.tk_attn_weights(x.c, q, x.seq, 3000, b, ws, x.seq)
     torch.cuda.synchronize()
     assert torch.equal(bits(a), bits(b)) and a.sum() > 0
+    q = _queries(2, 8, 2, 32, 11)
     with pytest.raises(tb.TkError, match="TK_ERR_WORKSPACE"):
-        tb.tk_attn_weights(x.c, q, x.seq, 3000, b, ws[:256])
+        tb.tk_attn_weights(x.c, q, x.seq, 3000, b, tb.attn_weights_workspace(x.c, 3000, 2)[:256])

@@ -292,7 +292,7 @@ def test_decode_with_a_table_of_the_callers_own():
     rows = np.concatenate([np.arange(224, 256), np.arange(64, 96), np.arange(64, 96), np.arange(288, 293)])
     ref = oa.attention_head(f64(q)[0], x.keys64()[rows], x.values()[rows], 1 / math.sqrt(32))
     parity(f64(o)[0], ref)
-    sel.table[0, 1] = 10
+    sel.table[0, 2] = 10           # begins the second 64 tokens
     tb.tk_attn_decode_blocks(x.c, q, sel, o, ws)
     assert tb.tk_get_device_error() == 1
 

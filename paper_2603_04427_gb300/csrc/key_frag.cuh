@@ -20,15 +20,19 @@ __device__ __forceinline__ long long slot_row(const SlotMap& m, int b, int g, in
   return (static_cast<long long>(page) * m.Hkv + g) * m.page_size + (t & (m.page_size - 1));
 }
 
-// The same for a row that is written: -1 for a bad page.
-__device__ __forceinline__ long long slot_row_or_none(const SlotMap& m, int b, int g, int t) {
+// The same for a row that is written, with the table's entry in hand: -1 for a bad page.
+__device__ __forceinline__ long long slot_of_page(const SlotMap& m, int b, int g, int page, int t) {
   if (m.page_size == 0) return (static_cast<long long>(b) * m.Hkv + g) * m.capacity + t;
-  const int page = m.page_table[static_cast<long long>(b) * m.max_pages + (t >> m.page_shift)];
   if (page < 0 || page >= m.num_pages) {
     record_error(m.err, TK_DEVERR_INDEX);
     return -1;
   }
   return (static_cast<long long>(page) * m.Hkv + g) * m.page_size + (t & (m.page_size - 1));
+}
+
+__device__ __forceinline__ long long slot_row_or_none(const SlotMap& m, int b, int g, int t) {
+  const int page = m.page_size == 0 ? 0 : m.page_table[static_cast<long long>(b) * m.max_pages + (t >> m.page_shift)];
+  return slot_of_page(m, b, g, page, t);
 }
 
 // A context length, clamped into what the cache can hold.
@@ -40,7 +44,7 @@ __device__ __forceinline__ int checked_len(int L, const SlotMap& m) {
 
 __device__ __forceinline__ void mma_bf16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                          uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
       "{%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -50,7 +54,7 @@ __device__ __forceinline__ void mma_bf16(float* d, uint32_t a0, uint32_t a1, uin
 // The same onto zeros.
 __device__ __forceinline__ void mma_bf16_first(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                                uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
       "{%8,%9}, {%10,%10,%10,%10};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
@@ -70,27 +74,22 @@ struct KeyRow {
   static constexpr int GROUPS = R >= 32 ? R / 32 : 1;
   uint32_t w[WORDS];
 
-  __device__ __forceinline__ void load(const void* base, long long row, int t) {
-    const unsigned char* p = static_cast<const unsigned char*>(base) + row * BYTES;
+  // From a row that is in shared memory.
+  __device__ __forceinline__ void load(const unsigned char* row, int t) {
     constexpr int PER = WORDS / GROUPS;       // words of a lane in a group of 32 (16 for r = 16)
 #pragma unroll
     for (int j = 0; j < GROUPS; ++j) {
-      const unsigned char* s = p + j * (BYTES / GROUPS) + t * PER * 4;
+      const unsigned char* s = row + j * (BYTES / GROUPS) + t * PER * 4;
       if constexpr (PER == 4) {
-        const uint4 x = __ldg(reinterpret_cast<const uint4*>(s));
+        const uint4 x = *reinterpret_cast<const uint4*>(s);
         w[4 * j] = x.x; w[4 * j + 1] = x.y; w[4 * j + 2] = x.z; w[4 * j + 3] = x.w;
       } else if constexpr (PER == 2) {
-        const uint2 x = __ldg(reinterpret_cast<const uint2*>(s));
+        const uint2 x = *reinterpret_cast<const uint2*>(s);
         w[2 * j] = x.x; w[2 * j + 1] = x.y;
       } else {
-        w[j] = __ldg(reinterpret_cast<const uint32_t*>(s));
+        w[j] = *reinterpret_cast<const uint32_t*>(s);
       }
     }
-  }
-
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) w[i] = 0;
   }
 
   // bf16 pairs of step s: (k 2t, 2t+1) and (k 2t+8, 2t+9); codes are widened exactly.

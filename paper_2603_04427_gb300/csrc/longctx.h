@@ -71,7 +71,7 @@ struct WeightsParams {
   int sum_per_cta, sum_splits;   // second launch
   int store;                // the scores go through the workspace instead of being computed twice
   float2* part;             // [B * Hkv][splits][rows] maximum and sum
-  float* scores;            // [B * Hkv][limit][rows]
+  float* scores;            // [B * Hkv][rows][limit rounded up to 16]
 };
 // Most G * n_q rows of a (sequence, kv head).
 constexpr int kMaxWeightRows = 512;

@@ -32,8 +32,8 @@ int64_t cache_rows(const tk_cache_desc* d) {
 // Sizes that the kernels count in 32 bits.
 tk_status check_sizes(const tk_cache_desc* d) {
   TK_TRY(check_desc(d));
-  if (cache_tokens(d) > (1ll << 30) || static_cast<int64_t>(d->batch) * d->h_kv > (1ll << 24))
-    return fail(TK_ERR_UNSUPPORTED, "tokens of a sequence are at most 2^30, batch * h_kv at most 2^24");
+  if (cache_tokens(d) > (1ll << 30) || static_cast<int64_t>(d->batch) * d->h_kv > (1ll << 24) || cache_rows(d) > (1ll << 34))
+    return fail(TK_ERR_UNSUPPORTED, "tokens of a sequence are at most 2^30, batch * h_kv 2^24, rows of the cache 2^34");
   return TK_OK;
 }
 

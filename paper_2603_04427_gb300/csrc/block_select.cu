@@ -52,9 +52,9 @@ __device__ __forceinline__ uint64_t key_of(double x) {
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 
-// An 8-byte value into another block's shared memory.
-__device__ __forceinline__ void store_cluster(uint32_t addr, uint64_t v) {
-  asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+// A value into another block's shared memory.
+__device__ __forceinline__ void store_cluster(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 
 struct Shared {
@@ -63,25 +63,29 @@ struct Shared {
   int warp[32][2];
   int digit, above, bucket;
   int in, cand, listed, listed2;
+  uint8_t chosen[kFew];
   uint64_t key, list[kList];
   int id[kFew];
   double score[kFew];
 };
 
-// The n-th largest (n >= 1) of `count` keys in shared memory: its value, and how many
-// are larger.  Digits of 8 bits from the top.  All kThreads threads.
-template <typename Key, int kThreads, typename Get>
-__device__ __forceinline__ Key nth_largest(Shared& sh, int count, int n, Get get, int* larger) {
+// The n-th largest (n >= 1) of the block's keys, ITEMS a thread (a thread's items past
+// its `count` are not looked at): its value, and how many are larger.  Digits of 8
+// bits from the top, until few keys agree with them.  All kThreads threads.
+template <int kThreads, int ITEMS, typename Key>
+__device__ __forceinline__ Key nth_largest(Shared& sh, const Key (&keys)[ITEMS], int count, int n, int* larger) {
   const int tid = threadIdx.x;
   Key prefix = 0;
   int above = 0;
   for (int shift = static_cast<int>(sizeof(Key)) * 8 - 8; shift >= 0; shift -= 8) {
     for (int i = tid; i < kCopies * 256; i += kThreads) (&sh.hist[0][0])[i] = 0;
+    if (tid == 0) sh.listed = 0;
     __syncthreads();
-    for (int i = tid; i < count; i += kThreads) {
-      const Key k = get(i);
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
       // the digits above this one agree with the prefix
-      if (((k ^ prefix) >> shift) < 256) atomicAdd(&sh.hist[tid & (kCopies - 1)][(k >> shift) & 255], 1u);
+      if (j < count && ((keys[j] ^ prefix) >> shift) < 256)
+        atomicAdd(&sh.hist[tid & (kCopies - 1)][(keys[j] >> shift) & 255], 1u);
     }
     __syncthreads();
     if (tid < 32) {          // eight bins a lane, from the top
@@ -115,12 +119,9 @@ __device__ __forceinline__ Key nth_largest(Shared& sh, int count, int n, Get get
     above = sh.above;
     if (shift > 0 && sh.bucket <= kList) {
       // few keys agree with the prefix: listed and ranked against one another
-      if (tid == 0) sh.listed = 0;
-      __syncthreads();
-      for (int i = tid; i < count; i += kThreads) {
-        const Key k = get(i);
-        if (((k ^ prefix) >> shift) == 0) sh.list[atomicAdd(&sh.listed, 1)] = k;
-      }
+#pragma unroll
+      for (int j = 0; j < ITEMS; ++j)
+        if (j < count && ((keys[j] ^ prefix) >> shift) == 0) sh.list[atomicAdd(&sh.listed, 1)] = keys[j];
       __syncthreads();
       const int listed = sh.listed;
       if (tid < listed) {
@@ -177,13 +178,13 @@ __device__ __forceinline__ double score64(const SelectParams& p, int b, int g, i
   return __any_sync(0xffffffffu, odd) ? INFINITY : best;
 }
 
-template <int R, int kThreads>
+template <int R, int kThreads, int ITEMS>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads) block_select_kernel(const __grid_constant__ SelectParams p) {
   constexpr int kWarps = kThreads / 32;
   constexpr int STEPS = 2 * R / 16;            // of the product of length 2 R
   constexpr int LOADS = STEPS / 2;             // 16-byte loads of a lane and row
   constexpr float kGamma = (STEPS + 1) * 17 * 0x1p-23f;
-  extern __shared__ uint64_t keys[];           // [max_blocks] of the first block of the cluster
+  extern __shared__ uint32_t keys[];           // [max_blocks] of the first block of the cluster
   __shared__ Shared sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank(), parts = cluster_size();
@@ -233,35 +234,53 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) block_select_kernel
     const int from = min(static_cast<int>(rank) * per, n_blocks), to = min(from + per, n_blocks);
     const uint32_t first_keys = address_of(keys, 0);
     uint32_t bmax = 0;                         // bf16 pair, largest magnitudes
-    for (int t0 = from + warp * 16; t0 < to; t0 += kWarps * 16) {
-      const int ra = min(t0 + gq, to - 1), rb = min(t0 + gq + 8, to - 1);
-      const uint4* pa = reinterpret_cast<const uint4*>(p.bounds) + bounds_row(p, b, g, ra) * (R / 4) + tq;
-      const uint4* pb = reinterpret_cast<const uint4*>(p.bounds) + bounds_row(p, b, g, rb) * (R / 4) + tq;
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
-      uint4 xa[LOADS], xb[LOADS];
+    // tiles of 16 blocks of keys a warp has in flight
+    constexpr int TILES = R <= 32 ? 2 : 1;
+    for (int t0 = from + warp * 16; t0 < to; t0 += TILES * kWarps * 16) {
+      uint4 xa[TILES][LOADS], xb[TILES][LOADS];
+      const uint4* pa[TILES];
+      const uint4* pb[TILES];
 #pragma unroll
-      for (int j = 0; j < LOADS; ++j) xa[j] = __ldg(pa + 4 * j), xb[j] = __ldg(pb + 4 * j);
-#pragma unroll
-      for (int j = 0; j < LOADS; ++j) {
-        mma_bf16(s, xa[j].x, xb[j].x, xa[j].y, xb[j].y, qf[2 * j][0], qf[2 * j][1]);
-        mma_bf16(s, xa[j].z, xb[j].z, xa[j].w, xb[j].w, qf[2 * j + 1][0], qf[2 * j + 1][1]);
-        auto seen = [&](uint32_t x) { asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(bmax) : "r"(x & 0x7fff7fffu)); };
-        seen(xa[j].x); seen(xa[j].y); seen(xa[j].z); seen(xa[j].w);
-        seen(xb[j].x); seen(xb[j].y); seen(xb[j].z); seen(xb[j].w);
+      for (int i = 0; i < TILES; ++i) {
+        const int t = t0 + i * kWarps * 16;
+        pa[i] = reinterpret_cast<const uint4*>(p.bounds) + bounds_row(p, b, g, min(t + gq, to - 1)) * (R / 4) + tq;
+        pb[i] = reinterpret_cast<const uint4*>(p.bounds) + bounds_row(p, b, g, min(t + gq + 8, to - 1)) * (R / 4) + tq;
       }
-      float a = -INFINITY, c = -INFINITY;      // blocks gq, gq + 8: largest of this lane's heads
-      if (2 * tq < p.G) a = s[0], c = s[2];
-      if (2 * tq + 1 < p.G) a = fmaxf(a, s[1]), c = fmaxf(c, s[3]);
 #pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
-        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-        c = fmaxf(c, __shfl_xor_sync(0xffffffffu, c, o));
+      for (int i = 0; i < TILES; ++i) {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) xa[i][j] = __ldg(pa[i] + 4 * j), xb[i][j] = __ldg(pb[i] + 4 * j);
       }
-      if (tq < 2) {
-        const int blk = t0 + gq + 8 * tq;
-        const bool forced = blk < p.n_first || blk >= n_blocks - p.n_last;
-        const uint32_t k = forced ? kForced : key_of(tq ? c : a);
-        if (blk < to) store_cluster(first_keys + blk * 8, static_cast<uint64_t>(k) << 32);
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) {
+        float s[4];
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+          const uint4 x = xa[i][j], y = xb[i][j];
+          if (j == 0) mma_bf16_first(s, x.x, y.x, x.y, y.y, qf[0][0], qf[0][1]);
+          else mma_bf16(s, x.x, y.x, x.y, y.y, qf[2 * j][0], qf[2 * j][1]);
+          mma_bf16(s, x.z, y.z, x.w, y.w, qf[2 * j + 1][0], qf[2 * j + 1][1]);
+          auto seen = [&](uint32_t v) { asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(bmax) : "r"(v & 0x7fff7fffu)); };
+          seen(x.x); seen(x.y); seen(x.z); seen(x.w);
+          seen(y.x); seen(y.y); seen(y.z); seen(y.w);
+        }
+        float a = -INFINITY, c = -INFINITY;    // blocks gq, gq + 8: largest of this lane's heads
+        if (2 * tq < p.G) a = s[0], c = s[2];
+        if (2 * tq + 1 < p.G) a = fmaxf(a, s[1]), c = fmaxf(c, s[3]);
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+          a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+          c = fmaxf(c, __shfl_xor_sync(0xffffffffu, c, o));
+        }
+        if (tq < 2) {
+          const int blk = t0 + i * kWarps * 16 + gq + 8 * tq;
+          const bool forced = blk < p.n_first || blk >= n_blocks - p.n_last;
+          const uint32_t k = forced ? kForced : key_of(tq ? c : a);
+          if (blk < to) {
+            if (parts == 1) keys[blk] = k;
+            else store_cluster(first_keys + blk * 4, k);
+          }
+        }
       }
     }
     const float b0 = bf16lo(bmax), b1 = bf16hi(bmax);
@@ -275,18 +294,32 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) block_select_kernel
       asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(address_of(&sh.amax[rank], 0)), "r"(__float_as_int(big)) : "memory");
     }
   }
-  cluster_arrive();
-  cluster_wait();
+  if (parts == 1) __syncthreads();
+  else cluster_sync();
   if (rank != 0) return;
 
   int32_t* table = p.table + pair * p.n_select;
   int32_t* ids = p.ids ? p.ids + pair * p.n_select : nullptr;
-  uint64_t edge = 0;         // chosen: keys above edge, and the first `ties` that equal it
+  // A run of blocks for each warp, block r0 + 32 j + lane the j-th of a thread: chosen
+  // are those in `over`, and the first `ties` of those in `same`.
+  const int run = ((n_blocks + 31) / 32 + kWarps - 1) / kWarps * 32;
+  const int r0 = warp * run;
+  const int count = min(run / 32, max(0, (n_blocks - r0 - lane + 31) / 32));
+  uint32_t over = count >= 32 ? 0xffffffffu : (1u << count) - 1, same = 0;
   int ties = 0;
   if (!all) {
+    uint32_t k[ITEMS];
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) k[j] = j < count ? keys[r0 + 32 * j + lane] : 0;
+    // items of which `f` says so
+    auto mask = [&](auto f) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < ITEMS; ++j) m |= (j < count && f(j) ? 1u : 0u) << j;
+      return m;
+    };
     int larger;
-    const uint32_t top = nth_largest<uint32_t, kThreads>(
-        sh, n_blocks, n_take, [&](int i) { return static_cast<uint32_t>(keys[i] >> 32); }, &larger);
+    const uint32_t top = nth_largest<kThreads, ITEMS>(sh, k, count, n_take, &larger);
     float eps = 0.f;
     if (top != kForced) {
       float big = 0.f;
@@ -296,36 +329,36 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) block_select_kernel
       if (big != 0.f && q1 != 0.f) eps = big * q1 * kGamma + (big + q1) * 0x1p-120f + 0x1p-100f;
       if (isnan(eps)) eps = INFINITY;
     }
-    edge = static_cast<uint64_t>(top) << 32;
-    ties = n_take - larger;
-    if (eps != 0.f) {
+    if (eps == 0.f) {
+      over = mask([&](int j) { return k[j] > top; });
+      same = mask([&](int j) { return k[j] == top; });
+      ties = n_take - larger;
+    } else {
       // blocks that the 32-bit scores do not decide
       const float t = value_of(top);
       const bool open = !(eps < 0x1p100f) || !isfinite(t);
       const uint32_t hi = open ? kForced - 1 : key_of(t + 2.f * eps), lo = open ? 0u : key_of(t - 2.f * eps);
-      if (tid == 0) sh.in = 0, sh.cand = 0, sh.listed2 = 0;
+      over = mask([&](int j) { return k[j] > hi; });
+      uint32_t undecided = mask([&](int j) { return k[j] <= hi && k[j] >= lo; });
+      if (tid == 0) sh.in = 0, sh.cand = 0;
       __syncthreads();
-      int in = 0, cand = 0;
-      for (int i = tid; i < n_blocks; i += kThreads) {
-        const uint32_t k = static_cast<uint32_t>(keys[i] >> 32);
-        in += k > hi;
-        cand += k <= hi && k >= lo;
-      }
-      in = __reduce_add_sync(0xffffffffu, in);
-      cand = __reduce_add_sync(0xffffffffu, cand);
-      if (lane == 0) atomicAdd(&sh.in, in), atomicAdd(&sh.cand, cand);
+      const int in_w = __reduce_add_sync(0xffffffffu, __popc(over)), cand_w = __reduce_add_sync(0xffffffffu, __popc(undecided));
+      if (lane == 0) atomicAdd(&sh.in, in_w), atomicAdd(&sh.cand, cand_w);
       __syncthreads();
-      in = sh.in;
-      cand = sh.cand;
-      const int open_places = n_take - in;
-      if (cand == open_places) {
-        edge = static_cast<uint64_t>(lo) << 32;
-        ties = n_take;       // all that equal it
+      const int cand = sh.cand, places = n_take - sh.in;
+      if (cand == places) {
+        over |= undecided;
       } else if (cand <= kFew) {
         // listed, in any order; scored by a warp each; ranked against one another
-        for (int i = tid; i < n_blocks; i += kThreads) {
-          const uint32_t k = static_cast<uint32_t>(keys[i] >> 32);
-          if (k <= hi && k >= lo) sh.id[atomicAdd(&sh.listed2, 1)] = i;
+        if (tid == 0) sh.listed2 = 0;
+        __syncthreads();
+        uint32_t left = undecided;
+        while (left) {
+          const int j = __ffs(left) - 1;
+          left &= left - 1;
+          const int at = atomicAdd(&sh.listed2, 1);
+          sh.id[at] = r0 + 32 * j + lane;
+          keys[r0 + 32 * j + lane] = at;
         }
         __syncthreads();
         for (int i = warp; i < cand; i += kWarps) {
@@ -337,50 +370,50 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) block_select_kernel
           int before = 0;
           for (int j = 0; j < cand; ++j)
             before += sh.score[j] > sh.score[i] || (sh.score[j] == sh.score[i] && sh.id[j] < sh.id[i]);
-          keys[sh.id[i]] = before < open_places ? ~0ull : 0ull;
+          sh.chosen[i] = before < places;
         }
         __syncthreads();
-        edge = static_cast<uint64_t>(hi) << 32 | 0xffffffffull;
-        ties = 0;
+        for (left = undecided; left; left &= left - 1) {
+          const int j = __ffs(left) - 1;
+          if (sh.chosen[keys[r0 + 32 * j + lane]]) over |= 1u << j;
+        }
       } else {
-        for (int i = warp; i < n_blocks; i += kWarps) {
-          const uint32_t k = static_cast<uint32_t>(keys[i] >> 32);
-          const uint64_t x = k > hi ? ~0ull : (k < lo ? 0 : key_of(score64<R>(p, b, g, i, lane)));
-          __syncwarp();
-          if (lane == 0) keys[i] = x;
+        // all of them in 64 bits: the warp takes its lanes' blocks in turn
+        uint64_t e[ITEMS];
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) {
+          e[j] = over >> j & 1 ? ~0ull : 0ull;
+          uint32_t lanes = __ballot_sync(0xffffffffu, undecided >> j & 1);
+          while (lanes) {
+            const int l = __ffs(lanes) - 1;
+            lanes &= lanes - 1;
+            const double s = score64<R>(p, b, g, r0 + 32 * j + l, lane);
+            if (lane == l) e[j] = key_of(s);
+          }
         }
-        __syncthreads();
         int more;
-        edge = nth_largest<uint64_t, kThreads>(sh, n_blocks, n_take, [&](int i) { return keys[i]; }, &more);
+        const uint64_t edge = nth_largest<kThreads, ITEMS>(sh, e, count, n_take, &more);
+        over = mask([&](int j) { return e[j] > edge; });
+        same = mask([&](int j) { return e[j] == edge; });
         ties = n_take - more;
       }
     }
   }
 
-  // the chosen blocks in order: a run of them for each warp, counted, then written
-  const int run = ((n_blocks + 31) / 32 + kWarps - 1) / kWarps * 32;
-  const int r0 = min(warp * run, n_blocks), r1 = min(r0 + run, n_blocks);
-  int over = 0, same = 0;
-  for (int i0 = r0; i0 < r1; i0 += 32) {
-    const int i = i0 + lane;
-    const bool here = i < r1;
-    over += __popc(__ballot_sync(0xffffffffu, here && !all && keys[here ? i : 0] > edge));
-    same += __popc(__ballot_sync(0xffffffffu, here && !all && keys[here ? i : 0] == edge));
-  }
-  if (lane == 0) sh.warp[warp][0] = over, sh.warp[warp][1] = same;
+  // the chosen blocks in order: counted by warp, then written
+  int n_over = __reduce_add_sync(0xffffffffu, __popc(over)), n_same = __reduce_add_sync(0xffffffffu, __popc(same));
   __syncthreads();
-  int before_over = 0, before_same = 0;
-  for (int w = 0; w < warp; ++w) before_over += sh.warp[w][0], before_same += sh.warp[w][1];
+  if (lane == 0) sh.warp[warp][0] = n_over, sh.warp[warp][1] = n_same;
+  __syncthreads();
+  int before_over = static_cast<int>(__reduce_add_sync(0xffffffffu, lane < warp ? sh.warp[lane][0] : 0));
+  int before_same = static_cast<int>(__reduce_add_sync(0xffffffffu, lane < warp ? sh.warp[lane][1] : 0));
   const uint32_t below = (1u << lane) - 1;
-  for (int i0 = r0; i0 < r1; i0 += 32) {
-    const int i = i0 + lane;
-    const bool here = i < r1;
-    const bool gt = here && !all && keys[here ? i : 0] > edge, eq = here && !all && keys[here ? i : 0] == edge;
+  for (int j = 0; j < run / 32; ++j) {
+    const bool gt = over >> j & 1, eq = same >> j & 1;
     const uint32_t mgt = __ballot_sync(0xffffffffu, gt), meq = __ballot_sync(0xffffffffu, eq);
     const int ngt = before_over + __popc(mgt & below), neq = before_same + __popc(meq & below);
-    const bool take = here && (all || gt || (eq && neq < ties));
-    if (take) {
-      const int at = all ? i : ngt + min(neq, ties);
+    if (gt || (eq && neq < ties)) {
+      const int at = ngt + min(neq, ties), i = r0 + 32 * j + lane;
       table[at] = static_cast<int32_t>(bounds_row(p, b, g, i));
       if (ids) ids[at] = i;
     }
@@ -394,14 +427,15 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) block_select_kernel
   if (tid == 0) p.lens[pair] = n_blocks == 0 ? 0 : ((n_take - 1) << p.block_shift) + L - ((n_blocks - 1) << p.block_shift);
 }
 
-template <int R, int kThreads>
+template <int R, int kThreads, int ITEMS>
 cudaError_t launch_t(const SelectParams& p, int parts, cudaStream_t s) {
-  auto kern = block_select_kernel<R, kThreads>;
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSelectBlocks * 8);
+  static_assert(kThreads * ITEMS <= 8192 || kThreads * ITEMS == kMaxSelectBlocks, "");
+  auto kern = block_select_kernel<R, kThreads, ITEMS>;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSelectBlocks * 4);
   if (e != cudaSuccess) return e;
   const long long pairs = static_cast<long long>(p.B) * p.at.Hkv;
   return launch_cluster(kern, dim3(static_cast<unsigned>(pairs * parts)), dim3(kThreads), parts,
-                        static_cast<size_t>(std::max(p.max_blocks, 1)) * 8, s, p);
+                        static_cast<size_t>(std::max(p.max_blocks, 1)) * 4, s, p);
 }
 
 // One block of threads for every 512 blocks of keys, while all run at once; large
@@ -413,7 +447,9 @@ cudaError_t launch_r(const SelectParams& p, cudaStream_t s) {
   const long long room = static_cast<long long>(p.num_sms) * (large ? 1 : 2);
   int parts = 1;
   while (parts < kMaxCluster && p.max_blocks > parts * 512 && 2 * pairs * parts <= room) parts *= 2;
-  return large ? launch_t<R, 1024>(p, parts, s) : launch_t<R, 256>(p, parts, s);
+  if (p.max_blocks > 8192) return launch_t<R, 1024, 24>(p, parts, s);
+  if (large) return launch_t<R, 1024, 8>(p, parts, s);
+  return p.max_blocks > 1024 ? launch_t<R, 256, 8>(p, parts, s) : launch_t<R, 256, 4>(p, parts, s);
 }
 
 }  // namespace

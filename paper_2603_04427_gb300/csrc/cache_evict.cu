@@ -35,6 +35,7 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr int kBatch = 4;                 // loads of a thread in flight
 constexpr int kCopies = 8;                // of a histogram, so that equal digits of a warp do not queue up
 constexpr int kList = 256;                // weights of one bucket that are ranked instead of split further
 constexpr int kHeld = 16384;              // weights of a block that shared memory holds
@@ -58,7 +59,7 @@ struct Shared {
 };
 
 __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_constant__ EvictParams p) {
-  extern __shared__ uint32_t held[];       // [min(part, kHeld)]
+  extern __shared__ float held[];          // [min(part, kHeld)] weights
   __shared__ Shared sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank(), parts = cluster_size();
@@ -74,11 +75,21 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
   const int stride = static_cast<int>(parts) * kThreads, first = static_cast<int>(rank) * kThreads + tid;
   if (L <= p.keep) {                       // everything stays (the whole cluster agrees)
     if (rank == 0 && tid == 0) p.head[pair] = make_int4(raw, 0, 0, 0);
-    for (int i = first; i < p.keep; i += stride) {
-      if (kept) kept[i] = i < L ? i : -1;
-      if (i < L && p.w_out != p.w) {
-        const long long at = slot_row_or_none(p.at, b, g, i);
-        if (at >= 0) p.w_out[at] = p.w[at];
+    if (kept)
+      for (int i = first; i < p.keep; i += stride) kept[i] = i < L ? i : -1;
+    if (p.w_out != p.w) {
+      for (int i0 = first; i0 < L; i0 += kBatch * stride) {
+        long long at[kBatch];
+        float x[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          const int i = i0 + j * stride;
+          at[j] = i < L ? slot_row_or_none(p.at, b, g, i) : -1;
+          x[j] = at[j] >= 0 ? p.w[at[j]] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (at[j] >= 0) p.w_out[at[j]] = x[j];
       }
     }
     return;
@@ -88,9 +99,17 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
   // this block's part of them, in whole warps' runs
   const int part = ((n + static_cast<int>(parts) - 1) / static_cast<int>(parts) + 31) / 32 * 32;
   const int from = min(static_cast<int>(rank) * part, n), to = min(from + part, n);
-  auto weight = [&](int t) { return key_of(__ldg(p.w + slot_row(p.at, b, g, t))); };
-  for (int i = tid; i < min(to - from, kHeld); i += kThreads) held[i] = weight(from + i);
-  auto key = [&](int t) { return t - from < kHeld ? held[t - from] : weight(t); };
+  auto load = [&](int t) { return p.w[slot_row(p.at, b, g, t)]; };
+  for (int i0 = tid; i0 < min(to - from, kHeld); i0 += kBatch * kThreads) {
+    float x[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) x[j] = i0 + j * kThreads < to - from ? load(from + i0 + j * kThreads) : 0.f;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+      if (i0 + j * kThreads < min(to - from, kHeld)) held[i0 + j * kThreads] = x[j];
+  }
+  auto weight = [&](int t) { return t - from < kHeld ? held[t - from] : load(t); };
+  auto key = [&](int t) { return key_of(weight(t)); };
 
   // the want-th largest
   uint32_t edge = 0;
@@ -235,7 +254,7 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
       if (kept) kept[t] = t;
       if (p.w_out != p.w) {
         const long long at = slot_row_or_none(p.at, b, g, t);
-        if (at >= 0) p.w_out[at] = p.w[at];
+        if (at >= 0) p.w_out[at] = weight(t);
       }
     }
     h_at += __popc(h);
@@ -249,7 +268,8 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
 
 // ---------------------------------------------------------------- the moves
 constexpr int kMoveThreads = 512;
-constexpr int kInFlight = 8;
+constexpr int kInFlight = 8;              // tokens that a warp has in flight
+constexpr int kMoveWarps = kMoveThreads / 32;
 
 // One kind of a token's data: `lanes` 16-byte pieces (or one 4-byte value) a row.
 struct Kind {
@@ -348,13 +368,16 @@ __device__ void finish(const EvictParams& p) {
   if (p.free_pages && tid == 0) *p.free_count = static_cast<int>(min(top, static_cast<long long>(p.at.num_pages)));
 }
 
-// blockIdx.x: pair * parts + part; the last block of the grid finishes.  Part 0
-// moves, kind by kind, what needs an order, the others the rest.
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictParams p, const int parts,
+// blockIdx.x: pair * parts + part; the last block of the grid finishes.  Part 0 moves
+// what needs an order, the others the rest.  A warp takes kInFlight tokens at a time;
+// its lanes are the pieces of a token's value, key, weight and key scale (WIDE: more
+// than 32 of them).
+template <bool WIDE>
+__global__ void __launch_bounds__(kMoveThreads, WIDE ? 1 : 2) evict_move_kernel(const __grid_constant__ EvictParams p, const int parts,
                                                                   const int kinds) {
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const long long pairs = static_cast<long long>(p.B) * p.at.Hkv;
   if (blockIdx.x == pairs * parts) {
     finish(p);
@@ -364,55 +387,14 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
   const int part = static_cast<int>(blockIdx.x % parts);
   const int4 head = p.head[pair];
   const int L = head.x, moves = head.y;
+  const int early = head.z;                // tokens to move from slots below keep come first in the list
   if (L <= p.keep || L > p.at.limit) return;
   const int b = static_cast<int>(pair / p.at.Hkv), g = static_cast<int>(pair % p.at.Hkv);
   const int want = p.keep - p.recent;
   const int32_t* hole = p.hole + pair * p.keep;
   const int32_t* src = p.src + pair * p.keep;
-  const int early = head.z;                // tokens to move from slots below keep come first in the list
-  auto place = [&](int i, long long* from, long long* to) {
-    *from = slot_row_or_none(p.at, b, g, src[i]);
-    *to = slot_row_or_none(p.at, b, g, hole[i]);
-  };
-  if (part < kinds) {
-    // the early ones, then the recent ones: item i is token src[i] or token L - recent + i - early
-    const Kind kind = kind_of(p, part);
-    const int items = early + p.recent;
-    const int n = items << kind.shift;
-    for (int e0 = 0; e0 < n; e0 += kMoveThreads * kInFlight) {
-      uint4 x[kInFlight];
-      long long to[kInFlight];
-#pragma unroll
-      for (int k = 0; k < kInFlight; ++k) {
-        const int e = e0 + k * kMoveThreads + tid, i = e >> kind.shift, c = e & ((1 << kind.shift) - 1);
-        to[k] = -1;
-        if (e >= n) continue;
-        long long from;
-        if (i < early) {
-          place(i, &from, &to[k]);
-        } else {
-          from = slot_row_or_none(p.at, b, g, L - p.recent + (i - early));
-          to[k] = slot_row_or_none(p.at, b, g, want + (i - early));
-        }
-        if (from < 0) to[k] = -1;
-        if (to[k] >= 0) x[k] = load_piece(kind, from, c);
-        if (part == 0 && c == 0 && i < early && p.kept) p.kept[pair * p.keep + hole[i]] = src[i];
-      }
-      __syncthreads();                     // all of the round is loaded
-#pragma unroll
-      for (int k = 0; k < kInFlight; ++k) {
-        const int e = e0 + k * kMoveThreads + tid;
-        if (to[k] >= 0) store_piece(kind, to[k], e & ((1 << kind.shift) - 1), x[k]);
-      }
-    }
-    return;
-  }
-  // The others, a warp for every token of a few: lanes 0 .. take the pieces of its
-  // values, keys, weight and scale.
-  const int share = parts - kinds, mine = part - kinds;
-  const int warp = tid >> 5, lane = tid & 31;
   Kind kind = kind_of(p, 0);
-  int c = lane, pieces = 0;               // this lane's kind and piece; lanes past the last one idle
+  int c = lane, pieces = 0;                // this lane's kind and piece; lanes past the last one idle
   bool busy = false;
   for (int k0 = 0; k0 < kinds; ++k0) {
     const Kind k = kind_of(p, k0);
@@ -420,42 +402,59 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
     if (lane >= pieces && lane < pieces + n) kind = k, c = lane - pieces, busy = true;
     pieces += n;
   }
-  const int n_rows = moves - early;
-  constexpr int kMoveWarps = kMoveThreads / 32;
-  constexpr int kStep = kMoveWarps * kInFlight;
-  for (int i0 = mine * kStep; i0 < n_rows; i0 += share * kStep) {
+  // Part 0: item i < early is token src[i], then the recent ones follow.  Others: token
+  // src[early + i].
+  const bool ordered = part == 0;
+  const int items = ordered ? early + p.recent : moves - early;
+  const int step = kMoveWarps * kInFlight * (ordered ? 1 : parts - 1);
+  for (int i0 = ordered ? 0 : (part - 1) * kMoveWarps * kInFlight; i0 < items; i0 += step) {
     // lane k < kInFlight finds the places of the warp's k-th token
     long long from_k = -1, to_k = -1;
-    const int i_k = i0 + warp * kInFlight + lane;
-    if (lane < kInFlight && i_k < n_rows) {
-      place(early + i_k, &from_k, &to_k);
-      if (p.kept) p.kept[pair * p.keep + hole[early + i_k]] = src[early + i_k];
+    const int i = i0 + warp * kInFlight + lane;
+    if (lane < kInFlight && i < items) {
+      int s, d;
+      if (ordered && i >= early) {
+        s = L - p.recent + (i - early);
+        d = want + (i - early);
+      } else {
+        s = src[ordered ? i : early + i];
+        d = hole[ordered ? i : early + i];
+        if (p.kept) p.kept[pair * p.keep + d] = s;
+      }
+      from_k = slot_row_or_none(p.at, b, g, s);
+      to_k = slot_row_or_none(p.at, b, g, d);
+      if (to_k < 0) from_k = -1;
     }
     uint4 x[kInFlight];
-    long long to[kInFlight];
 #pragma unroll
     for (int k = 0; k < kInFlight; ++k) {
       const long long from = __shfl_sync(0xffffffffu, from_k, k);
-      to[k] = __shfl_sync(0xffffffffu, to_k, k);
-      if (from < 0 || !busy) to[k] = -1;
-      if (to[k] >= 0) x[k] = load_piece(kind, from, c);
+      if (from >= 0 && busy) x[k] = load_piece(kind, from, c);
     }
-#pragma unroll
-    for (int k = 0; k < kInFlight; ++k)
-      if (to[k] >= 0) store_piece(kind, to[k], c, x[k]);
-    // keys of 256 bytes with values of 256: a second turn for the lanes past 32
-    for (int extra = 32; extra < pieces; extra += 32) {
-      int left = extra + lane, k1 = 0;
-      Kind kx = kind_of(p, 0);
-      while (k1 < kinds && left >= 1 << kx.shift) {
-        left -= 1 << kx.shift;
-        if (++k1 < kinds) kx = kind_of(p, k1);
+    uint4 y[WIDE ? kInFlight : 1];
+    Kind more = kind;
+    int c2 = 0;
+    const bool second = WIDE && lane + 32 < pieces;
+    if constexpr (WIDE) {
+      int left = lane + 32;
+      for (int k0 = 0; k0 < kinds; ++k0) {
+        const Kind k = kind_of(p, k0);
+        if (left >= 0 && left < 1 << k.shift) more = k, c2 = left;
+        left -= 1 << k.shift;
       }
 #pragma unroll
       for (int k = 0; k < kInFlight; ++k) {
-        const long long from = __shfl_sync(0xffffffffu, from_k, k), t = __shfl_sync(0xffffffffu, to_k, k);
-        if (from >= 0 && t >= 0 && k1 < kinds) store_piece(kx, t, left, load_piece(kx, from, left));
+        const long long from = __shfl_sync(0xffffffffu, from_k, k);
+        if (from >= 0 && second) y[k] = load_piece(more, from, c2);
       }
+    }
+    if (ordered) __syncthreads();          // all of the round is loaded
+#pragma unroll
+    for (int k = 0; k < kInFlight; ++k) {
+      const long long from = __shfl_sync(0xffffffffu, from_k, k), to = __shfl_sync(0xffffffffu, to_k, k);
+      if (from >= 0 && busy) store_piece(kind, to, c, x[k]);
+      if constexpr (WIDE)
+        if (from >= 0 && second) store_piece(more, to, c2, y[k]);
     }
   }
 }
@@ -483,8 +482,12 @@ cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t s) {
   // for 128 tokens (a round of each warp), four per SM together.
   const long long most = std::max<long long>(0, std::min<long long>(p.keep - p.recent, static_cast<long long>(p.at.limit) - p.recent - p.keep));
   const long long rest = std::min<long long>((4ll * p.num_sms + pairs - 1) / pairs, (most + 127) / 128);
-  const int parts = kinds + static_cast<int>(rest);
-  return launch_pdl(evict_move_kernel, dim3(static_cast<unsigned>(pairs * parts + 1)), dim3(kMoveThreads), 0, s, p, parts, kinds);
+  const int parts = 1 + static_cast<int>(rest);
+  const dim3 grid(static_cast<unsigned>(pairs * parts + 1));
+  const int key_bytes = p.k_fmt == 0 ? 2 * p.R : (p.k_fmt == 1 ? p.R : p.R / 2);
+  if (p.DV / 8 + key_bytes / 16 + kinds - 2 > 32)
+    return launch_pdl(evict_move_kernel<true>, grid, dim3(kMoveThreads), 0, s, p, parts, kinds);
+  return launch_pdl(evict_move_kernel<false>, grid, dim3(kMoveThreads), 0, s, p, parts, kinds);
 }
 
 }  // namespace tk

@@ -502,7 +502,9 @@ tk_status tk_block_tables(int32_t batch, int32_t page_size, int32_t num_pages,
 /* ------------------------------------------------------------------------
  * A long context, read or kept in part (not part of the paper's method; thin
  * keys make it cheap: which blocks a query needs, and how much attention a token
- * gets, follow from r of the r + d_v numbers of a token).
+ * gets, follow from r of the r + d_v numbers of a token).  What these calls
+ * write per slot or page (bounds, weights, an evicted cache) belongs to one
+ * sequence: a page must not stand in the page-table rows of two of them.
  * ------------------------------------------------------------------------ */
 
 /* Element-wise minimum and maximum of the cached keys of every block of `block`

@@ -107,7 +107,7 @@ struct KeyRing {
   int found;                              // lane i: rows of the i-th 16 tokens that are fetched next
   uint64_t policy;
   int fetch, take;                        // stages fetched and taken so far
-  bool ok;
+  int lost;                               // the first one that did not come, or -1
 
   __device__ __forceinline__ void find(const SlotMap& m, const TileRows& rows, int t, int to, int lane) {
     if (lane < PIECES && t + 16 * lane < to) found = rows.at(m, t + 16 * lane);
@@ -141,7 +141,7 @@ struct KeyRing {
     policy = ONCE ? l2_policy_evict_first() : 0;
     fetch = take = 0;
     found = 0;
-    ok = true;
+    lost = -1;
 #pragma unroll
     for (int s = 0; s < N; ++s) {
       if (t + s * STEP >= to) break;
@@ -154,14 +154,19 @@ struct KeyRing {
   // error word says so).
   __device__ __forceinline__ const unsigned char* wait(const WeightsParams& p) {
     const int s = take % N;
-    ok = __all_sync(0xffffffffu, ok && mbar_wait(bar + s, (take / N) & 1, p.at.err));
+    if (lost < 0 && !__all_sync(0xffffffffu, mbar_wait(bar + s, (take / N) & 1, p.at.err))) lost = take;
     return base + s * STAGE;
+  }
+  // Copies still on their way after a wait that ran out.
+  __device__ __forceinline__ void drain(const WeightsParams& p) {
+    if (lost < 0) return;
+    for (int i = lost; i < fetch; ++i) mbar_wait(bar + i % N, (i / N) & 1, p.at.err);
   }
   // Gives the stage back (all lanes have read it) and fetches its next tokens.
   __device__ __forceinline__ void next(const WeightsParams& p, const TileRows& rows, int t, int to, int lane) {
     ++take;
     __syncwarp();
-    if (ok && t + N * STEP < to) {
+    if (lost < 0 && t + N * STEP < to) {
       issue(p, t + N * STEP, to, lane);
       find(p.at, rows, t + (N + 1) * STEP, to, lane);
     }
@@ -266,14 +271,12 @@ __global__ void __launch_bounds__(kThreads, STORE ? 2 : kPerSm<R>) weights_stats
   __syncthreads();
   const float u = unit<KF>(p);
   float m[GROUP][H], l[GROUP][H];
-  int see[GROUP][H];                       // the last token that the lane's queries see
 #pragma unroll
   for (int c = 0; c < GROUP; ++c) {
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       m[c][h] = -INFINITY;
       l[c][h] = 0.f;
-      see[c][h] = min(r.to - 1, r.L - p.n_q + ((tile0 + c) * 16 + 8 * h + gq) % p.n_q);
     }
   }
   for (; t0 < r.to; t0 += STEP) {
@@ -305,9 +308,11 @@ __global__ void __launch_bounds__(kThreads, STORE ? 2 : kPerSm<R>) weights_stats
         for (int i = 0; i < TILES; ++i) {
 #pragma unroll
           for (int h = 0; h < H; ++h) {
+            // the last token that the lane's query sees
+            const int see = min(r.to - 1, r.L - p.n_q + ((tile0 + c) * 16 + 8 * h + gq) % p.n_q);
             const int t = t0 + 8 * i + 2 * tq;
-            if (t > see[c][h]) s[i][2 * h] = -INFINITY;
-            if (t + 1 > see[c][h]) s[i][2 * h + 1] = -INFINITY;
+            if (t > see) s[i][2 * h] = -INFINITY;
+            if (t + 1 > see) s[i][2 * h + 1] = -INFINITY;
           }
         }
       }
@@ -326,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, STORE ? 2 : kPerSm<R>) weights_stats
       }
     }
   }
+  ring.drain(p);
   // over the four lanes of a row, then over the warps
 #pragma unroll
   for (int c = 0; c < GROUP; ++c) {
@@ -349,6 +355,11 @@ __global__ void __launch_bounds__(kThreads, STORE ? 2 : kPerSm<R>) weights_stats
     p.part[block * p.rows + row] = x;
   }
 }
+
+template <bool V>
+struct Bool {
+  static constexpr bool value = V;
+};
 
 // A row's statistics for the second launch: maximum, 1 / sum (0 for a row that
 // sees no token) and the last token that it sees.
@@ -439,11 +450,11 @@ __global__ void __launch_bounds__(kThreads, 2) weights_sum_kernel(const __grid_c
     k.load(p, ring.wait(p), gq, tq);
     ring.next(p, rows, t0, r.to, lane);
     const bool masked = t0 + Keys::TOKENS - 1 > r.L - p.n_q;
-    const int odd = p.rows & 15 ? tiles - 1 : -1;
     float sum[TILES][2];
 #pragma unroll
     for (int i = 0; i < TILES; ++i) sum[i][0] = sum[i][1] = 0.f;
-    for (int c = 0; c < tiles; ++c) {
+    auto add = [&](int c, auto with_mask) {
+      constexpr bool kMask = decltype(with_mask)::value;
       RowStat x[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -462,8 +473,7 @@ __global__ void __launch_bounds__(kThreads, 2) weights_sum_kernel(const __grid_c
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           float a = fast_exp2(fmaf(s[2 * h], u, -x[h].m)), b = fast_exp2(fmaf(s[2 * h + 1], u, -x[h].m));
-          if (masked || c == odd) {
-            // also the rows past the last query, whose zeros may meet an infinite key
+          if constexpr (kMask) {
             const int t = t0 + 8 * i + 2 * tq;
             if (t > x[h].see) a = 0.f;
             if (t + 1 > x[h].see) b = 0.f;
@@ -472,7 +482,12 @@ __global__ void __launch_bounds__(kThreads, 2) weights_sum_kernel(const __grid_c
           sum[i][1] = fmaf(b, x[h].inv, sum[i][1]);
         }
       }
-    }
+    };
+    // tokens that some queries do not see, or (whose zeros may meet an infinite key)
+    // rows past the last query
+    const int plain = masked ? 0 : p.rows / 16;
+    for (int c = 0; c < plain; ++c) add(c, Bool<false>{});
+    for (int c = plain; c < tiles; ++c) add(c, Bool<true>{});
     // over the eight rows of four lanes: all then have tokens 2 tq, 2 tq + 1
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
@@ -486,6 +501,7 @@ __global__ void __launch_bounds__(kThreads, 2) weights_sum_kernel(const __grid_c
       if (tq == (i & 1) && at[i / 2] >= 0) p.w[at[i / 2]] = before[i / 2] + (gq & 1 ? b : a);
     }
   }
+  ring.drain(p);
 }
 
 // Four tokens a thread: slots and earlier weights.  Four tokens from a multiple of four
@@ -636,6 +652,7 @@ __global__ void __launch_bounds__(kThreads, 2) weights_fused_kernel(const __grid
       }
     }
   }
+  ring.drain(p);
 #pragma unroll
   for (int o = 1; o < 4; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   if (tq == 0) warp_part[warp][gq] = m;

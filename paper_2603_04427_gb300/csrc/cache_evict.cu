@@ -52,7 +52,8 @@ struct Shared {
   uint32_t total[256];
   uint32_t mine[2][256];                   // this block's sum of the copies
   int digit, above, bucket, listed;
-  uint32_t key, list[kList];
+  uint32_t key, list[kList], all[kList];
+  int at[kMaxCluster + 1];                 // first of each block's list among all of them
   int equal;                               // weights that equal the border's, of the block
   int count[3];                            // holes, tokens to move, those of them below keep, of the block
   int warp[kWarps][3];
@@ -162,20 +163,43 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
       __syncthreads();
       edge |= static_cast<uint32_t>(sh.digit) << shift;
       above = sh.above;
-      if (parts == 1 && shift > 0 && sh.bucket <= kList) {
-        // few weights agree with the digits so far: listed and ranked against one another
+      if (shift > 0 && sh.bucket <= kList) {
+        // few weights agree with the digits so far: listed by each block, ranked
+        // against one another by all
         if (tid == 0) sh.listed = 0;
         __syncthreads();
         for (int t = from + tid; t < to; t += kThreads) {
           const uint32_t k = key(t);
           if ((k ^ edge) >> shift == 0) sh.list[atomicAdd(&sh.listed, 1)] = k;
         }
+        if (parts > 1) {
+          cluster_sync();
+          if (warp == 0) {
+            // where each block's list goes: sh.at[r], sh.at[parts] = all of them
+            const int n_r = lane < static_cast<int>(parts) ? static_cast<int>(load_of(&sh.listed, lane)) : 0;
+            int inc = n_r;
+#pragma unroll
+            for (int o = 1; o < kMaxCluster; o <<= 1) {
+              const int y = __shfl_up_sync(0xffffffffu, inc, o);
+              if (lane >= o) inc += y;
+            }
+            if (lane < static_cast<int>(parts)) sh.at[lane] = inc - n_r;
+            if (lane == static_cast<int>(parts) - 1) sh.at[parts] = inc;
+          }
+          __syncthreads();
+          for (int i = tid; i < sh.at[parts]; i += kThreads) {
+            uint32_t r = 0;
+            while (i >= sh.at[r + 1]) ++r;
+            sh.all[i] = load_of(&sh.list[i - sh.at[r]], r);
+          }
+        }
         __syncthreads();
-        const int listed = sh.listed;
+        const uint32_t* list = parts > 1 ? sh.all : sh.list;
+        const int listed = parts > 1 ? sh.at[parts] : sh.listed;
         if (tid < listed) {
-          const uint32_t mine = sh.list[tid];
+          const uint32_t mine = list[tid];
           int more = 0, same = 0;
-          for (int j = 0; j < listed; ++j) more += sh.list[j] > mine, same += sh.list[j] == mine;
+          for (int j = 0; j < listed; ++j) more += list[j] > mine, same += list[j] == mine;
           if (above + more < want && above + more + same >= want) sh.key = mine, sh.above = above + more;   // equal ones agree
         }
         __syncthreads();

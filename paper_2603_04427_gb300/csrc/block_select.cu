@@ -33,7 +33,9 @@ namespace tk {
 namespace {
 
 constexpr int kMaxCluster = 8;
-constexpr int kCopies = 4;         // of a histogram, so that equal digits of a warp do not queue up
+// Copies of a histogram, next to each other, so that equal digits of a warp meet
+// neither at one address nor in one bank.
+constexpr int kCopies = 2;
 constexpr int kList = 64;          // keys of one bucket that are ranked instead of split further
 constexpr int kFew = 256;          // undecided blocks that are ranked by comparing all of them
 // Key of the blocks that are chosen whatever their score; above +inf's.
@@ -58,7 +60,7 @@ __device__ __forceinline__ void store_cluster(uint32_t addr, uint32_t v) {
 }
 
 struct Shared {
-  uint32_t hist[kCopies][256];
+  uint32_t hist[256][kCopies];
   float amax[kMaxCluster];   // largest |bound| of each block of threads' part
   int warp[32][2];
   int digit, above, bucket;
@@ -85,7 +87,7 @@ __device__ __forceinline__ Key nth_largest(Shared& sh, const Key (&keys)[ITEMS],
     for (int j = 0; j < ITEMS; ++j) {
       // the digits above this one agree with the prefix
       if (j < count && ((keys[j] ^ prefix) >> shift) < 256)
-        atomicAdd(&sh.hist[tid & (kCopies - 1)][(keys[j] >> shift) & 255], 1u);
+        atomicAdd(&sh.hist[(keys[j] >> shift) & 255][tid & (kCopies - 1)], 1u);
     }
     __syncthreads();
     if (tid < 32) {          // eight bins a lane, from the top
@@ -95,7 +97,7 @@ __device__ __forceinline__ Key nth_largest(Shared& sh, const Key (&keys)[ITEMS],
         const int bin = 255 - (tid * 8 + j);
         c[j] = 0;
 #pragma unroll
-        for (int w = 0; w < kCopies; ++w) c[j] += sh.hist[w][bin];
+        for (int w = 0; w < kCopies; ++w) c[j] += sh.hist[bin][w];
         sum += c[j];
       }
       uint32_t inc = sum;
@@ -190,30 +192,36 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) block_select_kernel
   const uint32_t rank = cluster_rank(), parts = cluster_size();
   const long long pair = blockIdx.x / parts;
   const int b = static_cast<int>(pair / p.at.Hkv), g = static_cast<int>(pair % p.at.Hkv);
+  const int gq = lane >> 2, tq = lane & 3;
   // the other blocks' shared memory may be written once they run
-  cluster_arrive();
+  if (parts > 1) cluster_arrive();
   pdl_wait();
+  // the lane's pieces of its query head, on their way beside the context's length: chunk
+  // c = tq + 4 j of 8 elements of [lo | hi]
+  uint4 xq[LOADS];
+  {
+    const uint4* qrow = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + (pair * p.G + gq) * R);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      xq[j] = make_uint4(0, 0, 0, 0);
+      if (gq < p.G) xq[j] = __ldg(qrow + (tq + 4 * j) % (R / 8));
+    }
+  }
   const int L = checked_len(p.seq_lens[b], p.at);
   const int n_blocks = (L + p.block - 1) >> p.block_shift;
   const int n_take = min(p.n_select, n_blocks);
   const bool all = n_take == n_blocks;         // uniform over the cluster
-  cluster_wait();
+  if (parts > 1) cluster_wait();
 
-  const int gq = lane >> 2, tq = lane & 3;
   float q1 = 0.f;                              // sum |q| of one of the kv head's query heads
   if (!all) {
-    // Q as the B operand: chunk c = tq + 4 j of 8 elements is steps 2j, 2j + 1; the
-    // first R of the 2 R elements meet lo with min(q, 0), the others hi with max(q, 0)
+    // Q as the B operand: chunk j is steps 2j, 2j + 1; the first R of the 2 R elements meet
+    // lo with min(q, 0), the others hi with max(q, 0)
     uint32_t qf[STEPS][2];
-    const uint32_t* qrow = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(p.q) +
-                                                             (pair * p.G + gq) * R);
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int e = (tq + 4 * j) * 8;          // element of [lo | hi]
-      const bool up = e >= R;
-      uint4 x = make_uint4(0, 0, 0, 0);
-      if (gq < p.G) x = __ldg(reinterpret_cast<const uint4*>(qrow + (up ? e - R : e) / 2));
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      const bool up = (tq + 4 * j) * 8 >= R;
+      const uint32_t w[4] = {xq[j].x, xq[j].y, xq[j].z, xq[j].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (up) q1 += fabsf(bf16lo(w[i])) + fabsf(bf16hi(w[i]));

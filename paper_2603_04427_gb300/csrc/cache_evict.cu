@@ -36,7 +36,9 @@ constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kBatch = 4;                 // loads of a thread in flight
-constexpr int kCopies = 8;                // of a histogram, so that equal digits of a warp do not queue up
+// Copies of a histogram, next to each other, so that equal digits of a warp meet
+// neither at one address nor in one bank.
+constexpr int kCopies = 2;
 constexpr int kList = 256;                // weights of one bucket that are ranked instead of split further
 constexpr int kHeld = 16384;              // weights of a block that shared memory holds
 
@@ -48,7 +50,7 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 
 struct Shared {
-  uint32_t hist[2][kCopies][256];
+  uint32_t hist[2][256][kCopies];
   uint32_t total[256];
   uint32_t mine[2][256];                   // this block's sum of the copies
   int digit, above, bucket, listed;
@@ -59,6 +61,9 @@ struct Shared {
   int warp[kWarps][3];
 };
 
+// HELD: shared memory holds all of a block's weights (the code that reads the others
+// from the cache, even where none is, took 40 of the 50 instructions of each pass).
+template <bool HELD>
 __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_constant__ EvictParams p) {
   extern __shared__ float held[];          // [min(part, kHeld)] weights
   __shared__ Shared sh;
@@ -109,7 +114,7 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
     for (int j = 0; j < kBatch; ++j)
       if (i0 + j * kThreads < min(to - from, kHeld)) held[i0 + j * kThreads] = x[j];
   }
-  auto weight = [&](int t) { return t - from < kHeld ? held[t - from] : load(t); };
+  auto weight = [&](int t) { return HELD || t - from < kHeld ? held[t - from] : load(t); };
   auto key = [&](int t) { return key_of(weight(t)); };
 
   // the want-th largest
@@ -123,13 +128,13 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
       __syncthreads();
       for (int t = from + tid; t < to; t += kThreads) {
         const uint32_t k = key(t);
-        if ((k ^ edge) >> shift < 256) atomicAdd(&hist[(lane & (kCopies - 1)) * 256 + ((k >> shift) & 255)], 1u);
+        if ((k ^ edge) >> shift < 256) atomicAdd(&hist[((k >> shift) & 255) * kCopies + (lane & (kCopies - 1))], 1u);
       }
       __syncthreads();
       if (tid < 256) {
         uint32_t c = 0;
 #pragma unroll
-        for (int w = 0; w < kCopies; ++w) c += hist[w * 256 + tid];
+        for (int w = 0; w < kCopies; ++w) c += hist[tid * kCopies + ((w + tid) & (kCopies - 1))];
         if (parts == 1) sh.total[tid] = c;
         else sh.mine[flip][tid] = c;
       }
@@ -497,9 +502,10 @@ cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t s) {
   while (cluster < kMaxCluster && p.at.limit > cluster * 4096 && pairs * cluster <= p.num_sms) cluster *= 2;
   const int part = ((p.at.limit + cluster - 1) / cluster + 31) / 32 * 32;
   const size_t smem = static_cast<size_t>(std::min(part, kHeld)) * 4;
-  cudaError_t e = cudaFuncSetAttribute(evict_choose_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeld * 4);
+  auto choose = part <= kHeld ? evict_choose_kernel<true> : evict_choose_kernel<false>;
+  cudaError_t e = cudaFuncSetAttribute(choose, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeld * 4);
   if (e != cudaSuccess) return e;
-  e = launch_cluster(evict_choose_kernel, dim3(static_cast<unsigned>(pairs * cluster)), dim3(kThreads), cluster, smem, s, p);
+  e = launch_cluster(choose, dim3(static_cast<unsigned>(pairs * cluster)), dim3(kThreads), cluster, smem, s, p);
   if (e != cudaSuccess) return e;
   const int kinds = p.k_fmt ? 4 : 3;
   // Blocks of the tokens from slot keep on, of which there are so many at most: one

@@ -412,6 +412,76 @@ __device__ void prefetch_first_chunks(const DecodeParams& p, int lane, int limit
 }
 
 
+// The same for batches of 33 to 128 sequences, four of them a lane (128 sequences of one
+// kv head, 64 pages of 64 tokens each: 35.1 us without, 30.2 with).  Not inlined: the
+// small batches' code stays as it is.
+template <int RB, int DV>
+__device__ __noinline__ void prefetch_first_chunks_wide(const DecodeParams& p, int lane, int limit, int nunits) {
+  const int B = p.B, Hkv = p.Hkv;
+  int L[4];
+  long long x[4], sum = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int b = lane * 4 + i;
+    L[i] = b < B ? p.seq_lens[b] : 0;
+    if (p.fuse_append && b < B && L[i] >= 0) ++L[i];
+    L[i] = min(max(L[i], 0), limit);
+    x[i] = static_cast<long long>((L[i] + kChunk - 1) / kChunk) * Hkv;
+    sum += x[i];
+  }
+  long long inc = sum;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, inc, off);
+    if (lane >= off) inc += y;
+  }
+  const long long T = __shfl_sync(0xffffffffu, inc, 31);
+  const int N = split_ctas(T, gridDim.x);
+  const int c = blockIdx.x;
+  if (T == 0 || c >= N) return;  // warp-uniform
+  const long long u_begin = T * c / N, u_end = T * (c + 1) / N;
+  const long long u = u_begin + lane;
+  // the last lane whose sequences begin at or before u, then the sequence among its four
+  int owner = 0;
+  for (int l = 1; l < 32; ++l)
+    if (__shfl_sync(0xffffffffu, inc - sum, l) <= u) owner = l;
+  long long left = u - __shfl_sync(0xffffffffu, inc - sum, owner);
+  int b = owner * 4, Lb = 0;
+  bool found = false;
+  long long off = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long long xi = __shfl_sync(0xffffffffu, x[i], owner);
+    const int Li = __shfl_sync(0xffffffffu, L[i], owner);
+    if (!found && left < xi) found = true, b = owner * 4 + i, Lb = Li, off = left;
+    left -= xi;
+  }
+  if (!found || lane >= nunits || u >= u_end) return;
+  const int nb = (Lb + kChunk - 1) / kChunk;
+  const int g = static_cast<int>(off / nb), t0 = static_cast<int>(off % nb) * kChunk;
+  long long row;
+  int rows;
+  if (p.page_size == 0) {
+    row = (static_cast<long long>(b) * Hkv + g) * p.capacity + t0;
+    rows = min(kChunk, p.capacity - t0);
+  } else {
+    const int pidx = t0 >> p.page_shift;
+    if (pidx >= p.max_pages) return;
+    const int page = p.page_table[static_cast<long long>(b) * p.max_pages + pidx];
+    if (page < 0 || page >= p.num_pages) return;
+    const int in_page = t0 & (p.page_size - 1);
+    row = (static_cast<long long>(page) * Hkv + g) * p.page_size + in_page;
+    rows = min(kChunk, p.page_size - in_page);
+  }
+  if (rows <= 0) return;
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const unsigned char*>(p.k) + row * RB),
+               "r"(static_cast<uint32_t>(rows * RB))
+               : "memory");
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const unsigned char*>(p.v) + row * DV * 2),
+               "r"(static_cast<uint32_t>(rows * DV * 2))
+               : "memory");
+}
+
 // The grid is persistent (CTAS_PER_SM CTAs on every SM at once): the bound
 // keeps the register count low enough for that many CTAs to be resident.
 template <int R, int DV, int G, int KF>
@@ -451,6 +521,7 @@ decode_kernel(const __grid_constant__ DecodeMaps maps, const DecodeParams p) {
   else limit = min(limit, p.max_pages * p.page_size);
   // before the wait only reads that may be stale and L2 prefetches are issued
   if (warp == kCW && B <= 32) prefetch_first_chunks<C::RB, DV>(p, lane, limit, 2 * C::NSTAGE);
+  else if (warp == kCW && B <= 128) prefetch_first_chunks_wide<C::RB, DV>(p, lane, limit, 2 * C::NSTAGE);
   pdl_wait();
   pdl_trigger();
 

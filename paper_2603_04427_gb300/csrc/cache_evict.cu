@@ -499,7 +499,7 @@ cudaError_t launch_cache_evict(const EvictParams& p, cudaStream_t s) {
   const long long pairs = static_cast<long long>(p.B) * p.at.Hkv;
   // a block of threads for every 4096 tokens, while all run at once
   int cluster = 1;
-  while (cluster < kMaxCluster && p.at.limit > cluster * 4096 && pairs * cluster <= p.num_sms) cluster *= 2;
+  while (cluster < kMaxCluster && p.at.limit > cluster * 4096 && 2 * pairs * cluster <= p.num_sms) cluster *= 2;
   const int part = ((p.at.limit + cluster - 1) / cluster + 31) / 32 * 32;
   const size_t smem = static_cast<size_t>(std::min(part, kHeld)) * 4;
   auto choose = part <= kHeld ? evict_choose_kernel<true> : evict_choose_kernel<false>;

@@ -505,6 +505,9 @@ tk_status tk_block_tables(int32_t batch, int32_t page_size, int32_t num_pages,
  * gets, follow from r of the r + d_v numbers of a token).  What these calls
  * write per slot or page (bounds, weights, an evicted cache) belongs to one
  * sequence: a page must not stand in the page-table rows of two of them.
+ * At most 2^30 tokens of a sequence, batch * h_kv 2^24, 2^34 slots of all kv heads
+ * (fewer than 2^31 for the choice of blocks and the decode over them), else
+ * TK_ERR_UNSUPPORTED.
  * ------------------------------------------------------------------------ */
 
 /* Element-wise minimum and maximum of the cached keys of every block of `block`
@@ -600,8 +603,10 @@ size_t tk_attn_weights_workspace_size(const tk_cache_desc* desc, int32_t n_q, in
  *   weights  : device fp32, one per slot, laid out as k_scale: [batch][h_kv][capacity] or
  *              [num_pages][h_kv][page_size]; slots past seq_lens are not written
  *   workspace: tk_attn_weights_workspace_size bytes, 256-byte aligned
- * Sums in fp32, in an order fixed by the sizes and the device's SM count.  Two
- * launches, with programmatic dependent launch.                              */
+ * Sums in fp32, in an order fixed by the sizes and the device's SM count.  A score
+ * of +infinity or NaN makes its kv head's weights NaN, one of -infinity is a weight
+ * of zero.  One launch (one query, and scores of a context that shared memory holds) or
+ * two, with programmatic dependent launch.                                  */
 tk_status tk_attn_weights(const tk_cache_desc* desc, const void* q, int32_t n_q, const void* k_cache,
                           const float* k_scale, const int32_t* page_table, const int32_t* old_lens,
                           const int32_t* seq_lens, int32_t max_seq_len, float scale, float decay, float* weights,
@@ -633,7 +638,8 @@ size_t tk_cache_evict_workspace_size(const tk_cache_desc* desc, int32_t n_keep);
  *   free_pages, free_count: paged: pages that hold no token any more are pushed
  *              on this stack (see tk_block_tables), in order of sequence and
  *              page, so that tk_block_tables finds a sequence's pages by its
- *              new length; both NULL: the pages stay with the sequence
+ *              new length (which the caller then has to take over); both NULL:
+ *              the pages stay with the sequence
  *   workspace: tk_cache_evict_workspace_size bytes, 256-byte aligned
  * Two launches, with programmatic dependent launch.                          */
 tk_status tk_cache_evict(const tk_cache_desc* desc, void* k_cache, void* v_cache, float* k_scale,

@@ -32,8 +32,8 @@
 // SM quarter).
 #include <algorithm>
 
+#include "attn_weights.cuh"
 #include "cluster.cuh"
-#include "key_frag.cuh"
 #include "kernels.h"
 
 namespace tk {
@@ -211,34 +211,7 @@ struct KeyTiles {
   }
 };
 
-__device__ __forceinline__ void join(float& m, float& l, float m2, float l2) {
-  const float n = fmaxf(m, m2);
-  if (n == -INFINITY) {        // no score yet; a NaN stays
-    l += l2;
-    return;
-  }
-  l = l * fast_exp2(m - n) + l2 * fast_exp2(m2 - n);
-  m = n;
-}
-
 // ---------------------------------------------------------------- two launches
-struct Range {
-  int b, g, L, from, to;
-  long long pair;
-};
-
-__device__ __forceinline__ Range range_of(const WeightsParams& p, long long block, int splits, int per_cta) {
-  Range r;
-  r.pair = block / splits;
-  r.b = static_cast<int>(r.pair / p.at.Hkv);
-  r.g = static_cast<int>(r.pair % p.at.Hkv);
-  r.L = checked_len(p.seq_lens[r.b], p.at);
-  const long long from = block % splits * per_cta;
-  r.from = static_cast<int>(min(from, static_cast<long long>(r.L)));
-  r.to = static_cast<int>(min(from + per_cta, static_cast<long long>(r.L)));
-  return r;
-}
-
 // Tokens of a row of stored scores.
 __device__ __forceinline__ int score_stride(const WeightsParams& p) { return (p.at.limit + 15) & ~15; }
 
@@ -366,50 +339,6 @@ struct Bool {
   static constexpr bool value = V;
 };
 
-// A row's statistics for the second launch: maximum, 1 / sum (0 for a row that
-// sees no token) and the last token that it sees.
-struct RowStat {
-  float m, inv;
-  int see;
-  int pad;
-};
-
-// Joins the ranges' statistics of every row.  A power of two of lanes per row, so
-// that the block's threads share the loads whether rows are few or many.
-__device__ __forceinline__ void join_rows(const WeightsParams& p, const Range& r, int padded, RowStat* stat) {
-  int lanes = 32;
-  while (lanes > 1 && lanes * padded > kThreads) lanes >>= 1;
-  const int splits = (r.L + p.per_cta - 1) / p.per_cta;
-  const int sub = threadIdx.x % lanes;
-  for (int row0 = 0; row0 < padded; row0 += kThreads / lanes) {
-    const int row = row0 + static_cast<int>(threadIdx.x) / lanes;
-    float m = -INFINITY, l = 0.f;
-    if (row < p.rows) {
-      const float2* part = p.part + r.pair * p.splits * p.rows + row;
-      for (int s = sub; s < splits; s += 4 * lanes) {
-        float2 x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          x[i] = s + i * lanes < splits ? __ldcg(part + static_cast<long long>(s + i * lanes) * p.rows) : make_float2(-INFINITY, 0.f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) join(m, l, x[i].x, x[i].y);
-      }
-    }
-    for (int o = 1; o < lanes; o <<= 1) {
-      const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
-      join(m, l, m2, l2);
-    }
-    if (sub == 0 && row < padded) {
-      RowStat x;
-      x.m = m == -INFINITY ? 0.f : m;
-      x.inv = l == 0.f ? 0.f : 1.f / l;
-      x.see = row < p.rows ? r.L - p.n_q + row % p.n_q : -1;
-      x.pad = 0;
-      stat[row] = x;
-    }
-  }
-}
-
 // Second launch, scores computed again.
 template <int R, int KF>
 __global__ void __launch_bounds__(kThreads, 2) weights_sum_kernel(const __grid_constant__ WeightsParams p) {
@@ -436,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 2) weights_sum_kernel(const __grid_c
   Ring ring;
   ring.start(p, rows, dyn, bars, t0, r.to, warp, lane);
   stage_queries<R, KF>(p, r.pair, 0, tiles, sq);
-  join_rows(p, r, tiles * 16, stat);
+  join_rows<kThreads>(p, r, tiles * 16, stat);
   __syncthreads();
   const float u = unit<KF>(p);
   const int old = p.decay == 0.f ? 0 : (p.old_lens ? p.old_lens[r.b] : 0);
@@ -567,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, ROWS <= 4 ? 4 : 2) weights_join_kern
   int t = r.from + 4 * static_cast<int>(threadIdx.x);
   find(t);
   if (t < r.to) load(t);
-  join_rows(p, r, 8, stat);
+  join_rows<kThreads>(p, r, 8, stat);
   __syncthreads();
   float m[ROWS], inv[ROWS];
 #pragma unroll
@@ -833,7 +762,7 @@ size_t plan_weights(WeightsParams* p, int num_sms) {
   const long long pairs = static_cast<long long>(p->B) * p->at.Hkv, limit = std::max(p->at.limit, 1);
   p->per_cta = p->sum_per_cta = 16;
   p->splits = p->sum_splits = 1;
-  p->store = p->fused = 0;
+  p->store = p->fused = p->tensor = 0;
   if (p->n_q == 1) {
     // blocks of a cluster: as many as run at once (two on every SM) and have 512
     // tokens each, or more for the scores to fit
@@ -843,6 +772,19 @@ size_t plan_weights(WeightsParams* p, int num_sms) {
       p->fused = parts;
       return 0;
     }
+  }
+  if (weights_on_tcgen05(*p)) {
+    // one block an SM: tiles of 128 tokens for a tile of 128 rows, or for all rows
+    p->tensor = 1;
+    auto tiles = [&](long long copies) {
+      const long long splits = std::max(1ll, num_sms / (pairs * copies));
+      return static_cast<int>(((limit + splits - 1) / splits + 127) / 128 * 128);
+    };
+    p->per_cta = tiles((p->rows + 127) / 128);
+    p->sum_per_cta = tiles(1);
+    p->splits = static_cast<int>((limit + p->per_cta - 1) / p->per_cta);
+    p->sum_splits = static_cast<int>((limit + p->sum_per_cta - 1) / p->sum_per_cta);
+    return (static_cast<size_t>(pairs) * p->splits * p->rows * sizeof(float2) + 255) / 256 * 256;
   }
   // as many blocks as run at once, each warp with at least one stage of keys
   const int step = kWarps * 8 * (p->R <= 32 ? 8 : (p->R == 64 ? 4 : 2));
@@ -862,6 +804,7 @@ size_t plan_weights(WeightsParams* p, int num_sms) {
 }
 
 cudaError_t launch_attn_weights(const WeightsParams& p, cudaStream_t s, int* unsupported) {
+  if (p.tensor) return launch_attn_weights_tc(p, s);
 #define TK_CASE(R_, K_) if (p.R == R_ && p.k_fmt == K_) return launch_t<R_, K_>(p, s);
   TK_CASE(16, 0) TK_CASE(32, 0) TK_CASE(64, 0) TK_CASE(128, 0)
   TK_CASE(16, 1) TK_CASE(32, 1) TK_CASE(64, 1) TK_CASE(128, 1)

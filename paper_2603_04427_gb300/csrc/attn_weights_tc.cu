@@ -1,0 +1,420 @@
+// Accumulated attention weights of many queries (attn_weights.cu), products on tcgen05.
+//
+// Two launches that both compute the scores, as there: the first with query rows as the
+// MMA's M, so that a thread owns a row (a TMEM lane) and its maximum and sum need no other
+// thread; the second with tokens as M, so that a thread owns a token and adds up its
+// weights over the rows, whose (maximum, 1 / sum) it reads from shared memory.  Either
+// way the operands are K-major tiles of the same layout, keys and queries just change
+// places in the instruction.
+//
+// mma.sync takes 18 cycles a product and SM quarter here and set the time of the form
+// that uses it (r = 64); on tcgen05 a tile of 128 x 128 scores takes about 130 cycles
+// (r = 64), and the exponentials, 128 x 128 for each of the launches, are what is left.
+//
+// One block per SM.  Warps 0-3 and 4-7: two groups of softmax threads, tiles in turn;
+// warp 8: TMA of key tiles into a ring; warp 9: the products.  Scores pass through TMEM
+// buffers of 128 columns: a group copies one into registers and gives it back before it
+// works on it.
+#include <algorithm>
+
+#include "attn_weights.cuh"
+#include "kernels.h"
+#include "tc05.cuh"
+
+namespace tk {
+namespace {
+
+constexpr int kThreads = 320;
+constexpr int kTile = 128;
+
+template <int R>
+struct TCfg {
+  static constexpr int SW = 2 * R < 128 ? 2 * R : 128;       // swizzle span
+  static constexpr int BOX = SW / 2;                         // elements of a box row
+  static constexpr int NBOX = 2 * R / SW;                    // boxes of a tile
+  static constexpr int BOXB = kTile * SW;                    // bytes of a box
+  static constexpr int TILEB = kTile * R * 2;                // bytes of a tile of 128 rows
+  static constexpr uint32_t LAYOUT = SW == 32 ? 6u : (SW == 64 ? 4u : 2u);
+  static constexpr int STEPS_PER_BOX = SW / 32;
+  static constexpr uint32_t IDESC = instr_desc(kTile, kTile, false);
+};
+
+struct WeightMaps {
+  CUtensorMap q, k;
+};
+
+// Key tile j of the range (128 tokens) into `dst`: one box, or one for each page.
+template <int R>
+__device__ __forceinline__ void load_keys(const WeightMaps& maps, const WeightsParams& p, const Range& r, int t0,
+                                          unsigned char* dst, uint64_t* bar, int lane) {
+  using T = TCfg<R>;
+  const SlotMap& m = p.at;
+  const int rows_per_box = m.page_size == 0 || m.page_size >= kTile ? kTile : m.page_size;
+  int plane = r.b * m.Hkv + r.g, row = t0;
+  if (m.page_size != 0) {
+    const int t = t0 + lane * rows_per_box;
+    int page = -1;                         // past the context: the zero fill
+    if (lane < kTile / rows_per_box && t < r.L) {
+      page = m.page_table[static_cast<long long>(r.b) * m.max_pages + (t >> m.page_shift)];
+      if (page < 0 || page >= m.num_pages) {
+        record_error(m.err, TK_DEVERR_INDEX);
+        page = -1;
+      }
+    }
+    plane = page < 0 ? -1 : page * m.Hkv + r.g;
+    row = t & (m.page_size - 1);
+  }
+  if (lane == 0) mbar_arrive_expect_tx(bar, T::TILEB);
+  __syncwarp();
+  if (lane < kTile / rows_per_box) {
+#pragma unroll
+    for (int i = 0; i < T::NBOX; ++i)
+      tma_load_3d(dst + i * T::BOXB + lane * rows_per_box * T::SW, &maps.k, i * T::BOX, row, plane, bar);
+  }
+}
+
+// 128 x 128 scores: rows of a, columns of b, both tiles of 128 rows in shared memory.
+template <int R>
+__device__ __forceinline__ void scores(uint32_t d, const Desc& a, uint32_t ao, const Desc& b, uint32_t bo) {
+  using T = TCfg<R>;
+#pragma unroll
+  for (int k = 0; k < R / 16; ++k) {
+    const uint32_t off = (k / T::STEPS_PER_BOX) * T::BOXB + (k % T::STEPS_PER_BOX) * 32;
+    mma_ss_e(d, a.at(ao + off), b.at(bo + off), T::IDESC, k > 0);
+  }
+}
+
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* err) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, err));
+}
+
+__device__ __forceinline__ float f(uint32_t x) { return __uint_as_float(x); }
+
+// ---------------------------------------------------------------- first launch
+template <int R>
+struct StatCfg {
+  static constexpr int NST = R == 128 ? 3 : 4;               // stages of keys
+  static constexpr int OFF_K = TCfg<R>::TILEB;
+  static constexpr int SMEM = OFF_K + NST * TCfg<R>::TILEB + 1024;
+};
+
+template <int R>
+__global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __grid_constant__ WeightMaps maps,
+                                                                       const __grid_constant__ WeightsParams p) {
+  using T = TCfg<R>;
+  constexpr int NST = StatCfg<R>::NST;
+  extern __shared__ unsigned char raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  __shared__ uint64_t q_full, k_full[NST], k_empty[NST], s_full[2], s_empty[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ float2 other[kTile];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    mbar_init(&q_full, 1);
+    for (int i = 0; i < NST; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
+    for (int i = 0; i < 2; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_empty[i], 128);
+    fence_barrier_init();
+  }
+  if (warp == 8) {
+    tmem_alloc(&tmem_slot, 2 * kTile);
+    tmem_relinquish();
+  }
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  pdl_wait();
+  pdl_trigger();
+  const int row_tiles = (p.rows + kTile - 1) / kTile;
+  const int c = static_cast<int>(blockIdx.x % row_tiles);
+  const long long block = blockIdx.x / row_tiles;
+  const Range r = range_of(p, block, p.splits, p.per_cta);
+  const int tiles = (r.to - r.from + kTile - 1) / kTile;      // 0 past the context's end
+  float m = -INFINITY, l = 0.f;
+
+  if (warp == 8) {
+    if (tiles > 0) {
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&q_full, T::TILEB);
+        for (int i = 0; i < T::NBOX; ++i)
+          tma_load_3d(smem + i * T::BOXB, &maps.q, i * T::BOX, c * kTile, static_cast<int>(r.pair), &q_full);
+      }
+      int j = 0;
+      for (; j < tiles; ++j) {
+        const int st = j % NST;
+        if (j >= NST && !warp_wait(&k_empty[st], (j / NST - 1) & 1, p.at.err)) break;
+        load_keys<R>(maps, p, r, r.from + j * kTile, smem + StatCfg<R>::OFF_K + st * T::TILEB, &k_full[st], lane);
+      }
+      // every copy has landed before the block ends
+      warp_wait(&q_full, 0, p.at.err);
+      for (int i = max(0, j - NST); i < j; ++i) warp_wait(&k_full[i % NST], (i / NST) & 1, p.at.err);
+      // and so have the products' arrivals
+      for (int i = max(0, j - NST); i < j; ++i) warp_wait(&k_empty[i % NST], (i / NST) & 1, p.at.err);
+    }
+  } else if (warp == 9) {
+    const Desc dq = make_desc(smem_addr(smem), 16, 8 * T::SW, T::LAYOUT);
+    const Desc dk = make_desc(smem_addr(smem + StatCfg<R>::OFF_K), 16, 8 * T::SW, T::LAYOUT);
+    bool ok = tiles > 0 && warp_wait(&q_full, 0, p.at.err);
+    for (int j = 0; ok && j < tiles; ++j) {
+      const int st = j % NST, x = j & 1, use = j >> 1;
+      ok = warp_wait(&k_full[st], (j / NST) & 1, p.at.err);
+      if (ok && use > 0) ok = warp_wait(&s_empty[x], (use - 1) & 1, p.at.err);
+      if (!ok) break;
+      tc_fence_after();
+      scores<R>(tmem + x * kTile, dq, 0, dk, st * T::TILEB);
+      tc_commit_e(&s_full[x]);
+      tc_commit_e(&k_empty[st]);
+    }
+  } else {
+    const int x = warp >> 2;               // group
+    const int row = c * kTile + (tid & 127);
+    const int see = min(r.to - 1, r.L - p.n_q + row % p.n_q);   // the last token that the row sees
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const float u = p.unit;
+    const float sign = p.scale_log2 < 0.f ? -1.f : (p.scale_log2 == 0.f ? 0.f : 1.f);
+    for (int j = x; j < tiles; j += 2) {
+      if (!warp_wait(&s_full[x], (j >> 1) & 1, p.at.err)) break;
+      tc_fence_after();
+      // half a tile at a time: 64 registers of scores
+#pragma unroll 1
+      for (int h = 0; h < kTile; h += 64) {
+        uint32_t v[64];
+        tmem_ld64(tmem + x * kTile + h + lanes, v);
+        if (h != 0) {
+          tc_fence_before();
+          mbar_arrive(&s_empty[x]);
+        }
+        const int t0 = r.from + j * kTile + h;
+        if (sign != 1.f) {
+#pragma unroll
+          for (int i = 0; i < 64; ++i) v[i] = __float_as_uint(f(v[i]) * sign);
+        }
+        if (t0 + 64 > r.L - p.n_q + 1) {
+#pragma unroll
+          for (int i = 0; i < 64; ++i)
+            if (t0 + i > see) v[i] = 0xff800000u;
+        }
+        float a[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = f(v[i]);
+#pragma unroll
+        for (int i = 8; i < 64; ++i) a[i & 7] = fmaxf(a[i & 7], f(v[i]));
+        const float n = fmaxf(m, fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7]))));
+        // no score above -inf: exponentials of zero maximum, which a NaN survives
+        const float z = n == -INFINITY ? 0.f : -n * u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) a[i & 7] += fast_exp2(fmaf(f(v[i]), u, z));
+        l = fmaf(l, fast_exp2(fmaf(m, u, z)), ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7])));
+        m = n;
+      }
+    }
+    m *= u;                                // log2 units from here on
+    if (x == 1) other[tid & 127] = make_float2(m, l);
+  }
+  __syncthreads();
+  if (warp < 4 && tiles > 0) {
+    join(m, l, other[tid].x, other[tid].y);
+    const int row = c * kTile + tid;
+    if (row < p.rows) p.part[block * p.rows + row] = make_float2(m, l);
+  }
+  if (warp == 8) tmem_dealloc(tmem, 2 * kTile);
+}
+
+// ---------------------------------------------------------------- second launch
+template <int R>
+struct SumCfg {
+  static constexpr int NST = R == 128 ? 2 : 4;
+  // query tiles, key stages, statistics of a row: (maximum, 1 / sum) and the last token
+  static constexpr int smem(int row_tiles) { return (row_tiles + NST) * TCfg<R>::TILEB + row_tiles * kTile * 12 + 1024; }
+};
+
+template <int R>
+__global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __grid_constant__ WeightMaps maps,
+                                                                     const __grid_constant__ WeightsParams p) {
+  using T = TCfg<R>;
+  constexpr int NST = SumCfg<R>::NST;
+  extern __shared__ unsigned char raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  __shared__ uint64_t q_full, k_full[NST], k_empty[NST], s_full[4], s_empty[4];
+  __shared__ uint32_t tmem_slot;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int row_tiles = (p.rows + kTile - 1) / kTile;
+  unsigned char* sk = smem + row_tiles * T::TILEB;
+  float2* stat = reinterpret_cast<float2*>(sk + NST * T::TILEB);
+  int* see = reinterpret_cast<int*>(stat + row_tiles * kTile);
+  if (tid == 0) {
+    mbar_init(&q_full, 1);
+    for (int i = 0; i < NST; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
+    for (int i = 0; i < 4; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_empty[i], 128);
+    fence_barrier_init();
+  }
+  if (warp == 8) {
+    tmem_alloc(&tmem_slot, 4 * kTile);
+    tmem_relinquish();
+  }
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  pdl_wait();
+  pdl_trigger();
+  const Range r = range_of(p, blockIdx.x, p.sum_splits, p.sum_per_cta);
+  const int tiles = (r.to - r.from + kTile - 1) / kTile;
+  // item n of group x: tile 2 (n / row_tiles) + x with rows n % row_tiles, in buffer 2 x + (n & 1)
+  if (warp == 8) {
+    if (tiles > 0) {
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&q_full, row_tiles * T::TILEB);
+        for (int c = 0; c < row_tiles; ++c)
+          for (int i = 0; i < T::NBOX; ++i)
+            tma_load_3d(smem + c * T::TILEB + i * T::BOXB, &maps.q, i * T::BOX, c * kTile, static_cast<int>(r.pair), &q_full);
+      }
+      int j = 0;
+      for (; j < tiles; ++j) {
+        const int st = j % NST;
+        if (j >= NST && !warp_wait(&k_empty[st], (j / NST - 1) & 1, p.at.err)) break;
+        load_keys<R>(maps, p, r, r.from + j * kTile, sk + st * T::TILEB, &k_full[st], lane);
+      }
+      warp_wait(&q_full, 0, p.at.err);
+      for (int i = max(0, j - NST); i < j; ++i) warp_wait(&k_full[i % NST], (i / NST) & 1, p.at.err);
+      // and so have the products' arrivals
+      for (int i = max(0, j - NST); i < j; ++i) warp_wait(&k_empty[i % NST], (i / NST) & 1, p.at.err);
+    }
+  } else if (warp == 9) {
+    const Desc dq = make_desc(smem_addr(smem), 16, 8 * T::SW, T::LAYOUT);
+    const Desc dk = make_desc(smem_addr(sk), 16, 8 * T::SW, T::LAYOUT);
+    bool ok = tiles > 0 && warp_wait(&q_full, 0, p.at.err);
+    for (int j0 = 0; ok && j0 < tiles; j0 += 2) {
+      for (int c = 0; ok && c < row_tiles; ++c) {
+        for (int x = 0; ok && x < 2 && j0 + x < tiles; ++x) {
+          const int j = j0 + x, st = j % NST;
+          const int n = (j0 >> 1) * row_tiles + c, buf = 2 * x + (n & 1), use = n >> 1;
+          if (c == 0) ok = warp_wait(&k_full[st], (j / NST) & 1, p.at.err);
+          if (ok && use > 0) ok = warp_wait(&s_empty[buf], (use - 1) & 1, p.at.err);
+          if (!ok) break;
+          tc_fence_after();
+          scores<R>(tmem + buf * kTile, dk, st * T::TILEB, dq, c * T::TILEB);
+          tc_commit_e(&s_full[buf]);
+          if (c == row_tiles - 1) tc_commit_e(&k_empty[st]);
+        }
+      }
+    }
+  } else {
+    // statistics of every row, by the softmax threads
+    if (tiles > 0) {
+      const int splits = (r.L + p.per_cta - 1) / p.per_cta;
+      for (int row = tid; row < row_tiles * kTile; row += 256) {
+        float m = -INFINITY, l = 0.f;
+        if (row < p.rows) {
+          const float2* part = p.part + r.pair * p.splits * p.rows + row;
+          for (int s0 = 0; s0 < splits; s0 += 4) {
+            float2 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              x[i] = s0 + i < splits ? __ldcg(part + static_cast<long long>(s0 + i) * p.rows) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) join(m, l, x[i].x, x[i].y);
+          }
+        }
+        stat[row] = make_float2(m == -INFINITY ? 0.f : -m, l == 0.f ? 0.f : 1.f / l);
+        see[row] = row < p.rows ? r.L - p.n_q + row % p.n_q : -1;
+      }
+    }
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    const int x = warp >> 2;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const float u = p.scale_log2;          // scores as they are: signed
+    const int old = p.decay == 0.f ? 0 : (p.old_lens ? p.old_lens[r.b] : 0);
+    int n = 0;
+    bool ok = true;
+    for (int j = x; ok && j < tiles; j += 2) {
+      const int t0 = r.from + j * kTile, t = t0 + (tid & 127);
+      const long long at = t < r.to ? slot_row_or_none(p.at, r.b, r.g, t) : -1;
+      const float before = at >= 0 && t < old ? p.decay * p.w[at] : 0.f;
+      const bool masked = t0 + kTile > r.L - p.n_q + 1;
+      float sum = 0.f;
+      for (int c = 0; c < row_tiles; ++c, ++n) {
+        const int buf = 2 * x + (n & 1);
+        ok = warp_wait(&s_full[buf], (n >> 1) & 1, p.at.err);
+        if (!ok) break;
+        tc_fence_after();
+        const float4* st = reinterpret_cast<const float4*>(stat + c * kTile);
+        const bool all = !masked && (c + 1) * kTile <= p.rows;
+        float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
+#pragma unroll 1
+        for (int h = 0; h < kTile; h += 64) {
+          uint32_t v[64];
+          tmem_ld64(tmem + buf * kTile + h + lanes, v);
+          if (h != 0) {
+            tc_fence_before();
+            mbar_arrive(&s_empty[buf]);
+          }
+          if (all) {
+#pragma unroll
+            for (int i = 0; i < 64; i += 4) {
+              const float4 y = st[(h + i) / 2], w = st[(h + i) / 2 + 1];
+              a0 = fmaf(fast_exp2(fmaf(f(v[i]), u, y.x)), y.y, a0);
+              a1 = fmaf(fast_exp2(fmaf(f(v[i + 1]), u, y.z)), y.w, a1);
+              a2 = fmaf(fast_exp2(fmaf(f(v[i + 2]), u, w.x)), w.y, a2);
+              a3 = fmaf(fast_exp2(fmaf(f(v[i + 3]), u, w.z)), w.w, a3);
+            }
+          } else {
+            // rows that do not see the token, and those past the last (whose zeros may
+            // meet an infinite key)
+            const int* last = see + c * kTile + h;
+#pragma unroll
+            for (int i = 0; i < 64; i += 2) {
+              const float4 y = st[(h + i) / 2];
+              const float b0 = fast_exp2(fmaf(f(v[i]), u, y.x)) * y.y;
+              const float b1 = fast_exp2(fmaf(f(v[i + 1]), u, y.z)) * y.w;
+              a0 += t > last[i] ? 0.f : b0;
+              a1 += t > last[i + 1] ? 0.f : b1;
+            }
+          }
+        }
+        sum += (a0 + a1) + (a2 + a3);
+      }
+      if (ok && at >= 0) p.w[at] = before + sum;
+    }
+  }
+  __syncthreads();
+  if (warp == 8) tmem_dealloc(tmem, 4 * kTile);
+}
+
+template <int R>
+cudaError_t launch_t(const WeightsParams& p, cudaStream_t s) {
+  using T = TCfg<R>;
+  const int pairs = p.B * p.at.Hkv;
+  const bool paged = p.at.page_size != 0;
+  WeightMaps maps;
+  if (!make_map(&maps.q, p.q, R, p.rows, pairs, T::BOX, kTile, T::SW) ||
+      !make_map(&maps.k, p.k, R, paged ? p.at.page_size : p.at.capacity, (paged ? p.at.num_pages : p.B) * p.at.Hkv, T::BOX,
+                paged ? std::min(p.at.page_size, kTile) : kTile, T::SW))
+    return cudaErrorInvalidValue;
+  const int row_tiles = (p.rows + kTile - 1) / kTile;
+  cudaError_t e = cudaFuncSetAttribute(weights_stats_tc_kernel<R>, cudaFuncAttributeMaxDynamicSharedMemorySize, StatCfg<R>::SMEM);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(weights_stats_tc_kernel<R>, dim3(static_cast<unsigned>(static_cast<long long>(pairs) * p.splits * row_tiles)),
+                 dim3(kThreads), StatCfg<R>::SMEM, s, maps, p);
+  if (e != cudaSuccess) return e;
+  constexpr int kMost = SumCfg<R>::smem(kMaxWeightRows / kTile);
+  static_assert(kMost <= 226 * 1024, "shared memory");
+  e = cudaFuncSetAttribute(weights_sum_tc_kernel<R>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(weights_sum_tc_kernel<R>, dim3(static_cast<unsigned>(static_cast<long long>(pairs) * p.sum_splits)),
+                    dim3(kThreads), static_cast<size_t>(SumCfg<R>::smem(row_tiles)), s, maps, p);
+}
+
+}  // namespace
+
+// Keys in bf16 as the MMA takes them, and enough rows for half of its tile.
+bool weights_on_tcgen05(const WeightsParams& p) {
+  const long long planes = static_cast<long long>(p.at.page_size ? p.at.num_pages : p.B) * p.at.Hkv;
+  return p.k_fmt == 0 && p.n_q > 1 && p.rows >= 64 && p.R >= 64 && planes < (1ll << 31);
+}
+
+cudaError_t launch_attn_weights_tc(const WeightsParams& p, cudaStream_t s) {
+  return p.R == 64 ? launch_t<64>(p, s) : launch_t<128>(p, s);
+}
+
+}  // namespace tk

@@ -67,6 +67,7 @@ struct WeightsParams {
   int rows;                 // G * n_q
   // set by plan_weights
   int fused;                // blocks of a cluster of the one-launch form, or 0
+  int tensor;               // many queries: products on tcgen05
   int per_cta, splits;      // first of two launches: tokens of a block, blocks of a (sequence, kv head)
   int sum_per_cta, sum_splits;   // second launch
   int store;                // the scores go through the workspace instead of being computed twice
@@ -78,6 +79,8 @@ constexpr int kMaxWeightRows = 512;
 // Fills the plan and returns the workspace's bytes.
 size_t plan_weights(WeightsParams* p, int num_sms);
 cudaError_t launch_attn_weights(const WeightsParams& p, cudaStream_t stream, int* unsupported);
+bool weights_on_tcgen05(const WeightsParams& p);
+cudaError_t launch_attn_weights_tc(const WeightsParams& p, cudaStream_t stream);
 
 struct EvictParams {
   SlotMap at;

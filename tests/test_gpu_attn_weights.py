@@ -92,6 +92,75 @@ def test_many_queries(G, n):
     _check(x, _queries(3, 2 * G, n, 32, n), [0, 650, 64], 0.5)
 
 
+@pytest.mark.parametrize("r,G,n,ps,cap", [
+    (64, 4, 16, 0, 1312), (64, 4, 32, 16, 1536), (64, 1, 65, 64, 1536), (64, 8, 64, 128, 1536), (64, 2, 200, 256, 1536),
+    (128, 2, 32, 0, 1328), (128, 8, 64, 32, 1536), (128, 4, 33, 128, 1536), (128, 4, 100, 0, 1504)])
+def test_tiles_of_many_queries(r, G, n, ps, cap):
+    """From 64 rows of bf16 keys on: products of 128 x 128 tiles.  Contexts of less than a tile,
+    of one, and that end inside one; rows that see nothing; row tiles that are not full."""
+    lens = [0, 1, 63, 127, 128, 129, 640, 1000, 1300]
+    x = Cache(lens, 2 * G, 2, r, 64, cap, ps, "bf16", seed=r + n)
+    q = _queries(x.B, x.h_q, n, r, G)
+    _check(x, q)
+    _check(x, q, [max(0, L - n) for L in lens], 0.9, scale=-0.2)
+    w = _check(x, q, scale=0.0)
+    assert torch.isfinite(w.view(-1)[torch.from_numpy(x.rows(8, 1)).cuda()]).all()
+
+
+@pytest.mark.parametrize("B,G,n,L,ps", [(1, 4, 32, 40001, 64), (40, 4, 16, 1500, 0), (2, 8, 64, 9001, 16)])
+def test_tiles_of_many_queries_in_long_ranges(B, G, n, L, ps):
+    """Rings and score buffers that are used more than once, more pairs than processors."""
+    lens = [L - 37 * i for i in range(B)]
+    x = Cache(lens, 4 * G, 4, 64, 64, (L + 255) // 256 * 256, ps, "bf16", seed=n + B)
+    _check(x, _queries(B, 4 * G, n, 64, B, size=2.0))
+
+
+def test_tiles_of_many_queries_infinities_nans_and_bad_pages():
+    x = Cache([300, 300], 4, 2, 64, 64, 304, 16, "bf16", seed=31)
+    q, ws = _queries(2, 4, 40, 64, 13), tb.attn_weights_workspace(x.c, 300, 40)
+    keys = x.c.k.view(-1, 64)
+    saved = keys.clone()
+    _check(x, q)
+    keys[int(x.rows(0, 0)[50]), 3] = float("nan")
+    keys[int(x.rows(1, 1)[60]), 3] = float("inf")
+    w = tb.slot_weights(x.c)
+    tb.tk_attn_weights(x.c, q, x.seq, 300, w, ws)
+    flat = w.view(-1).cpu().numpy()
+    assert all(np.isfinite(flat[x.rows(b, g)]).all() == (b != g) for b in range(2) for g in range(2))
+    keys.copy_(saved)
+    # a key that scores -inf has no weight, and the others have theirs
+    keys[int(x.rows(0, 0)[7]), 0] = float("-inf")
+    tb.tk_attn_weights(x.c, q.abs(), x.seq, 300, w, ws)
+    got = w.view(-1).cpu().numpy()[x.rows(0, 0)]
+    assert got[7] == 0 and np.isfinite(got).all() and abs(got.sum() / 80 - 1) < 1e-5
+    keys.copy_(saved)
+    x.c.page_table[0, 1] = 1 << 20
+    w.zero_()
+    tb.tk_attn_weights(x.c, q, x.seq, 300, w, ws)
+    assert tb.tk_get_device_error() == 1
+    other = np.ones(w.numel(), bool)
+    other[np.concatenate([x.rows(0, g)[i] for g in range(2) for i in (slice(16), slice(32, None))] + [x.rows(1, 0), x.rows(1, 1)])] = False
+    assert (w.view(-1).cpu().numpy()[other] == 0).all()
+
+
+def test_tiles_of_many_queries_the_same_bits_again_and_through_a_graph():
+    x = Cache([3000, 777], 8, 2, 64, 64, 3008, 0, "bf16", seed=14)
+    q = _queries(2, 8, 24, 64, 12)
+    s = torch.cuda.Stream()
+    ws = tb.attn_weights_workspace(x.c, 3000, 24)
+    a, b = tb.slot_weights(x.c), tb.slot_weights(x.c)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        call = tb.prepare_attn_weights(x.c, q, x.seq, 3000, a, ws, x.seq, stream=s, graph=True)
+        for _ in range(3):
+            call()
+    s.synchronize()
+    for _ in range(4):
+        tb.tk_attn_weights(x.c, q, x.seq, 3000, b, ws, x.seq)
+    torch.cuda.synchronize()
+    assert torch.equal(bits(a), bits(b)) and a.sum() > 0
+
+
 @pytest.mark.parametrize("k,r,G", [("bf16", 32, 4), ("bf16", 64, 8), ("bf16", 32, 1), ("int8", 64, 2)])
 def test_scores_kept_in_the_workspace(k, r, G):
     """Keys beyond what the L2 holds: the other form of the second launch."""

@@ -11,10 +11,10 @@
 // that uses it (r = 64); on tcgen05 a tile of 128 x 128 scores takes about 130 cycles
 // (r = 64), and the exponentials, 128 x 128 for each of the launches, are what is left.
 //
-// One block per SM.  Warps 0-3 and 4-7: two groups of softmax threads, tiles in turn;
-// warp 8: TMA of key tiles into a ring; warp 9: the products.  Scores pass through TMEM
-// buffers of 128 columns: a group copies one into registers and gives it back before it
-// works on it.
+// One block per SM.  Sixteen warps of softmax threads: two groups that take tiles in turn,
+// each in two halves of 64 columns; one warp for the TMA of key tiles into a ring, one for
+// the products.  Scores pass through TMEM buffers of 128 columns, two for each group: its
+// threads copy one into registers and give it back before they work on it.
 #include <algorithm>
 
 #include "attn_weights.cuh"
@@ -24,8 +24,12 @@
 namespace tk {
 namespace {
 
-constexpr int kThreads = 320;
 constexpr int kTile = 128;
+constexpr int kHalf = kTile / 2;
+constexpr int kSoft = 512;                // softmax threads
+constexpr int kLoadWarp = kSoft / 32, kMmaWarp = kLoadWarp + 1;
+constexpr int kThreads = kSoft + 64;
+constexpr int kBufs = 4;
 
 template <int R>
 struct TCfg {
@@ -105,18 +109,18 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
   constexpr int NST = StatCfg<R>::NST;
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  __shared__ uint64_t q_full, k_full[NST], k_empty[NST], s_full[2], s_empty[2];
+  __shared__ uint64_t q_full, k_full[NST], k_empty[NST], s_full[kBufs], s_empty[kBufs];
   __shared__ uint32_t tmem_slot;
-  __shared__ float2 other[kTile];
+  __shared__ float2 other[3][kTile];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     mbar_init(&q_full, 1);
     for (int i = 0; i < NST; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
-    for (int i = 0; i < 2; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_empty[i], 128);
+    for (int i = 0; i < kBufs; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_empty[i], kSoft / 2);
     fence_barrier_init();
   }
-  if (warp == 8) {
-    tmem_alloc(&tmem_slot, 2 * kTile);
+  if (warp == kLoadWarp) {
+    tmem_alloc(&tmem_slot, kBufs * kTile);
     tmem_relinquish();
   }
   __syncthreads();
@@ -131,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
   const int tiles = (r.to - r.from + kTile - 1) / kTile;      // 0 past the context's end
   float m = -INFINITY, l = 0.f;
 
-  if (warp == 8) {
+  if (warp == kLoadWarp) {
     if (tiles > 0) {
       if (lane == 0) {
         mbar_arrive_expect_tx(&q_full, T::TILEB);
@@ -150,12 +154,12 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
       // and so have the products' arrivals
       for (int i = max(0, j - NST); i < j; ++i) warp_wait(&k_empty[i % NST], (i / NST) & 1, p.at.err);
     }
-  } else if (warp == 9) {
+  } else if (warp == kMmaWarp) {
     const Desc dq = make_desc(smem_addr(smem), 16, 8 * T::SW, T::LAYOUT);
     const Desc dk = make_desc(smem_addr(smem + StatCfg<R>::OFF_K), 16, 8 * T::SW, T::LAYOUT);
     bool ok = tiles > 0 && warp_wait(&q_full, 0, p.at.err);
     for (int j = 0; ok && j < tiles; ++j) {
-      const int st = j % NST, x = j & 1, use = j >> 1;
+      const int st = j % NST, x = j % kBufs, use = j / kBufs;   // of the group j & 1
       ok = warp_wait(&k_full[st], (j / NST) & 1, p.at.err);
       if (ok && use > 0) ok = warp_wait(&s_empty[x], (use - 1) & 1, p.at.err);
       if (!ok) break;
@@ -165,60 +169,55 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
       tc_commit_e(&k_empty[st]);
     }
   } else {
-    const int x = warp >> 2;               // group
+    const int x = warp >> 2 & 1, h = (warp >> 3) * kHalf;      // group, first column
     const int row = c * kTile + (tid & 127);
     const int see = min(r.to - 1, r.L - p.n_q + row % p.n_q);   // the last token that the row sees
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const float u = p.unit;
     const float sign = p.scale_log2 < 0.f ? -1.f : (p.scale_log2 == 0.f ? 0.f : 1.f);
     for (int j = x; j < tiles; j += 2) {
-      if (!warp_wait(&s_full[x], (j >> 1) & 1, p.at.err)) break;
+      const int buf = j % kBufs;
+      if (!warp_wait(&s_full[buf], (j / kBufs) & 1, p.at.err)) break;
       tc_fence_after();
-      // half a tile at a time: 64 registers of scores
-#pragma unroll 1
-      for (int h = 0; h < kTile; h += 64) {
-        uint32_t v[64];
-        tmem_ld64(tmem + x * kTile + h + lanes, v);
-        if (h != 0) {
-          tc_fence_before();
-          mbar_arrive(&s_empty[x]);
-        }
-        const int t0 = r.from + j * kTile + h;
-        if (sign != 1.f) {
+      uint32_t v[kHalf];
+      tmem_ld64(tmem + buf * kTile + h + lanes, v);
+      tc_fence_before();
+      mbar_arrive(&s_empty[buf]);
+      const int t0 = r.from + j * kTile + h;
+      if (sign != 1.f) {
 #pragma unroll
-          for (int i = 0; i < 64; ++i) v[i] = __float_as_uint(f(v[i]) * sign);
-        }
-        if (t0 + 64 > r.L - p.n_q + 1) {
-#pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (t0 + i > see) v[i] = 0xff800000u;
-        }
-        float a[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = f(v[i]);
-#pragma unroll
-        for (int i = 8; i < 64; ++i) a[i & 7] = fmaxf(a[i & 7], f(v[i]));
-        const float n = fmaxf(m, fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7]))));
-        // no score above -inf: exponentials of zero maximum, which a NaN survives
-        const float z = n == -INFINITY ? 0.f : -n * u;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 64; ++i) a[i & 7] += fast_exp2(fmaf(f(v[i]), u, z));
-        l = fmaf(l, fast_exp2(fmaf(m, u, z)), ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7])));
-        m = n;
+        for (int i = 0; i < kHalf; ++i) v[i] = __float_as_uint(f(v[i]) * sign);
       }
+      if (t0 + kHalf > r.L - p.n_q + 1) {
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i)
+          if (t0 + i > see) v[i] = 0xff800000u;
+      }
+      float a[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = f(v[i]);
+#pragma unroll
+      for (int i = 8; i < kHalf; ++i) a[i & 7] = fmaxf(a[i & 7], f(v[i]));
+      const float n = fmaxf(m, fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7]))));
+      // no score above -inf: exponentials of zero maximum, which a NaN survives
+      const float z = n == -INFINITY ? 0.f : -n * u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kHalf; ++i) a[i & 7] += fast_exp2(fmaf(f(v[i]), u, z));
+      l = fmaf(l, fast_exp2(fmaf(m, u, z)), ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7])));
+      m = n;
     }
     m *= u;                                // log2 units from here on
-    if (x == 1) other[tid & 127] = make_float2(m, l);
+    if (warp >= 4) other[(warp >> 2) - 1][tid & 127] = make_float2(m, l);
   }
   __syncthreads();
   if (warp < 4 && tiles > 0) {
-    join(m, l, other[tid].x, other[tid].y);
+    for (int i = 0; i < 3; ++i) join(m, l, other[i][tid].x, other[i][tid].y);
     const int row = c * kTile + tid;
     if (row < p.rows) p.part[block * p.rows + row] = make_float2(m, l);
   }
-  if (warp == 8) tmem_dealloc(tmem, 2 * kTile);
+  if (warp == kLoadWarp) tmem_dealloc(tmem, kBufs * kTile);
 }
 
 // ---------------------------------------------------------------- second launch
@@ -236,8 +235,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
   constexpr int NST = SumCfg<R>::NST;
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  __shared__ uint64_t q_full, k_full[NST], k_empty[NST], s_full[4], s_empty[4];
+  __shared__ uint64_t q_full, k_full[NST], k_empty[NST], s_full[kBufs], s_empty[kBufs];
   __shared__ uint32_t tmem_slot;
+  __shared__ float half_sum[2][2][kTile];   // group, tiles in turn
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row_tiles = (p.rows + kTile - 1) / kTile;
   unsigned char* sk = smem + row_tiles * T::TILEB;
@@ -246,22 +246,23 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
   if (tid == 0) {
     mbar_init(&q_full, 1);
     for (int i = 0; i < NST; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
-    for (int i = 0; i < 4; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_empty[i], 128);
+    for (int i = 0; i < kBufs; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_empty[i], kSoft / 2);
     fence_barrier_init();
   }
-  if (warp == 8) {
-    tmem_alloc(&tmem_slot, 4 * kTile);
+  if (warp == kLoadWarp) {
+    tmem_alloc(&tmem_slot, kBufs * kTile);
     tmem_relinquish();
   }
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  pdl_wait();
   pdl_trigger();
+  // What the first launch did not write can be read before it ends: its blocks have waited
+  // for everything before it.
   const Range r = range_of(p, blockIdx.x, p.sum_splits, p.sum_per_cta);
   const int tiles = (r.to - r.from + kTile - 1) / kTile;
   // item n of group x: tile 2 (n / row_tiles) + x with rows n % row_tiles, in buffer 2 x + (n & 1)
-  if (warp == 8) {
+  if (warp == kLoadWarp) {
     if (tiles > 0) {
       if (lane == 0) {
         mbar_arrive_expect_tx(&q_full, row_tiles * T::TILEB);
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
       // and so have the products' arrivals
       for (int i = max(0, j - NST); i < j; ++i) warp_wait(&k_empty[i % NST], (i / NST) & 1, p.at.err);
     }
-  } else if (warp == 9) {
+  } else if (warp == kMmaWarp) {
     const Desc dq = make_desc(smem_addr(smem), 16, 8 * T::SW, T::LAYOUT);
     const Desc dk = make_desc(smem_addr(sk), 16, 8 * T::SW, T::LAYOUT);
     bool ok = tiles > 0 && warp_wait(&q_full, 0, p.at.err);
@@ -301,9 +302,10 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
     }
   } else {
     // statistics of every row, by the softmax threads
+    pdl_wait();
     if (tiles > 0) {
       const int splits = (r.L + p.per_cta - 1) / p.per_cta;
-      for (int row = tid; row < row_tiles * kTile; row += 256) {
+      for (int row = tid; row < row_tiles * kTile; row += kSoft) {
         float m = -INFINITY, l = 0.f;
         if (row < p.rows) {
           const float2* part = p.part + r.pair * p.splits * p.rows + row;
@@ -320,65 +322,65 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
         see[row] = row < p.rows ? r.L - p.n_q + row % p.n_q : -1;
       }
     }
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    const int x = warp >> 2;
+    asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
+    const int x = warp >> 2 & 1, h = (warp >> 3) * kHalf;      // group, first column
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const float u = p.scale_log2;          // scores as they are: signed
     const int old = p.decay == 0.f ? 0 : (p.old_lens ? p.old_lens[r.b] : 0);
     int n = 0;
     bool ok = true;
-    for (int j = x; ok && j < tiles; j += 2) {
+    // after a wait that ran out the barriers below are still met, with nothing written
+    for (int j = x; j < tiles; j += 2) {
       const int t0 = r.from + j * kTile, t = t0 + (tid & 127);
-      const long long at = t < r.to ? slot_row_or_none(p.at, r.b, r.g, t) : -1;
+      const long long at = h == 0 && t < r.to ? slot_row_or_none(p.at, r.b, r.g, t) : -1;
       const float before = at >= 0 && t < old ? p.decay * p.w[at] : 0.f;
       const bool masked = t0 + kTile > r.L - p.n_q + 1;
       float sum = 0.f;
       for (int c = 0; c < row_tiles; ++c, ++n) {
         const int buf = 2 * x + (n & 1);
-        ok = warp_wait(&s_full[buf], (n >> 1) & 1, p.at.err);
+        ok = ok && warp_wait(&s_full[buf], (n >> 1) & 1, p.at.err);
         if (!ok) break;
         tc_fence_after();
         const float4* st = reinterpret_cast<const float4*>(stat + c * kTile);
         const bool all = !masked && (c + 1) * kTile <= p.rows;
         float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
-#pragma unroll 1
-        for (int h = 0; h < kTile; h += 64) {
-          uint32_t v[64];
-          tmem_ld64(tmem + buf * kTile + h + lanes, v);
-          if (h != 0) {
-            tc_fence_before();
-            mbar_arrive(&s_empty[buf]);
+        uint32_t v[kHalf];
+        tmem_ld64(tmem + buf * kTile + h + lanes, v);
+        tc_fence_before();
+        mbar_arrive(&s_empty[buf]);
+        if (all) {
+#pragma unroll
+          for (int i = 0; i < kHalf; i += 4) {
+            const float4 y = st[(h + i) / 2], w = st[(h + i) / 2 + 1];
+            a0 = fmaf(fast_exp2(fmaf(f(v[i]), u, y.x)), y.y, a0);
+            a1 = fmaf(fast_exp2(fmaf(f(v[i + 1]), u, y.z)), y.w, a1);
+            a2 = fmaf(fast_exp2(fmaf(f(v[i + 2]), u, w.x)), w.y, a2);
+            a3 = fmaf(fast_exp2(fmaf(f(v[i + 3]), u, w.z)), w.w, a3);
           }
-          if (all) {
+        } else {
+          // rows that do not see the token, and those past the last (whose zeros may
+          // meet an infinite key)
+          const int* last = see + c * kTile + h;
 #pragma unroll
-            for (int i = 0; i < 64; i += 4) {
-              const float4 y = st[(h + i) / 2], w = st[(h + i) / 2 + 1];
-              a0 = fmaf(fast_exp2(fmaf(f(v[i]), u, y.x)), y.y, a0);
-              a1 = fmaf(fast_exp2(fmaf(f(v[i + 1]), u, y.z)), y.w, a1);
-              a2 = fmaf(fast_exp2(fmaf(f(v[i + 2]), u, w.x)), w.y, a2);
-              a3 = fmaf(fast_exp2(fmaf(f(v[i + 3]), u, w.z)), w.w, a3);
-            }
-          } else {
-            // rows that do not see the token, and those past the last (whose zeros may
-            // meet an infinite key)
-            const int* last = see + c * kTile + h;
-#pragma unroll
-            for (int i = 0; i < 64; i += 2) {
-              const float4 y = st[(h + i) / 2];
-              const float b0 = fast_exp2(fmaf(f(v[i]), u, y.x)) * y.y;
-              const float b1 = fast_exp2(fmaf(f(v[i + 1]), u, y.z)) * y.w;
-              a0 += t > last[i] ? 0.f : b0;
-              a1 += t > last[i + 1] ? 0.f : b1;
-            }
+          for (int i = 0; i < kHalf; i += 2) {
+            const float4 y = st[(h + i) / 2];
+            const float b0 = fast_exp2(fmaf(f(v[i]), u, y.x)) * y.y;
+            const float b1 = fast_exp2(fmaf(f(v[i + 1]), u, y.z)) * y.w;
+            a0 += t > last[i] ? 0.f : b0;
+            a1 += t > last[i + 1] ? 0.f : b1;
           }
         }
         sum += (a0 + a1) + (a2 + a3);
       }
-      if (ok && at >= 0) p.w[at] = before + sum;
+      // both halves of the rows
+      float* pair = half_sum[x][(j >> 1) & 1];
+      if (h != 0) pair[tid & 127] = sum;
+      asm volatile("bar.sync %0, %1;" ::"r"(2 + x), "n"(kSoft / 2) : "memory");
+      if (ok && at >= 0) p.w[at] = before + (sum + pair[tid & 127]);
     }
   }
   __syncthreads();
-  if (warp == 8) tmem_dealloc(tmem, 4 * kTile);
+  if (warp == kLoadWarp) tmem_dealloc(tmem, kBufs * kTile);
 }
 
 template <int R>

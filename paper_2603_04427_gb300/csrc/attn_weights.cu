@@ -212,6 +212,14 @@ struct KeyTiles {
 };
 
 // ---------------------------------------------------------------- two launches
+// A row's statistics for the second launch: maximum, 1 / sum (0 for a row that
+// sees no token) and the last token that it sees.
+struct RowStat {
+  float m, inv;
+  int see;
+  int pad;
+};
+
 // Tokens of a row of stored scores.
 __device__ __forceinline__ int score_stride(const WeightsParams& p) { return (p.at.limit + 15) & ~15; }
 
@@ -365,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 2) weights_sum_kernel(const __grid_c
   Ring ring;
   ring.start(p, rows, dyn, bars, t0, r.to, warp, lane);
   stage_queries<R, KF>(p, r.pair, 0, tiles, sq);
-  join_rows<kThreads>(p, r, tiles * 16, stat);
+  join_rows<kThreads>(p, r, tiles * 16, [&](int row, float m, float inv, int see) { stat[row] = {m, inv, see, 0}; });
   __syncthreads();
   const float u = unit<KF>(p);
   const int old = p.decay == 0.f ? 0 : (p.old_lens ? p.old_lens[r.b] : 0);
@@ -496,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, ROWS <= 4 ? 4 : 2) weights_join_kern
   int t = r.from + 4 * static_cast<int>(threadIdx.x);
   find(t);
   if (t < r.to) load(t);
-  join_rows<kThreads>(p, r, 8, stat);
+  join_rows<kThreads>(p, r, 8, [&](int row, float m, float inv, int see) { stat[row] = {m, inv, see, 0}; });
   __syncthreads();
   float m[ROWS], inv[ROWS];
 #pragma unroll

@@ -34,18 +34,11 @@ __device__ __forceinline__ Range range_of(const WeightsParams& p, long long bloc
   return r;
 }
 
-// A row's statistics for the second launch: maximum, 1 / sum (0 for a row that
-// sees no token) and the last token that it sees.
-struct RowStat {
-  float m, inv;
-  int see;
-  int pad;
-};
-
 // Joins the ranges' statistics of every row.  A power of two of lanes per row, so
-// that the block's threads share the loads whether rows are few or many.
-template <int kThreads>
-__device__ __forceinline__ void join_rows(const WeightsParams& p, const Range& r, int padded, RowStat* stat) {
+// that the block's threads share the loads whether rows are few or many.  store(row,
+// maximum, 1 / sum or 0 for a row that sees no token, the last token that it sees).
+template <int kThreads, class Store>
+__device__ __forceinline__ void join_rows(const WeightsParams& p, const Range& r, int padded, Store store) {
   int lanes = 32;
   while (lanes > 1 && lanes * padded > kThreads) lanes >>= 1;
   const int splits = (r.L + p.per_cta - 1) / p.per_cta;
@@ -69,12 +62,7 @@ __device__ __forceinline__ void join_rows(const WeightsParams& p, const Range& r
       join(m, l, m2, l2);
     }
     if (sub == 0 && row < padded) {
-      RowStat x;
-      x.m = m == -INFINITY ? 0.f : m;
-      x.inv = l == 0.f ? 0.f : 1.f / l;
-      x.see = row < p.rows ? r.L - p.n_q + row % p.n_q : -1;
-      x.pad = 0;
-      stat[row] = x;
+      store(row, m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l, row < p.rows ? r.L - p.n_q + row % p.n_q : -1);
     }
   }
 }

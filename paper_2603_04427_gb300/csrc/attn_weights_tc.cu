@@ -92,7 +92,23 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* e
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, err));
 }
 
+// 32 columns of a thread's TMEM lane at each of two addresses: two loads, one wait.
+__device__ __forceinline__ void tmem_ld32_2(uint32_t ta, uint32_t tb, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
+      "%11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, "
+      "%28, %29, %30, %31}, [%64];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, "
+      "%41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, "
+      "%58, %59, %60, %61, %62, %63}, [%65];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : TK_R8(0), TK_R8(8), TK_R8(16), TK_R8(24), TK_R8(32), TK_R8(40), TK_R8(48), TK_R8(56)
+      : "r"(ta), "r"(tb)
+      : "memory");
+}
+
 __device__ __forceinline__ float f(uint32_t x) { return __uint_as_float(x); }
+__device__ __forceinline__ float2 exp2_2(float2 x) { return make_float2(fast_exp2(x.x), fast_exp2(x.y)); }
 
 // ---------------------------------------------------------------- first launch
 template <int R>
@@ -201,11 +217,14 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
       const float n = fmaxf(m, fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7]))));
       // no score above -inf: exponentials of zero maximum, which a NaN survives
       const float z = n == -INFINITY ? 0.f : -n * u;
+      float2 e[4] = {{0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) a[i] = 0.f;
-#pragma unroll
-      for (int i = 0; i < kHalf; ++i) a[i & 7] += fast_exp2(fmaf(f(v[i]), u, z));
-      l = fmaf(l, fast_exp2(fmaf(m, u, z)), ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7])));
+      for (int i = 0; i < kHalf; i += 2) {
+        const float2 x2 = ffma2(make_float2(f(v[i]), f(v[i + 1])), make_float2(u, u), make_float2(z, z));
+        e[(i >> 1) & 3] = fadd2(e[(i >> 1) & 3], exp2_2(x2));
+      }
+      const float2 sum = fadd2(fadd2(e[0], e[1]), fadd2(e[2], e[3]));
+      l = fmaf(l, fast_exp2(fmaf(m, u, z)), sum.x + sum.y);
       m = n;
     }
     m *= u;                                // log2 units from here on
@@ -235,18 +254,19 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
   constexpr int NST = SumCfg<R>::NST;
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  __shared__ uint64_t q_full, k_full[NST], k_empty[NST], s_full[kBufs], s_empty[kBufs];
+  __shared__ uint64_t q_full, k_full[NST], k_empty[NST], s_full[2], s_empty[2];
   __shared__ uint32_t tmem_slot;
-  __shared__ float half_sum[2][2][kTile];   // group, tiles in turn
+  __shared__ float part_sum[2][4][2 * kTile];   // pairs of tiles in turn; rows by quarters of their tiles
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row_tiles = (p.rows + kTile - 1) / kTile;
   unsigned char* sk = smem + row_tiles * T::TILEB;
-  float2* stat = reinterpret_cast<float2*>(sk + NST * T::TILEB);
-  int* see = reinterpret_cast<int*>(stat + row_tiles * kTile);
+  float* neg_max = reinterpret_cast<float*>(sk + NST * T::TILEB);
+  float* inv = neg_max + row_tiles * kTile;
+  int* see = reinterpret_cast<int*>(inv + row_tiles * kTile);
   if (tid == 0) {
     mbar_init(&q_full, 1);
     for (int i = 0; i < NST; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
-    for (int i = 0; i < kBufs; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_empty[i], kSoft / 2);
+    for (int i = 0; i < 2; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_empty[i], kSoft);
     fence_barrier_init();
   }
   if (warp == kLoadWarp) {
@@ -261,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
   // for everything before it.
   const Range r = range_of(p, blockIdx.x, p.sum_splits, p.sum_per_cta);
   const int tiles = (r.to - r.from + kTile - 1) / kTile;
-  // item n of group x: tile 2 (n / row_tiles) + x with rows n % row_tiles, in buffer 2 x + (n & 1)
+  // item n: tiles 2 (n / row_tiles) and the next with row tile n % row_tiles, in buffers n & 1
   if (warp == kLoadWarp) {
     if (tiles > 0) {
       if (lane == 0) {
@@ -285,98 +305,83 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
     const Desc dq = make_desc(smem_addr(smem), 16, 8 * T::SW, T::LAYOUT);
     const Desc dk = make_desc(smem_addr(sk), 16, 8 * T::SW, T::LAYOUT);
     bool ok = tiles > 0 && warp_wait(&q_full, 0, p.at.err);
-    for (int j0 = 0; ok && j0 < tiles; j0 += 2) {
-      for (int c = 0; ok && c < row_tiles; ++c) {
-        for (int x = 0; ok && x < 2 && j0 + x < tiles; ++x) {
-          const int j = j0 + x, st = j % NST;
-          const int n = (j0 >> 1) * row_tiles + c, buf = 2 * x + (n & 1), use = n >> 1;
-          if (c == 0) ok = warp_wait(&k_full[st], (j / NST) & 1, p.at.err);
-          if (ok && use > 0) ok = warp_wait(&s_empty[buf], (use - 1) & 1, p.at.err);
-          if (!ok) break;
-          tc_fence_after();
-          scores<R>(tmem + buf * kTile, dk, st * T::TILEB, dq, c * T::TILEB);
-          tc_commit_e(&s_full[buf]);
-          if (c == row_tiles - 1) tc_commit_e(&k_empty[st]);
-        }
+    for (int j = 0, n = 0; ok && j < tiles; j += 2) {
+      const int both = min(2, tiles - j);
+      for (int c = 0; c < row_tiles; ++c, ++n) {
+        const int buf = n & 1, use = n >> 1;
+        for (int e = 0; ok && c == 0 && e < both; ++e) ok = warp_wait(&k_full[(j + e) % NST], ((j + e) / NST) & 1, p.at.err);
+        if (ok && use > 0) ok = warp_wait(&s_empty[buf], (use - 1) & 1, p.at.err);
+        if (!ok) break;
+        tc_fence_after();
+        for (int e = 0; e < both; ++e)
+          scores<R>(tmem + (2 * buf + e) * kTile, dk, (j + e) % NST * T::TILEB, dq, c * T::TILEB);
+        tc_commit_e(&s_full[buf]);
+        for (int e = 0; e < both && c == row_tiles - 1; ++e) tc_commit_e(&k_empty[(j + e) % NST]);
       }
     }
   } else {
     // statistics of every row, by the softmax threads
     pdl_wait();
     if (tiles > 0) {
-      const int splits = (r.L + p.per_cta - 1) / p.per_cta;
-      for (int row = tid; row < row_tiles * kTile; row += kSoft) {
-        float m = -INFINITY, l = 0.f;
-        if (row < p.rows) {
-          const float2* part = p.part + r.pair * p.splits * p.rows + row;
-          for (int s0 = 0; s0 < splits; s0 += 4) {
-            float2 x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              x[i] = s0 + i < splits ? __ldcg(part + static_cast<long long>(s0 + i) * p.rows) : make_float2(-INFINITY, 0.f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) join(m, l, x[i].x, x[i].y);
-          }
-        }
-        stat[row] = make_float2(m == -INFINITY ? 0.f : -m, l == 0.f ? 0.f : 1.f / l);
-        see[row] = row < p.rows ? r.L - p.n_q + row % p.n_q : -1;
-      }
+      join_rows<kSoft>(p, r, row_tiles * kTile, [&](int row, float m, float i, int last) {
+        neg_max[row] = -m;
+        inv[row] = i;
+        see[row] = last;
+      });
     }
     asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
-    const int x = warp >> 2 & 1, h = (warp >> 3) * kHalf;      // group, first column
+    const int h = (warp >> 2) * (kTile / 4);                   // first column
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const float u = p.scale_log2;          // scores as they are: signed
+    const float2 u = make_float2(p.scale_log2, p.scale_log2);  // scores as they are: signed
     const int old = p.decay == 0.f ? 0 : (p.old_lens ? p.old_lens[r.b] : 0);
     int n = 0;
     bool ok = true;
     // after a wait that ran out the barriers below are still met, with nothing written
-    for (int j = x; j < tiles; j += 2) {
-      const int t0 = r.from + j * kTile, t = t0 + (tid & 127);
-      const long long at = h == 0 && t < r.to ? slot_row_or_none(p.at, r.b, r.g, t) : -1;
-      const float before = at >= 0 && t < old ? p.decay * p.w[at] : 0.f;
-      const bool masked = t0 + kTile > r.L - p.n_q + 1;
-      float sum = 0.f;
+    for (int j = 0; j < tiles; j += 2) {
+      const int t0 = r.from + j * kTile, mine = t0 + tid;      // the token that this thread writes
+      const long long at = tid < 2 * kTile && mine < r.to ? slot_row_or_none(p.at, r.b, r.g, mine) : -1;
+      const float before = at >= 0 && mine < old ? p.decay * p.w[at] : 0.f;
+      const int ta = t0 + (tid & 127), tb = ta + kTile;        // the tokens whose weights it adds up
+      const bool masked = t0 + 2 * kTile > r.L - p.n_q + 1;
+      float2 a0 = {0.f, 0.f}, a1 = a0, b0 = a0, b1 = a0;
       for (int c = 0; c < row_tiles; ++c, ++n) {
-        const int buf = 2 * x + (n & 1);
+        const int buf = n & 1, row = c * kTile + h;
         ok = ok && warp_wait(&s_full[buf], (n >> 1) & 1, p.at.err);
         if (!ok) break;
         tc_fence_after();
-        const float4* st = reinterpret_cast<const float4*>(stat + c * kTile);
-        const bool all = !masked && (c + 1) * kTile <= p.rows;
-        float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
-        uint32_t v[kHalf];
-        tmem_ld64(tmem + buf * kTile + h + lanes, v);
+        uint32_t v[64];                                        // 32 rows' scores of ta, of tb
+        tmem_ld32_2(tmem + 2 * buf * kTile + h + lanes, tmem + (2 * buf + 1) * kTile + h + lanes, v);
         tc_fence_before();
         mbar_arrive(&s_empty[buf]);
-        if (all) {
+        if (!masked && (c + 1) * kTile <= p.rows) {
 #pragma unroll
-          for (int i = 0; i < kHalf; i += 4) {
-            const float4 y = st[(h + i) / 2], w = st[(h + i) / 2 + 1];
-            a0 = fmaf(fast_exp2(fmaf(f(v[i]), u, y.x)), y.y, a0);
-            a1 = fmaf(fast_exp2(fmaf(f(v[i + 1]), u, y.z)), y.w, a1);
-            a2 = fmaf(fast_exp2(fmaf(f(v[i + 2]), u, w.x)), w.y, a2);
-            a3 = fmaf(fast_exp2(fmaf(f(v[i + 3]), u, w.z)), w.w, a3);
+          for (int i = 0; i < 32; i += 4) {
+            const float4 m = *reinterpret_cast<const float4*>(neg_max + row + i);
+            const float4 w = *reinterpret_cast<const float4*>(inv + row + i);
+            a0 = ffma2(exp2_2(ffma2(make_float2(f(v[i]), f(v[i + 1])), u, make_float2(m.x, m.y))), make_float2(w.x, w.y), a0);
+            b0 = ffma2(exp2_2(ffma2(make_float2(f(v[i + 32]), f(v[i + 33])), u, make_float2(m.x, m.y))), make_float2(w.x, w.y), b0);
+            a1 = ffma2(exp2_2(ffma2(make_float2(f(v[i + 2]), f(v[i + 3])), u, make_float2(m.z, m.w))), make_float2(w.z, w.w), a1);
+            b1 = ffma2(exp2_2(ffma2(make_float2(f(v[i + 34]), f(v[i + 35])), u, make_float2(m.z, m.w))), make_float2(w.z, w.w), b1);
           }
         } else {
           // rows that do not see the token, and those past the last (whose zeros may
           // meet an infinite key)
-          const int* last = see + c * kTile + h;
 #pragma unroll
-          for (int i = 0; i < kHalf; i += 2) {
-            const float4 y = st[(h + i) / 2];
-            const float b0 = fast_exp2(fmaf(f(v[i]), u, y.x)) * y.y;
-            const float b1 = fast_exp2(fmaf(f(v[i + 1]), u, y.z)) * y.w;
-            a0 += t > last[i] ? 0.f : b0;
-            a1 += t > last[i + 1] ? 0.f : b1;
+          for (int i = 0; i < 32; ++i) {
+            const float x = fast_exp2(fmaf(f(v[i]), u.x, neg_max[row + i])) * inv[row + i];
+            const float y = fast_exp2(fmaf(f(v[i + 32]), u.x, neg_max[row + i])) * inv[row + i];
+            a0.x += ta > see[row + i] ? 0.f : x;
+            b0.x += tb > see[row + i] ? 0.f : y;
           }
         }
-        sum += (a0 + a1) + (a2 + a3);
       }
-      // both halves of the rows
-      float* pair = half_sum[x][(j >> 1) & 1];
-      if (h != 0) pair[tid & 127] = sum;
-      asm volatile("bar.sync %0, %1;" ::"r"(2 + x), "n"(kSoft / 2) : "memory");
-      if (ok && at >= 0) p.w[at] = before + (sum + pair[tid & 127]);
+      float(*sum)[2 * kTile] = part_sum[(j >> 1) & 1];
+      a0 = fadd2(a0, a1);
+      b0 = fadd2(b0, b1);
+      sum[warp >> 2][tid & 127] = a0.x + a0.y;
+      sum[warp >> 2][(tid & 127) + kTile] = b0.x + b0.y;
+      asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
+      if (ok && at >= 0) p.w[at] = before + ((sum[0][tid] + sum[1][tid]) + (sum[2][tid] + sum[3][tid]));
     }
   }
   __syncthreads();

@@ -108,12 +108,17 @@ __device__ __forceinline__ void tmem_ld32_2(uint32_t ta, uint32_t tb, uint32_t* 
 }
 
 __device__ __forceinline__ float f(uint32_t x) { return __uint_as_float(x); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ float2 exp2_2(float2 x) { return make_float2(fast_exp2(x.x), fast_exp2(x.y)); }
 
 // ---------------------------------------------------------------- first launch
 template <int R>
 struct StatCfg {
-  static constexpr int NST = R == 128 ? 3 : 4;               // stages of keys
+  static constexpr int NST = R == 128 ? 5 : 8;               // stages of keys
   static constexpr int OFF_K = TCfg<R>::TILEB;
   static constexpr int SMEM = OFF_K + NST * TCfg<R>::TILEB + 1024;
 };
@@ -134,6 +139,10 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
     for (int i = 0; i < NST; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
     for (int i = 0; i < kBufs; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_empty[i], kSoft / 2);
     fence_barrier_init();
+  }
+  if (warp == kMmaWarp && lane == 0) {
+    prefetch_map(&maps.q);
+    prefetch_map(&maps.k);
   }
   if (warp == kLoadWarp) {
     tmem_alloc(&tmem_slot, kBufs * kTile);
@@ -195,6 +204,10 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
       const int buf = j % kBufs;
       if (!warp_wait(&s_full[buf], (j / kBufs) & 1, p.at.err)) break;
       tc_fence_after();
+      if (row - lane >= p.rows) {          // a warp without a row
+        mbar_arrive(&s_empty[buf]);
+        continue;
+      }
       uint32_t v[kHalf];
       tmem_ld64(tmem + buf * kTile + h + lanes, v);
       tc_fence_before();
@@ -213,8 +226,8 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] = f(v[i]);
 #pragma unroll
-      for (int i = 8; i < kHalf; ++i) a[i & 7] = fmaxf(a[i & 7], f(v[i]));
-      const float n = fmaxf(m, fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7]))));
+      for (int i = 8; i + 1 < kHalf; i += 2) a[(i >> 1) & 7] = max3(a[(i >> 1) & 7], f(v[i]), f(v[i + 1]));
+      const float n = max3(max3(a[0], a[1], a[2]), max3(a[3], a[4], a[5]), max3(m, a[6], a[7]));
       // no score above -inf: exponentials of zero maximum, which a NaN survives
       const float z = n == -INFINITY ? 0.f : -n * u;
       float2 e[4] = {{0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}};
@@ -240,34 +253,42 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
 }
 
 // ---------------------------------------------------------------- second launch
+// Stages of keys beside the row tiles' queries: as many as fit.
+constexpr int kMaxStages = 8;
 template <int R>
-struct SumCfg {
-  static constexpr int NST = R == 128 ? 2 : 4;
-  // query tiles, key stages, statistics of a row: (maximum, 1 / sum) and the last token
-  static constexpr int smem(int row_tiles) { return (row_tiles + NST) * TCfg<R>::TILEB + row_tiles * kTile * 12 + 1024; }
-};
+constexpr int sum_stages(int row_tiles) {
+  const int fit = 200 * 1024 / TCfg<R>::TILEB - row_tiles;
+  return fit < kMaxStages ? fit : kMaxStages;
+}
+// Queries, keys; each row's exponent and last token.
+template <int R>
+constexpr int sum_smem(int row_tiles) {
+  return (row_tiles + sum_stages<R>(row_tiles)) * TCfg<R>::TILEB + row_tiles * kTile * 8 + 1024;
+}
 
 template <int R>
 __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __grid_constant__ WeightMaps maps,
                                                                      const __grid_constant__ WeightsParams p) {
   using T = TCfg<R>;
-  constexpr int NST = SumCfg<R>::NST;
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  __shared__ uint64_t q_full, k_full[NST], k_empty[NST], s_full[2], s_empty[2];
+  __shared__ uint64_t q_full, k_full[kMaxStages], k_empty[kMaxStages], s_full[2], s_empty[2];
   __shared__ uint32_t tmem_slot;
   __shared__ float part_sum[2][4][2 * kTile];   // pairs of tiles in turn; rows by quarters of their tiles
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int row_tiles = (p.rows + kTile - 1) / kTile;
+  const int row_tiles = (p.rows + kTile - 1) / kTile, stages = sum_stages<R>(row_tiles);
   unsigned char* sk = smem + row_tiles * T::TILEB;
-  float* neg_max = reinterpret_cast<float*>(sk + NST * T::TILEB);
-  float* inv = neg_max + row_tiles * kTile;
-  int* see = reinterpret_cast<int*>(inv + row_tiles * kTile);
+  float* expo = reinterpret_cast<float*>(sk + stages * T::TILEB);   // -(maximum + log2 of the sum)
+  int* see = reinterpret_cast<int*>(expo + row_tiles * kTile);
   if (tid == 0) {
     mbar_init(&q_full, 1);
-    for (int i = 0; i < NST; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
+    for (int i = 0; i < kMaxStages; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
     for (int i = 0; i < 2; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_empty[i], kSoft);
     fence_barrier_init();
+  }
+  if (warp == kMmaWarp && lane == 0) {
+    prefetch_map(&maps.q);
+    prefetch_map(&maps.k);
   }
   if (warp == kLoadWarp) {
     tmem_alloc(&tmem_slot, kBufs * kTile);
@@ -290,42 +311,54 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
           for (int i = 0; i < T::NBOX; ++i)
             tma_load_3d(smem + c * T::TILEB + i * T::BOXB, &maps.q, i * T::BOX, c * kTile, static_cast<int>(r.pair), &q_full);
       }
-      int j = 0;
+      int j = 0, st = 0, lap = 0;
       for (; j < tiles; ++j) {
-        const int st = j % NST;
-        if (j >= NST && !warp_wait(&k_empty[st], (j / NST - 1) & 1, p.at.err)) break;
+        if (lap > 0 && !warp_wait(&k_empty[st], (lap - 1) & 1, p.at.err)) break;
         load_keys<R>(maps, p, r, r.from + j * kTile, sk + st * T::TILEB, &k_full[st], lane);
+        if (++st == stages) st = 0, ++lap;
       }
+      // every copy has landed before the block ends, and so have the products' arrivals
       warp_wait(&q_full, 0, p.at.err);
-      for (int i = max(0, j - NST); i < j; ++i) warp_wait(&k_full[i % NST], (i / NST) & 1, p.at.err);
-      // and so have the products' arrivals
-      for (int i = max(0, j - NST); i < j; ++i) warp_wait(&k_empty[i % NST], (i / NST) & 1, p.at.err);
+      for (int i = max(0, j - stages); i < j; ++i) warp_wait(&k_full[i % stages], (i / stages) & 1, p.at.err);
+      for (int i = max(0, j - stages); i < j; ++i) warp_wait(&k_empty[i % stages], (i / stages) & 1, p.at.err);
     }
   } else if (warp == kMmaWarp) {
     const Desc dq = make_desc(smem_addr(smem), 16, 8 * T::SW, T::LAYOUT);
     const Desc dk = make_desc(smem_addr(sk), 16, 8 * T::SW, T::LAYOUT);
     bool ok = tiles > 0 && warp_wait(&q_full, 0, p.at.err);
+    int st[2] = {0, 1 % stages}, lap[2] = {0, 1 / stages};     // stages of both tiles
     for (int j = 0, n = 0; ok && j < tiles; j += 2) {
       const int both = min(2, tiles - j);
       for (int c = 0; c < row_tiles; ++c, ++n) {
         const int buf = n & 1, use = n >> 1;
-        for (int e = 0; ok && c == 0 && e < both; ++e) ok = warp_wait(&k_full[(j + e) % NST], ((j + e) / NST) & 1, p.at.err);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (ok && c == 0 && e < both) ok = warp_wait(&k_full[st[e]], lap[e] & 1, p.at.err);
         if (ok && use > 0) ok = warp_wait(&s_empty[buf], (use - 1) & 1, p.at.err);
         if (!ok) break;
         tc_fence_after();
-        for (int e = 0; e < both; ++e)
-          scores<R>(tmem + (2 * buf + e) * kTile, dk, (j + e) % NST * T::TILEB, dq, c * T::TILEB);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (e < both) scores<R>(tmem + (2 * buf + e) * kTile, dk, st[e] * T::TILEB, dq, c * T::TILEB);
         tc_commit_e(&s_full[buf]);
-        for (int e = 0; e < both && c == row_tiles - 1; ++e) tc_commit_e(&k_empty[(j + e) % NST]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (e < both && c == row_tiles - 1) tc_commit_e(&k_empty[st[e]]);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        st[e] += 2;
+        if (st[e] >= stages) st[e] -= stages, ++lap[e];
       }
     }
   } else {
     // statistics of every row, by the softmax threads
     pdl_wait();
     if (tiles > 0) {
-      join_rows<kSoft>(p, r, row_tiles * kTile, [&](int row, float m, float i, int last) {
-        neg_max[row] = -m;
-        inv[row] = i;
+      // one number a row: a weight is one exponential, and -inf where a row has no weight;
+      // the number's rounding is that of one more term of the row's sum
+      join_rows<kSoft>(p, r, row_tiles * kTile, [&](int row, float m, float inv, int last) {
+        expo[row] = log2f(inv) - m;
         see[row] = last;
       });
     }
@@ -353,23 +386,22 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
         tmem_ld32_2(tmem + 2 * buf * kTile + h + lanes, tmem + (2 * buf + 1) * kTile + h + lanes, v);
         tc_fence_before();
         mbar_arrive(&s_empty[buf]);
-        if (!masked && (c + 1) * kTile <= p.rows) {
+        if (!masked && row + kTile / 4 <= p.rows) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
-            const float4 m = *reinterpret_cast<const float4*>(neg_max + row + i);
-            const float4 w = *reinterpret_cast<const float4*>(inv + row + i);
-            a0 = ffma2(exp2_2(ffma2(make_float2(f(v[i]), f(v[i + 1])), u, make_float2(m.x, m.y))), make_float2(w.x, w.y), a0);
-            b0 = ffma2(exp2_2(ffma2(make_float2(f(v[i + 32]), f(v[i + 33])), u, make_float2(m.x, m.y))), make_float2(w.x, w.y), b0);
-            a1 = ffma2(exp2_2(ffma2(make_float2(f(v[i + 2]), f(v[i + 3])), u, make_float2(m.z, m.w))), make_float2(w.z, w.w), a1);
-            b1 = ffma2(exp2_2(ffma2(make_float2(f(v[i + 34]), f(v[i + 35])), u, make_float2(m.z, m.w))), make_float2(w.z, w.w), b1);
+            const float4 x = *reinterpret_cast<const float4*>(expo + row + i);
+            a0 = fadd2(a0, exp2_2(ffma2(make_float2(f(v[i]), f(v[i + 1])), u, make_float2(x.x, x.y))));
+            b0 = fadd2(b0, exp2_2(ffma2(make_float2(f(v[i + 32]), f(v[i + 33])), u, make_float2(x.x, x.y))));
+            a1 = fadd2(a1, exp2_2(ffma2(make_float2(f(v[i + 2]), f(v[i + 3])), u, make_float2(x.z, x.w))));
+            b1 = fadd2(b1, exp2_2(ffma2(make_float2(f(v[i + 34]), f(v[i + 35])), u, make_float2(x.z, x.w))));
           }
-        } else {
+        } else if (row < p.rows) {
           // rows that do not see the token, and those past the last (whose zeros may
           // meet an infinite key)
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            const float x = fast_exp2(fmaf(f(v[i]), u.x, neg_max[row + i])) * inv[row + i];
-            const float y = fast_exp2(fmaf(f(v[i + 32]), u.x, neg_max[row + i])) * inv[row + i];
+            const float x = fast_exp2(fmaf(f(v[i]), u.x, expo[row + i]));
+            const float y = fast_exp2(fmaf(f(v[i + 32]), u.x, expo[row + i]));
             a0.x += ta > see[row + i] ? 0.f : x;
             b0.x += tb > see[row + i] ? 0.f : y;
           }
@@ -404,12 +436,12 @@ cudaError_t launch_t(const WeightsParams& p, cudaStream_t s) {
   e = launch_pdl(weights_stats_tc_kernel<R>, dim3(static_cast<unsigned>(static_cast<long long>(pairs) * p.splits * row_tiles)),
                  dim3(kThreads), StatCfg<R>::SMEM, s, maps, p);
   if (e != cudaSuccess) return e;
-  constexpr int kMost = SumCfg<R>::smem(kMaxWeightRows / kTile);
-  static_assert(kMost <= 226 * 1024, "shared memory");
+  constexpr int kMost = 216 * 1024;
+  static_assert(sum_smem<R>(1) <= kMost && sum_smem<R>(4) <= kMost && sum_stages<R>(kMaxWeightRows / kTile) >= 2, "shared memory");
   e = cudaFuncSetAttribute(weights_sum_tc_kernel<R>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
   if (e != cudaSuccess) return e;
   return launch_pdl(weights_sum_tc_kernel<R>, dim3(static_cast<unsigned>(static_cast<long long>(pairs) * p.sum_splits)),
-                    dim3(kThreads), static_cast<size_t>(SumCfg<R>::smem(row_tiles)), s, maps, p);
+                    dim3(kThreads), static_cast<size_t>(sum_smem<R>(row_tiles)), s, maps, p);
 }
 
 }  // namespace
@@ -417,11 +449,16 @@ cudaError_t launch_t(const WeightsParams& p, cudaStream_t s) {
 // Keys in bf16 as the MMA takes them, and enough rows for half of its tile.
 bool weights_on_tcgen05(const WeightsParams& p) {
   const long long planes = static_cast<long long>(p.at.page_size ? p.at.num_pages : p.B) * p.at.Hkv;
-  return p.k_fmt == 0 && p.n_q > 1 && p.rows >= 64 && p.R >= 64 && planes < (1ll << 31);
+  return p.k_fmt == 0 && p.n_q > 1 && p.rows >= 64 && planes < (1ll << 31);
 }
 
 cudaError_t launch_attn_weights_tc(const WeightsParams& p, cudaStream_t s) {
-  return p.R == 64 ? launch_t<64>(p, s) : launch_t<128>(p, s);
+  switch (p.R) {
+    case 16: return launch_t<16>(p, s);
+    case 32: return launch_t<32>(p, s);
+    case 64: return launch_t<64>(p, s);
+    default: return launch_t<128>(p, s);
+  }
 }
 
 }  // namespace tk

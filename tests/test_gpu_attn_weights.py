@@ -93,6 +93,7 @@ def test_many_queries(G, n):
 
 
 @pytest.mark.parametrize("r,G,n,ps,cap", [
+    (16, 4, 16, 0, 1312), (16, 8, 40, 64, 1536), (32, 8, 64, 16, 1536), (32, 2, 50, 0, 1312),
     (64, 4, 16, 0, 1312), (64, 4, 32, 16, 1536), (64, 1, 65, 64, 1536), (64, 8, 64, 128, 1536), (64, 2, 200, 256, 1536),
     (128, 2, 32, 0, 1328), (128, 8, 64, 32, 1536), (128, 4, 33, 128, 1536), (128, 4, 100, 0, 1504)])
 def test_tiles_of_many_queries(r, G, n, ps, cap):

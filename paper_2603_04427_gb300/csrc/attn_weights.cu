@@ -16,19 +16,19 @@
 //         once, nothing in global memory in between.
 // stored  one query, longer contexts: two launches over the same token ranges, the
 //         scores (4 G bytes a token, less than a key) in the workspace.
-// twice   many queries: two launches that each compute the scores, from keys that
+// twice   more queries: two launches that each compute the scores, from keys that
 //         the L2 mostly still holds; scores of many rows are more bytes than keys.
 //
-// Products on mma.sync.m16n8k16: 16 query rows by 8 tokens, keys as the second operand,
+// Many rows of bf16 keys take a form of "twice" on tcgen05 (attn_weights_tc.cu).  Here
+// products are mma.sync.m16n8k16: 16 query rows by 8 tokens, keys as the second operand,
 // so that a lane's 16-byte load of a key row is two operands as it stands (as the first
-// one, four registers would have to be brought together from two rows for each
-// product).  tcgen05's 128-row tiles would be empty with one query (G rows), and with many
-// the exponentials, two a score, come next.  Statistics and weights are fp32; scores in
-// log2 units.
+// one, four registers would have to be brought together from two rows for each product);
+// tcgen05's 128-row tiles would be empty with one query (G rows).  Statistics and weights
+// are fp32; scores in log2 units.
 //
 // Measured: fused, 16 sequences of 4096 tokens, r = 32: 10.1 us (3.3 TB/s; latency);
-// stored, 4 x 128 K tokens: 68 us, the first launch at 5.5 TB/s; twice, 32 queries of 4
-// heads on 2 x 16381 tokens, r = 64: 42.4 us, bound by mma.sync (18 cycles a product and
+// stored, 4 x 128 K tokens: 68 us, the first launch at 5.5 TB/s; twice, 8 queries of 4
+// heads on 2 x 16381 tokens, r = 32: 14.6 us, bound by mma.sync (18 cycles a product and
 // SM quarter).
 #include <algorithm>
 

@@ -2,18 +2,26 @@
 //
 // Two launches that both compute the scores, as there: the first with query rows as the
 // MMA's M, so that a thread owns a row (a TMEM lane) and its maximum and sum need no other
-// thread; the second with tokens as M, so that a thread owns a token and adds up its
-// weights over the rows, whose (maximum, 1 / sum) it reads from shared memory.  Either
-// way the operands are K-major tiles of the same layout, keys and queries just change
-// places in the instruction.
+// thread; the second with tokens as M, so that a thread owns tokens and adds up their
+// weights over the rows.  A row is one number there, -(maximum + log2 of its sum), from
+// shared memory: a weight is one FMA, one exponential and one addition, and two tokens of
+// a thread share each load.  Either way the operands are K-major tiles of the same layout,
+// keys and queries just change places in the instruction.
 //
-// mma.sync takes 18 cycles a product and SM quarter here and set the time of the form
-// that uses it (r = 64); on tcgen05 a tile of 128 x 128 scores takes about 130 cycles
-// (r = 64), and the exponentials, 128 x 128 for each of the launches, are what is left.
+// What bounds it: a tile of 128 x 128 scores takes the exponential units 512 cycles (a
+// warp's ex2 takes 4 here) and the tensor cores 240; it takes about 850.  A softmax
+// thread's wait, TMEM load, maximum and exponentials follow one another (some 270, 150 and
+// 1200 cycles an item, four warps an SM quarter), and waits and exponentials share a queue.
+// About 8 us of a call are two launches, prologues, first loads and the rows' join.
+// Measured, 32 queries of 4 heads on 2 x 16381 tokens, r = 64: 24.2 us (mma.sync: 42.4,
+// bound by 18 cycles a product and SM quarter).  Without any exponential or maximum the
+// first launch would gain 1.1 us, the second 4.  Not kept: eight softmax warps (33.4 us),
+// loads of the next 32 columns ahead of the exponentials (25.6), one arrival a warp
+// instead of one a thread (24.6).
 //
 // One block per SM.  Sixteen warps of softmax threads: two groups that take tiles in turn,
-// each in two halves of 64 columns; one warp for the TMA of key tiles into a ring, one for
-// the products.  Scores pass through TMEM buffers of 128 columns, two for each group: its
+// each in two halves of 64 columns (first launch), or all take pairs of tiles in quarters of
+// 32 rows (second); one warp for the TMA of key tiles into a ring, one for the products.  Scores pass through TMEM buffers of 128 columns, two for each group: its
 // threads copy one into registers and give it back before they work on it.
 #include <algorithm>
 
@@ -446,10 +454,16 @@ cudaError_t launch_t(const WeightsParams& p, cudaStream_t s) {
 
 }  // namespace
 
-// Keys in bf16 as the MMA takes them, and enough rows for half of its tile.
+// Keys in bf16, as the MMA takes them, and rows enough that a tile that is partly empty
+// costs less than mma.sync.  Measured, us, this form and the other, on 2 x 16381 tokens
+// and on 32 x 4096, 8 kv heads:
+//   r = 16:  64 rows 20.7 : 16.3, 69.9 : 49.4    128 rows 22.5 : 24.4, 77.3 : 79.9
+//   r = 32:  64 rows 20.9 : 19.2, 71.3 : 57.9    128 rows 22.7 : 28.6, 78.5 : 95.0
+//   r = 64:  32 rows 20.8 : 22.4, 69.2 : 66.2     48 rows 22.9 : 25.8, 76.6 : 83.7
+//   r = 128: 16 rows 26.2 : 26.0, 93.0 : 88.5     32 rows 25.7 : 30.8, 92.5 : 101.7
 bool weights_on_tcgen05(const WeightsParams& p) {
   const long long planes = static_cast<long long>(p.at.page_size ? p.at.num_pages : p.B) * p.at.Hkv;
-  return p.k_fmt == 0 && p.n_q > 1 && p.rows >= 64 && planes < (1ll << 31);
+  return p.k_fmt == 0 && p.n_q > 1 && p.rows >= (p.R <= 32 ? 128 : (p.R == 64 ? 48 : 32)) && planes < (1ll << 31);
 }
 
 cudaError_t launch_attn_weights_tc(const WeightsParams& p, cudaStream_t s) {

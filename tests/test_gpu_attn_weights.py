@@ -93,11 +93,11 @@ def test_many_queries(G, n):
 
 
 @pytest.mark.parametrize("r,G,n,ps,cap", [
-    (16, 4, 16, 0, 1312), (16, 8, 40, 64, 1536), (32, 8, 64, 16, 1536), (32, 2, 50, 0, 1312),
-    (64, 4, 16, 0, 1312), (64, 4, 32, 16, 1536), (64, 1, 65, 64, 1536), (64, 8, 64, 128, 1536), (64, 2, 200, 256, 1536),
+    (16, 4, 32, 0, 1312), (16, 8, 40, 64, 1536), (32, 8, 64, 16, 1536), (32, 2, 64, 0, 1312),
+    (64, 4, 12, 0, 1312), (128, 4, 8, 16, 1536), (64, 4, 32, 16, 1536), (64, 1, 65, 64, 1536), (64, 8, 64, 128, 1536), (64, 2, 200, 256, 1536),
     (128, 2, 32, 0, 1328), (128, 8, 64, 32, 1536), (128, 4, 33, 128, 1536), (128, 4, 100, 0, 1504)])
 def test_tiles_of_many_queries(r, G, n, ps, cap):
-    """From 64 rows of bf16 keys on: products of 128 x 128 tiles.  Contexts of less than a tile,
+    """Rows of bf16 keys enough for products of 128 x 128 tiles.  Contexts of less than a tile,
     of one, and that end inside one; rows that see nothing; row tiles that are not full."""
     lens = [0, 1, 63, 127, 128, 129, 640, 1000, 1300]
     x = Cache(lens, 2 * G, 2, r, 64, cap, ps, "bf16", seed=r + n)

@@ -4,7 +4,9 @@ Tolerance, derived: with A = scale log2e max |q_i| . |k_i| (the largest sum of m
 a score of r / 16 steps is off by at most (r / 16) 17 2^-23 A on the tensor cores, and by 3 2^-24 A
 for the scale, its product and the difference with the maximum; two such errors meet in a weight
 (its own and, averaged, those of the sum), ln 2 each, with 2^-22 for each exponential and 2^-24
-for each of the log2(L) + 16 levels of a sum of positive terms."""
+for each of the log2(L) + 16 levels of a sum of positive terms.  Where a row is one number,
+maximum + log2 of the sum, that rounds by 2^-24 (A + log2 L): the difference's 2^-24 A, and ln 2
+log2(L) 2^-24 among the levels."""
 
 import math
 

@@ -27,7 +27,7 @@ __device__ __forceinline__ Range range_of(const WeightsParams& p, long long bloc
   r.pair = block / splits;
   r.b = static_cast<int>(r.pair / p.at.Hkv);
   r.g = static_cast<int>(r.pair % p.at.Hkv);
-  r.L = checked_len(p.seq_lens[r.b], p.at);
+  r.L = checked_len(__ldcg(p.seq_lens + r.b), p.at);
   const long long from = block % splits * per_cta;
   r.from = static_cast<int>(min(from, static_cast<long long>(r.L)));
   r.to = static_cast<int>(min(from + per_cta, static_cast<long long>(r.L)));

@@ -13,7 +13,7 @@
 // thread's wait, TMEM load, maximum and exponentials follow one another (some 270, 150 and
 // 1200 cycles an item, four warps an SM quarter), and waits and exponentials share a queue.
 // About 8 us of a call are two launches, prologues, first loads and the rows' join.
-// Measured, 32 queries of 4 heads on 2 x 16381 tokens, r = 64: 24.2 us (mma.sync: 42.4,
+// Measured, 32 queries of 4 heads on 2 x 16381 tokens, r = 64: 24.4 us (mma.sync: 42.4,
 // bound by 18 cycles a product and SM quarter).  Without any exponential or maximum the
 // first launch would gain 1.1 us, the second 4.  Not kept: eight softmax warps (33.4 us),
 // loads of the next 32 columns ahead of the exponentials (25.6), one arrival a warp
@@ -67,7 +67,7 @@ __device__ __forceinline__ void load_keys(const WeightMaps& maps, const WeightsP
     const int t = t0 + lane * rows_per_box;
     int page = -1;                         // past the context: the zero fill
     if (lane < kTile / rows_per_box && t < r.L) {
-      page = m.page_table[static_cast<long long>(r.b) * m.max_pages + (t >> m.page_shift)];
+      page = __ldcg(m.page_table + static_cast<long long>(r.b) * m.max_pages + (t >> m.page_shift));
       if (page < 0 || page >= m.num_pages) {
         record_error(m.err, TK_DEVERR_INDEX);
         page = -1;
@@ -307,7 +307,8 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
   const uint32_t tmem = tmem_slot;
   pdl_trigger();
   // What the first launch did not write can be read before it ends: its blocks have waited
-  // for everything before it.
+  // for everything before it.  From the L2, by TMA or __ldcg: a line of this SM's L1 may be
+  // older than that.
   const Range r = range_of(p, blockIdx.x, p.sum_splits, p.sum_per_cta);
   const int tiles = (r.to - r.from + kTile - 1) / kTile;
   // item n: tiles 2 (n / row_tiles) and the next with row tile n % row_tiles, in buffers n & 1

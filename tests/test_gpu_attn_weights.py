@@ -253,3 +253,26 @@ def test_the_same_bits_again_and_through_a_graph():
     q = _queries(2, 8, 2, 32, 11)
     with pytest.raises(tb.TkError, match="TK_ERR_WORKSPACE"):
         tb.tk_attn_weights(x.c, q, x.seq, 3000, b, tb.attn_weights_workspace(x.c, 3000, 2)[:256])
+
+
+def test_tiles_of_many_queries_behind_changing_lengths_and_keys():
+    """Steps in a row, each with new lengths, keys and a new page, as with a wait between them."""
+    def run(wait):
+        x = Cache([700, 130], 8, 2, 64, 64, 1024, 16, "bf16", seed=15)
+        keys, w, ws = x.c.k, tb.slot_weights(x.c), tb.attn_weights_workspace(x.c, 1024, 16)
+        keys.nan_to_num_(0.25)
+        q, seq, old = _queries(2, 8, 16, 64, 14), x.seq.clone(), x.seq.clone()
+        for step in range(12):
+            old.copy_(seq)
+            seq.add_(16)
+            keys.mul_(-1)
+            x.c.page_table[:, 3:5] = x.c.page_table[:, 3:5].flip(1)
+            if wait:
+                torch.cuda.synchronize()
+            tb.tk_attn_weights(x.c, q, seq, 1024, w, ws, old, 0.75)
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return w
+    a, b = run(False), run(True)
+    assert torch.equal(bits(a), bits(b)) and a.sum() > 0

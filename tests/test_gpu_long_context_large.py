@@ -207,3 +207,41 @@ def test_wrong_shapes_and_types_are_refused():
                                            pool=tb.PagePool.allocate(1, 4, 16, x.c.desc.num_pages))):
         with pytest.raises((ValueError, TypeError, tb.TkError)):
             call()
+
+
+def test_many_queries_beyond_32_bit_offsets():
+    """As above for the weights of 64 queries, whose key tiles come through a tensor map."""
+    B, hq, hkv, r, L, n = 3, 4, 2, 128, 300, 64
+    cap = (2 ** 32 // 128 // 5 // 64 + 1) * 64
+    c = tb.ThinKeyCache.allocate(B, hq, hkv, r, 64, capacity=cap)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    c.k[2, :, :L] = torch.randn(hkv, L, r, device="cuda", generator=g).to(torch.bfloat16)
+    q = torch.randn(B, hq, n, r, device="cuda", generator=g).to(torch.bfloat16)
+    w = tb.slot_weights(c)
+    tb.tk_attn_weights(c, q, i32([0, 0, L]), 512, w, tb.attn_weights_workspace(c, 512, n))
+    for h in range(hkv):
+        ref = lc.attn_weights(f64(q)[2, 2 * h:2 * h + 2], f64(c.k[2, h, :L]), 1 / math.sqrt(r), n)
+        assert np.allclose(f64(w[2, h, :L]), ref, rtol=1e-3, atol=0) and (w[2, h, L:512] == 0).all()
+    assert (w[:2] == 0).all()
+
+
+def test_many_queries_beside_prefills_on_another_stream():
+    """Both hold tensor memory: calls that overlap give what they give alone."""
+    x = Cache([2000, 1500, 900], 8, 2, 64, 64, 2048, 16, "bf16", seed=50)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    qw = torch.randn(3, 8, 32, 64, device="cuda", generator=g).to(torch.bfloat16)
+    q, k, v = (torch.randn(2, h, 1024, 64, device="cuda", generator=g).to(torch.bfloat16) for h in (8, 2, 2))
+    ws, w = tb.attn_weights_workspace(x.c, 2048, 32), [tb.slot_weights(x.c) for _ in range(2)]
+    out = [torch.empty(2, 8, 1024, 64, device="cuda") for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(2):                       # alone, then both streams at once
+        for _ in range(20):
+            tb.tk_attn_weights(x.c, qw, x.seq, 2048, w[i], ws, x.seq, 0.5, stream=streams[0])
+            if i == 0:
+                streams[0].synchronize()
+            tb.tk_attn_prefill(q, k, v, out[i], stream=streams[1])
+            if i == 0:
+                streams[1].synchronize()
+        torch.cuda.synchronize()
+    assert torch.equal(bits(w[0]), bits(w[1])) and torch.equal(bits(out[0]), bits(out[1])) and w[0].sum() > 0

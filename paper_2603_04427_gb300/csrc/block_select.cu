@@ -40,12 +40,15 @@ constexpr int kMaxCluster = 8;
 constexpr int kCopies = 2;
 constexpr int kList = 64;          // keys of one bucket that are ranked instead of split further
 constexpr int kFew = 256;          // undecided blocks that are ranked by comparing all of them
-// Key of the blocks that are chosen whatever their score; above +inf's.
+// Key of the blocks that are chosen whatever their score; above that of any score.
 constexpr uint32_t kForced = 0xffffffffu;
+constexpr uint32_t kInfinite = 0xff800000u;   // of +inf
 
-// Order-preserving encodings (-0 as +0).
+// Order-preserving encodings (-0 as +0).  A NaN, which stands for a block that cannot be
+// ranked, has the key of +inf: its own bits could be those of kForced.
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
+  if (isnan(x)) return kInfinite;
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t k) {

@@ -337,10 +337,12 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) block_select_kernel
     if (top != kForced) {
       float big = 0.f;
       for (uint32_t r = 0; r < parts; ++r) big = fmaxf(big, sh.amax[r]);
+      // an infinite (or NaN) factor leaves scores that do not say what counts, also where
+      // the other one is zero
+      if (isinf(big) || isinf(q1)) eps = INFINITY;
       // nothing is rounded where one factor is zero; elsewhere operands and products
       // below the normal range may be taken for zero
-      if (big != 0.f && q1 != 0.f) eps = big * q1 * kGamma + (big + q1) * 0x1p-120f + 0x1p-100f;
-      if (isnan(eps)) eps = INFINITY;
+      else if (big != 0.f && q1 != 0.f) eps = big * q1 * kGamma + (big + q1) * 0x1p-120f + 0x1p-100f;
     }
     if (eps == 0.f) {
       over = mask([&](int j) { return k[j] > top; });

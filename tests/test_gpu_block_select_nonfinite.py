@@ -120,3 +120,30 @@ def test_from_keys_with_nans(G, k):
     box = tb.block_bounds(x.c, 16)
     tb.tk_block_bounds(x.c, box, x.seq, block=16)
     _check(x, box.cpu().view(-1, 2, 32), _queries(x, 6), 7)
+
+
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+def test_zero_queries_and_infinite_bounds(G):
+    """0 times infinity is no score: such a block counts as the largest, although every finite one
+    scores 0."""
+    x = _cache(G, 40)
+    box = _boxes(x, 21)
+    box[7::9, 0, 3] = -INF
+    box[8::9, 1, 4] = NAN
+    q = torch.zeros(x.B, x.h_q, x.r, dtype=torch.bfloat16)
+    for n in (4, 8, 20):
+        _check(x, box, q, n)
+    q[:, G:] = _queries(x, 22)[:, G:]                   # of one kv head alone
+    _check(x, box, q, 8)
+
+
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+def test_zero_bounds_and_infinite_queries(G):
+    """Blocks whose bounds are all zero, with queries of infinities and NaNs: nothing can be ranked."""
+    x = _cache(G, 40)
+    box = torch.zeros_like(_boxes(x, 1))
+    q = _queries(x, 23)
+    q[0, :, 2], q[1, 0, 3] = INF, NAN
+    _check(x, box, q, 8)
+    box[11, 1, 2] = 1.0
+    _check(x, box, q, 8)

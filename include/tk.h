@@ -582,8 +582,9 @@ tk_status tk_attn_decode_blocks(const tk_cache_desc* desc, int32_t block, const 
                                 void* workspace, size_t workspace_bytes, void* stream);
 
 /* Bytes of workspace of tk_attn_weights on the current device; 0 for invalid
- * arguments.  Scratch: reusable in stream order, never by two calls that may
- * run concurrently.                                                         */
+ * arguments.  One for a larger max_seq_len serves every smaller one (of the
+ * same cache and n_q).  Scratch: reusable in stream order, never by two calls
+ * that may run concurrently.                                                */
 size_t tk_attn_weights_workspace_size(const tk_cache_desc* desc, int32_t n_q, int32_t max_seq_len);
 
 /* Adds the attention weights of n_q queries per sequence up per cached token:

@@ -1059,7 +1059,7 @@ def slot_weights(cache: ThinKeyCache) -> torch.Tensor:
 
 
 def attn_weights_workspace(cache: ThinKeyCache, max_seq_len: int, n_queries: int = 1) -> torch.Tensor:
-    """A workspace of the size tk_attn_weights needs."""
+    """A workspace of the size tk_attn_weights needs for contexts of max_seq_len tokens or fewer."""
     dev = _device(cache.k, "cache.k")
     _need_current(dev.index)
     n = int(load_library().tk_attn_weights_workspace_size(ctypes.byref(cache.desc), int(n_queries), int(max_seq_len)))

@@ -764,6 +764,15 @@ cudaError_t launch_t(const WeightsParams& p, cudaStream_t s) {
   return launch_pdl(kern, grid, dim3(kThreads), smem, s, p);
 }
 
+// Bytes of the statistics.  A block's tokens are rounded up to whole tiles (`unit`), so that
+// a longer context may have fewer blocks than a shorter one; the bytes are those of as many
+// as were asked for, or of one for each tile if these are fewer: never less than the plan's
+// blocks need, and never less for a longer context.
+size_t stat_bytes(const WeightsParams& p, long long asked, long long limit, int unit) {
+  const long long splits = std::min(asked, (limit + unit - 1) / unit);
+  return (static_cast<size_t>(p.B) * p.at.Hkv * splits * p.rows * sizeof(float2) + 255) / 256 * 256;
+}
+
 }  // namespace
 
 size_t plan_weights(WeightsParams* p, int num_sms) {
@@ -784,30 +793,30 @@ size_t plan_weights(WeightsParams* p, int num_sms) {
   if (weights_on_tcgen05(*p)) {
     // one block an SM: tiles of 128 tokens for a tile of 128 rows, or for all rows
     p->tensor = 1;
-    auto tiles = [&](long long copies) {
-      const long long splits = std::max(1ll, num_sms / (pairs * copies));
-      return static_cast<int>(((limit + splits - 1) / splits + 127) / 128 * 128);
-    };
-    p->per_cta = tiles((p->rows + 127) / 128);
-    p->sum_per_cta = tiles(1);
+    auto want = [&](long long copies) { return std::max(1ll, num_sms / (pairs * copies)); };
+    auto tiles = [&](long long splits) { return static_cast<int>(((limit + splits - 1) / splits + 127) / 128 * 128); };
+    const long long splits = want((p->rows + 127) / 128);
+    p->per_cta = tiles(splits);
+    p->sum_per_cta = tiles(want(1));
     p->splits = static_cast<int>((limit + p->per_cta - 1) / p->per_cta);
     p->sum_splits = static_cast<int>((limit + p->sum_per_cta - 1) / p->sum_per_cta);
-    return (static_cast<size_t>(pairs) * p->splits * p->rows * sizeof(float2) + 255) / 256 * 256;
+    return stat_bytes(*p, splits, limit, 128);
   }
   // as many blocks as run at once, each warp with at least one stage of keys
   const int step = kWarps * 8 * (p->R <= 32 ? 8 : (p->R == 64 ? 4 : 2));
-  auto range = [&](long long copies, int per_sm) {
-    const long long splits = std::max(1ll, per_sm * num_sms / (pairs * copies));
+  auto want = [&](long long copies, int per_sm) { return std::max(1ll, per_sm * num_sms / (pairs * copies)); };
+  auto range = [&](long long splits) {
     const long long per = (limit + splits - 1) / splits;
     return static_cast<int>((per + step - 1) / step * step);
   };
   const int per_sm = p->n_q > 1 && p->R == 64 ? 3 : 2;
-  p->per_cta = range(((p->rows + 15) / 16 + kGroup - 1) / kGroup, per_sm);
-  p->sum_per_cta = range(1, p->n_q == 1 && p->rows <= 4 ? 4 : 2);
+  const long long splits = want(((p->rows + 15) / 16 + kGroup - 1) / kGroup, per_sm);
+  p->per_cta = range(splits);
+  p->sum_per_cta = range(want(1, p->n_q == 1 && p->rows <= 4 ? 4 : 2));
   p->splits = static_cast<int>((limit + p->per_cta - 1) / p->per_cta);
   p->sum_splits = static_cast<int>((limit + p->sum_per_cta - 1) / p->sum_per_cta);
   p->store = p->n_q == 1;
-  const size_t stats = (static_cast<size_t>(pairs) * p->splits * p->rows * sizeof(float2) + 255) / 256 * 256;
+  const size_t stats = stat_bytes(*p, splits, limit, step);
   return stats + (p->store ? static_cast<size_t>(pairs) * p->rows * ((limit + 15) / 16 * 16) * sizeof(float) : 0);
 }
 

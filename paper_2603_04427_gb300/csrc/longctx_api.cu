@@ -106,10 +106,14 @@ tk_status blocks_desc(const tk_cache_desc* d, int32_t block, int32_t n_select, t
 tk_status weights_plan(const tk_cache_desc* d, int32_t n_q, int32_t max_seq_len, tk::WeightsParams* p, size_t* bytes) {
   TK_TRY(check_sizes(d));
   const int G = d->h_q / d->h_kv;
-  if (n_q < 0 || max_seq_len < 0) return fail(TK_ERR_INVALID_ARG, "n_q=%d max_seq_len=%d", n_q, max_seq_len);
+  if (n_q < 1 || max_seq_len < 0) return fail(TK_ERR_INVALID_ARG, "n_q=%d max_seq_len=%d", n_q, max_seq_len);
   if (static_cast<int64_t>(G) * n_q > tk::kMaxWeightRows)
     return fail(TK_ERR_UNSUPPORTED, "n_q * h_q / h_kv = %lld (at most %d)", static_cast<long long>(G) * n_q,
                 tk::kMaxWeightRows);
+  if (d->batch == 0) {                   // nothing to plan
+    *bytes = 0;
+    return TK_OK;
+  }
   DeviceInfo dev;
   TK_TRY(device_info(&dev));
   p->at = slot_map(d, nullptr, max_seq_len, dev.err);

@@ -256,13 +256,18 @@ __global__ void __launch_bounds__(kThreads, STORE ? 2 : kPerSm<R>) weights_stats
   stage_queries<R, KF>(p, r.pair, tile0, tiles, sq);
   __syncthreads();
   const float u = unit<KF>(p);
-  float m[GROUP][H], l[GROUP][H];
+  // maximum m; the sum l is of exponentials of scores + z, where z = -m in log2 units, rounded:
+  // a step rescales l by the difference of two z, which is nothing where the maximum stays.
+  // (By the unrounded maximum, each step would multiply l by the rounding once more: 1e-3 after
+  // 128 steps at a maximum of 500.)
+  float m[GROUP][H], l[GROUP][H], z[GROUP][H];
 #pragma unroll
   for (int c = 0; c < GROUP; ++c) {
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       m[c][h] = -INFINITY;
       l[c][h] = 0.f;
+      z[c][h] = INFINITY;
     }
   }
   for (; t0 < r.to; t0 += STEP) {
@@ -308,11 +313,12 @@ __global__ void __launch_bounds__(kThreads, STORE ? 2 : kPerSm<R>) weights_stats
 #pragma unroll
         for (int i = 0; i < TILES; ++i) n = fmaxf(n, fmaxf(s[i][2 * h], s[i][2 * h + 1]));
         // no score above -inf: exponentials of zero maximum, which a NaN survives
-        const float z = n == -INFINITY ? 0.f : -n * u;
+        const float y = n == -INFINITY ? 0.f : -n * u;
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) sum += fast_exp2(fmaf(s[i][2 * h], u, z)) + fast_exp2(fmaf(s[i][2 * h + 1], u, z));
-        l[c][h] = fmaf(l[c][h], fast_exp2(fmaf(m[c][h], u, z)), sum);
+        for (int i = 0; i < TILES; ++i) sum += fast_exp2(fmaf(s[i][2 * h], u, y)) + fast_exp2(fmaf(s[i][2 * h + 1], u, y));
+        l[c][h] = fmaf(l[c][h], fast_exp2(y - z[c][h]), sum);
+        z[c][h] = n == -INFINITY ? INFINITY : y;
         m[c][h] = n;
       }
     }

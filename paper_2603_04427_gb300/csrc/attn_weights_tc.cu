@@ -208,6 +208,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const float u = p.unit;
     const float sign = p.scale_log2 < 0.f ? -1.f : (p.scale_log2 == 0.f ? 0.f : 1.f);
+    // l is of exponentials of scores + z, z = -m in log2 units, rounded; a step rescales it by
+    // the difference of two z, which is nothing where the maximum stays
+    float z = INFINITY;
     for (int j = x; j < tiles; j += 2) {
       const int buf = j % kBufs;
       if (!warp_wait(&s_full[buf], (j / kBufs) & 1, p.at.err)) break;
@@ -237,15 +240,16 @@ __global__ void __launch_bounds__(kThreads, 1) weights_stats_tc_kernel(const __g
       for (int i = 8; i + 1 < kHalf; i += 2) a[(i >> 1) & 7] = max3(a[(i >> 1) & 7], f(v[i]), f(v[i + 1]));
       const float n = max3(max3(a[0], a[1], a[2]), max3(a[3], a[4], a[5]), max3(m, a[6], a[7]));
       // no score above -inf: exponentials of zero maximum, which a NaN survives
-      const float z = n == -INFINITY ? 0.f : -n * u;
+      const float y = n == -INFINITY ? 0.f : -n * u;
       float2 e[4] = {{0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
       for (int i = 0; i < kHalf; i += 2) {
-        const float2 x2 = ffma2(make_float2(f(v[i]), f(v[i + 1])), make_float2(u, u), make_float2(z, z));
+        const float2 x2 = ffma2(make_float2(f(v[i]), f(v[i + 1])), make_float2(u, u), make_float2(y, y));
         e[(i >> 1) & 3] = fadd2(e[(i >> 1) & 3], exp2_2(x2));
       }
       const float2 sum = fadd2(fadd2(e[0], e[1]), fadd2(e[2], e[3]));
-      l = fmaf(l, fast_exp2(fmaf(m, u, z)), sum.x + sum.y);
+      l = fmaf(l, fast_exp2(y - z), sum.x + sum.y);
+      z = n == -INFINITY ? INFINITY : y;
       m = n;
     }
     m *= u;                                // log2 units from here on

@@ -3,9 +3,11 @@
 // Two launches that both compute the scores, as there: the first with query rows as the
 // MMA's M, so that a thread owns a row (a TMEM lane) and its maximum and sum need no other
 // thread; the second with tokens as M, so that a thread owns tokens and adds up their
-// weights over the rows.  A row is one number there, -(maximum + log2 of its sum), from
-// shared memory: a weight is one FMA, one exponential and one addition, and two tokens of
-// a thread share each load.  Either way the operands are K-major tiles of the same layout,
+// weights over the rows.  A row is two numbers there, -maximum and 1 / sum, from shared
+// memory: a weight is an FMA, an exponential and an FMA, and two tokens of a thread share each
+// load.  (As one number, -(maximum + log2 of the sum), 24.2 us, a row is rounded by its size:
+// 2e-5 of each weight at a maximum of 500, whose own rounding cancels with that of the sum's
+// terms.)  Either way the operands are K-major tiles of the same layout,
 // keys and queries just change places in the instruction.
 //
 // What bounds it: a tile of 128 x 128 scores takes the exponential units 512 cycles (a
@@ -13,7 +15,7 @@
 // thread's wait, TMEM load, maximum and exponentials follow one another (some 270, 150 and
 // 1200 cycles an item, four warps an SM quarter), and waits and exponentials share a queue.
 // About 8 us of a call are two launches, prologues, first loads and the rows' join.
-// Measured, 32 queries of 4 heads on 2 x 16381 tokens, r = 64: 24.4 us (mma.sync: 42.4,
+// Measured, 32 queries of 4 heads on 2 x 16381 tokens, r = 64: 24.9 us (mma.sync: 42.4,
 // bound by 18 cycles a product and SM quarter).  Without any exponential or maximum the
 // first launch would gain 1.1 us, the second 4.  Not kept: eight softmax warps (33.4 us),
 // loads of the next 32 columns ahead of the exponentials (25.6), one arrival a warp
@@ -21,8 +23,9 @@
 //
 // One block per SM.  Sixteen warps of softmax threads: two groups that take tiles in turn,
 // each in two halves of 64 columns (first launch), or all take pairs of tiles in quarters of
-// 32 rows (second); one warp for the TMA of key tiles into a ring, one for the products.  Scores pass through TMEM buffers of 128 columns, two for each group: its
-// threads copy one into registers and give it back before they work on it.
+// 32 rows (second); one warp for the TMA of key tiles into a ring, one for the products.
+// Scores pass through TMEM buffers of 128 columns, two for each group: its threads copy one
+// into registers and give it back before they work on it.
 #include <algorithm>
 
 #include "attn_weights.cuh"
@@ -272,10 +275,10 @@ constexpr int sum_stages(int row_tiles) {
   const int fit = 200 * 1024 / TCfg<R>::TILEB - row_tiles;
   return fit < kMaxStages ? fit : kMaxStages;
 }
-// Queries, keys; each row's exponent and last token.
+// Queries, keys; each row's maximum, sum and last token.
 template <int R>
 constexpr int sum_smem(int row_tiles) {
-  return (row_tiles + sum_stages<R>(row_tiles)) * TCfg<R>::TILEB + row_tiles * kTile * 8 + 1024;
+  return (row_tiles + sum_stages<R>(row_tiles)) * TCfg<R>::TILEB + row_tiles * kTile * 12 + 1024;
 }
 
 template <int R>
@@ -290,8 +293,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row_tiles = (p.rows + kTile - 1) / kTile, stages = sum_stages<R>(row_tiles);
   unsigned char* sk = smem + row_tiles * T::TILEB;
-  float* expo = reinterpret_cast<float*>(sk + stages * T::TILEB);   // -(maximum + log2 of the sum)
-  int* see = reinterpret_cast<int*>(expo + row_tiles * kTile);
+  float* neg_max = reinterpret_cast<float*>(sk + stages * T::TILEB);
+  float* inv = neg_max + row_tiles * kTile;                   // 1 / sum, 0 for a row that sees no token
+  int* see = reinterpret_cast<int*>(inv + row_tiles * kTile);
   if (tid == 0) {
     mbar_init(&q_full, 1);
     for (int i = 0; i < kMaxStages; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
@@ -368,10 +372,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
     // statistics of every row, by the softmax threads
     pdl_wait();
     if (tiles > 0) {
-      // one number a row: a weight is one exponential, and -inf where a row has no weight;
-      // the number's rounding is that of one more term of the row's sum
-      join_rows<kSoft>(p, r, row_tiles * kTile, [&](int row, float m, float inv, int last) {
-        expo[row] = log2f(inv) - m;
+      join_rows<kSoft>(p, r, row_tiles * kTile, [&](int row, float m, float i, int last) {
+        neg_max[row] = -m;
+        inv[row] = i;
         see[row] = last;
       });
     }
@@ -402,19 +405,20 @@ __global__ void __launch_bounds__(kThreads, 1) weights_sum_tc_kernel(const __gri
         if (!masked && row + kTile / 4 <= p.rows) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
-            const float4 x = *reinterpret_cast<const float4*>(expo + row + i);
-            a0 = fadd2(a0, exp2_2(ffma2(make_float2(f(v[i]), f(v[i + 1])), u, make_float2(x.x, x.y))));
-            b0 = fadd2(b0, exp2_2(ffma2(make_float2(f(v[i + 32]), f(v[i + 33])), u, make_float2(x.x, x.y))));
-            a1 = fadd2(a1, exp2_2(ffma2(make_float2(f(v[i + 2]), f(v[i + 3])), u, make_float2(x.z, x.w))));
-            b1 = fadd2(b1, exp2_2(ffma2(make_float2(f(v[i + 34]), f(v[i + 35])), u, make_float2(x.z, x.w))));
+            const float4 x = *reinterpret_cast<const float4*>(neg_max + row + i);
+            const float4 y = *reinterpret_cast<const float4*>(inv + row + i);
+            a0 = ffma2(exp2_2(ffma2(make_float2(f(v[i]), f(v[i + 1])), u, make_float2(x.x, x.y))), make_float2(y.x, y.y), a0);
+            b0 = ffma2(exp2_2(ffma2(make_float2(f(v[i + 32]), f(v[i + 33])), u, make_float2(x.x, x.y))), make_float2(y.x, y.y), b0);
+            a1 = ffma2(exp2_2(ffma2(make_float2(f(v[i + 2]), f(v[i + 3])), u, make_float2(x.z, x.w))), make_float2(y.z, y.w), a1);
+            b1 = ffma2(exp2_2(ffma2(make_float2(f(v[i + 34]), f(v[i + 35])), u, make_float2(x.z, x.w))), make_float2(y.z, y.w), b1);
           }
         } else if (row < p.rows) {
           // rows that do not see the token, and those past the last (whose zeros may
           // meet an infinite key)
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            const float x = fast_exp2(fmaf(f(v[i]), u.x, expo[row + i]));
-            const float y = fast_exp2(fmaf(f(v[i + 32]), u.x, expo[row + i]));
+            const float x = fast_exp2(fmaf(f(v[i]), u.x, neg_max[row + i])) * inv[row + i];
+            const float y = fast_exp2(fmaf(f(v[i + 32]), u.x, neg_max[row + i])) * inv[row + i];
             a0.x += ta > see[row + i] ? 0.f : x;
             b0.x += tb > see[row + i] ? 0.f : y;
           }

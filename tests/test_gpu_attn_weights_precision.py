@@ -72,10 +72,21 @@ def _tol(steps, scale):
     (2, 8, 1, 32, 4096, 4096, 8),              # one query in one launch
     (304, 8, 1, 16, 65536, 65536, 128),        # with its scores kept: steps of 512 tokens
     (304, 4, 3, 32, 16384, 16381, 32),         # more on mma.sync
-    (304, 8, 2, 64, 16384, 16000, 63)])
+    (304, 8, 2, 64, 16384, 16000, 63),
+    (152, 8, 16, 16, 16384, 16384, 64),        # on tcgen05: two groups in turn, tiles of 128 tokens
+    (152, 8, 8, 64, 16384, 15999, 63)])
 def test_sums_over_many_steps(B, G, n_q, r, cap, L, steps, scale):
     """One range holds a whole context: a thread's running sum goes through many steps, whose maximum is
     the same."""
     got, want = _run(B, G, n_q, r, cap, L, scale)
     err = np.abs(got / want - 1).max()
     assert err <= _tol(steps, scale), (err, _tol(steps, scale))
+
+
+@pytest.mark.parametrize("scale", SCALES + [0.5, 0.9])
+@pytest.mark.parametrize("G,n_q,r,L", [(8, 16, 16, 100), (8, 6, 64, 128), (4, 8, 128, 90), (8, 64, 32, 128)])
+def test_tiles_of_many_queries_of_one_step(G, n_q, r, L, scale):
+    """Products on tcgen05, every row in one step: what is left is how its maximum and sum are kept."""
+    got, want = _run(1, G, n_q, r, 128, L, scale)
+    err = np.abs(got / want - 1).max()
+    assert err <= _tol(1, scale), (err, _tol(1, scale))

@@ -573,8 +573,8 @@ size_t tk_decode_blocks_workspace_size(const tk_cache_desc* desc, int32_t block,
  *              in any order, all but the last full; lens 0 gives a zero row)
  *   workspace: tk_decode_blocks_workspace_size bytes, 256-byte aligned
  *   The other arguments and errors are those of tk_attn_decode.  A table entry
- *   out of range is read as block 0 of the cache and sets the device error word
- *   (of blocks of 16 or 32 tokens only one that begins a run of 64 tokens does).
+ *   out of range within lens is read as block 0 of the cache and sets the device
+ *   error word; those past it are not looked at.
  *   One launch for every 1024 / h_kv sequences.                              */
 tk_status tk_attn_decode_blocks(const tk_cache_desc* desc, int32_t block, const void* q, const void* k_cache,
                                 const void* v_cache, const float* k_scale, const int32_t* table,

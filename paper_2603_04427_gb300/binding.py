@@ -1159,7 +1159,8 @@ def tk_cache_evict(cache: ThinKeyCache, seq_lens, max_seq_len: int, weights, n_k
 def prepare_cache_evict(cache: ThinKeyCache, seq_lens, max_seq_len: int, weights, n_keep: int, n_recent: int,
                         workspace, weights_out=None, seq_lens_out=None, kept=None, pool: PagePool | None = None,
                         stream=None, graph: bool = False) -> PreparedCall:
-    """tk_cache_evict on fixed buffers, checked and marshalled once (see PreparedCall)."""
+    """tk_cache_evict on fixed buffers, checked and marshalled once (see PreparedCall).  With
+    graph=True preparing evicts once, so contexts that are over n_keep by then are cut."""
     args, keep = _evict_args(cache, seq_lens, max_seq_len, weights, n_keep, n_recent, workspace, weights_out,
                              seq_lens_out, kept, pool, stream)
     return PreparedCall("tk_cache_evict", args, keep, graph=graph, stream=stream)

@@ -466,10 +466,10 @@ cudaError_t launch_t(const WeightsParams& p, cudaStream_t s) {
 // Keys in bf16, as the MMA takes them, and rows enough that a tile that is partly empty
 // costs less than mma.sync.  Measured, us, this form and the other, on 2 x 16381 tokens
 // and on 32 x 4096, 8 kv heads:
-//   r = 16:  64 rows 20.7 : 16.3, 69.9 : 49.4    128 rows 22.5 : 24.4, 77.3 : 79.9
-//   r = 32:  64 rows 20.9 : 19.2, 71.3 : 57.9    128 rows 22.7 : 28.6, 78.5 : 95.0
-//   r = 64:  32 rows 20.8 : 22.4, 69.2 : 66.2     48 rows 22.9 : 25.8, 76.6 : 83.7
-//   r = 128: 16 rows 26.2 : 26.0, 93.0 : 88.5     32 rows 25.7 : 30.8, 92.5 : 101.7
+//   r = 16:  64 rows 21.2 : 16.7, 72.5 : 50.3    128 rows 23.2 : 24.8, 80.7 : 81.5
+//   r = 32:  64 rows 21.6 : 19.1, 75.1 : 58.3    128 rows 23.7 : 28.7, 83.5 : 96.0
+//   r = 64:  32 rows 21.6 : 22.8, 70.2 : 66.5     48 rows 23.9 : 26.0, 79.8 : 81.7
+//   r = 128: 16 rows 26.8 : 25.9, 93.7 : 88.8     32 rows 25.8 : 30.8, 92.8 : 102.6
 bool weights_on_tcgen05(const WeightsParams& p) {
   const long long planes = static_cast<long long>(p.at.page_size ? p.at.num_pages : p.B) * p.at.Hkv;
   return p.k_fmt == 0 && p.n_q > 1 && p.rows >= (p.R <= 32 ? 128 : (p.R == 64 ? 48 : 32)) && planes < (1ll << 31);

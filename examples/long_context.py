@@ -95,20 +95,22 @@ class BudgetServer(_Server):
 
     def admit(self, prompts):
         outs = super().admit(prompts)
-        layer, n = self.layer, self.window
-        # the prompts' last queries, again (a real engine has them at hand)
-        q = torch.zeros(self.batch, layer.h_q, n, layer.r, dtype=torch.bfloat16, device="cuda")
-        for b, x in enumerate(prompts):
-            if x is None:
-                continue
-            tail = x[-n:]
-            pos = self.seen[b] - tail.shape[0] + torch.arange(tail.shape[0], dtype=torch.int32, device="cuda")
-            q[b, :, n - tail.shape[0]:] = layer.rotated((tail @ layer.w)[None], pos[None])[0][0]
-        # sequences without a prompt keep their weights: all their tokens have one already
-        started = torch.tensor([x is not None for x in prompts], device="cuda")
-        fresh = torch.where(started, self.pool.seq_lens, 0).to(torch.int32)
-        tk.tk_attn_weights(self.cache, q, fresh, self.max_len, self.weights,
-                           tk.attn_weights_workspace(self.cache, self.max_len, n), old_lens=self.old)
+        layer = self.layer
+        tails = [0 if x is None else min(self.window, x.shape[0]) for x in prompts]
+        # a call for the prompts of each number of queries: those of a prompt that goes on from
+        # cached tokens are its own alone
+        for n in sorted(set(tails) - {0}):
+            # the prompts' last queries, again (a real engine has them at hand)
+            q = torch.zeros(self.batch, layer.h_q, n, layer.r, dtype=torch.bfloat16, device="cuda")
+            for b, x in enumerate(prompts):
+                if tails[b] == n:
+                    pos = self.seen[b] - n + torch.arange(n, dtype=torch.int32, device="cuda")
+                    q[b] = layer.rotated((x[-n:] @ layer.w)[None], pos[None])[0][0]
+            # the other sequences keep their weights, or get them by a call of their own
+            these = torch.tensor([t == n for t in tails], device="cuda")
+            lens = torch.where(these, self.pool.seq_lens, 0).to(torch.int32)
+            tk.tk_attn_weights(self.cache, q, lens, self.max_len, self.weights,
+                               tk.attn_weights_workspace(self.cache, self.max_len, n), old_lens=self.old)
         self.evict()
         return outs
 

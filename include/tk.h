@@ -606,7 +606,8 @@ size_t tk_attn_weights_workspace_size(const tk_cache_desc* desc, int32_t n_q, in
  *   workspace: tk_attn_weights_workspace_size bytes, 256-byte aligned
  * Sums in fp32, in an order fixed by the sizes and the device's SM count.  A score
  * of +infinity or NaN makes its kv head's weights NaN, one of -infinity is a weight
- * of zero.  One launch (one query, and scores of a context that shared memory holds) or
+ * of zero.  A finite score has to be below 2^30 in size, in units of log 2 (scale q . k
+ * log2(e)); a larger one can make its kv head's weights NaN.  One launch (one query, and scores of a context that shared memory holds) or
  * two, with programmatic dependent launch.                                  */
 tk_status tk_attn_weights(const tk_cache_desc* desc, const void* q, int32_t n_q, const void* k_cache,
                           const float* k_scale, const int32_t* page_table, const int32_t* old_lens,

@@ -90,3 +90,24 @@ def test_tiles_of_many_queries_of_one_step(G, n_q, r, L, scale):
     got, want = _run(1, G, n_q, r, 128, L, scale)
     err = np.abs(got / want - 1).max()
     assert err <= _tol(1, scale), (err, _tol(1, scale))
+
+
+@pytest.mark.parametrize("n_q", [1, 3, 16])
+@pytest.mark.parametrize("size", [1e2, 1e3, 1e4])
+def test_scores_up_to_the_largest(n_q, size):
+    """Random keys and queries of a size that gives scores of up to 6e8 log2 units (below 2^30): a row has
+    nearly all of its weight on one token, and a sum of one."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    desc = tb.tk_cache_desc(1, 8, 1, 32, 64, 112, 0, 0, 0, tb.TK_BF16)
+    keys = (size * torch.randn(1, 1, 112, 32, device="cuda", generator=gen)).to(torch.bfloat16)
+    q = (size * torch.randn(1, 8, n_q, 32, device="cuda", generator=gen)).to(torch.bfloat16)
+    c = tb.ThinKeyCache(desc, keys, None, None, None)
+    w = tb.slot_weights(c)
+    tb.tk_attn_weights(c, q, torch.tensor([100], dtype=torch.int32, device="cuda"), 100, w,
+                       tb.attn_weights_workspace(c, 100, n_q))
+    w = w[0, 0].double().cpu().numpy()
+    x = np.abs((q[0].double() @ keys[0, 0, :100].double().T).cpu().numpy()).max() / math.sqrt(32) * math.log2(math.e)
+    assert x < 2.0 ** 30 and (w >= 0).all() and (w[100:] == 0).all()
+    # a row's weights are its terms over their own sum: two exponentials, the sums' levels and the
+    # division, all of them positive
+    assert abs(w.sum() / (8 * n_q) - 1) <= 4 * 2.0 ** -22 + 40 * 2.0 ** -24

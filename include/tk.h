@@ -525,11 +525,11 @@ tk_status tk_block_tables(int32_t batch, int32_t page_size, int32_t num_pages,
  *   bounds   : device bf16, a minimum of r numbers and a maximum of r numbers per
  *              block and kv head: [num_pages][h_kv][2][r] (paged) or
  *              [batch][h_kv][capacity / block][2][r]; others are not written
- * Quantised keys count as code * k_scale.  A bound is the nearest bf16 number on
- * the outer side (bf16 keys: exact); an element that is NaN in a key is bounded
- * by -infinity and +infinity.  Tokens past seq_lens take no part.  A block on a
- * page that is out of range is not bounded.  Launched with programmatic
- * dependent launch (see tk_attn_decode).                                     */
+ * Quantised keys count as code * k_scale, exactly.  A bound is the nearest bf16
+ * number on the outer side (bf16 keys: exact); an element that is NaN in a key
+ * is bounded by -infinity and +infinity.  Tokens past seq_lens take no part.  A
+ * block on a page that is out of range is not bounded.  Launched with
+ * programmatic dependent launch (see tk_attn_decode).                        */
 tk_status tk_block_bounds(const tk_cache_desc* desc, int32_t block, const void* k_cache, const float* k_scale,
                           const int32_t* page_table, const int32_t* old_lens, const int32_t* seq_lens,
                           int32_t max_new, void* bounds, void* stream);
